@@ -12,7 +12,9 @@
  *   proximal step      Z  = S_t(W - eta*dW), t = eta*lambda        prox_l1_step
  *   recompression      Z -> CSR                   csr_recompress
  *   adaptive solvers   Prox-RMSProp / Prox-ADAM   prox_adaptive_step, prox_adaptive_recompress
+ *   orthogonalised     momentum and its prox step muon_update
  *   conv layers        direct sparse convolution  csr_conv_fwd, csr_conv_bwd_data, conv_im2col
+ *   losses             cross-entropy, policy, preference  l1csr_softmax_xent, l1csr_policy_loss, l1csr_preference_loss
  *
  * Conventions shared by every call
  *   - CSR: row_ptr[n_rows+1] (row_ptr[0] = 0, non-decreasing), col_idx[nnz]
@@ -63,7 +65,15 @@ enum l1csr_status {
 enum l1csr_precision {
     L1CSR_F32 = 0,           /* fp32 operands at full precision: the 1e-4 contract */
     L1CSR_BF16 = 1,          /* operands rounded to bf16 (nearest even), exact products, fp32 sums */
-    L1CSR_BF16X3 = 2         /* operands split into bf16 hi + lo, three exact products, fp32 sums */
+    L1CSR_BF16X3 = 2,        /* operands split into bf16 hi + lo, three exact products, fp32 sums */
+    L1CSR_F16 = 3            /* muon_update: operands rounded to fp16, one exact product, fp32 sums */
+};
+
+/* element types of the calls that take more than float (muon_update, the losses over logits) */
+enum l1csr_dtype {
+    L1CSR_DTYPE_F32 = 0,
+    L1CSR_DTYPE_BF16 = 1,
+    L1CSR_DTYPE_F16 = 2
 };
 
 /* prox_l1_step modes */
@@ -92,7 +102,10 @@ enum l1csr_op {
     L1CSR_OP_WGRAD_PACKED = 10, /* dense_wgrad / dense_wgrad_prox with packed operands (nnz unused) */
     L1CSR_OP_SDDMM_PACKED = 11, /* sddmm_masked_wgrad over a dense pattern, packed operands */
     L1CSR_OP_SPMM_PACKED = 12,  /* csr_spmm_fwd / csr_spmm_bwd_t over a dense pattern, packed operands */
-    L1CSR_OP_PROX_DENSE = 13    /* prox_adaptive_recompress, dense result kept (nnz, B unused) */
+    L1CSR_OP_PROX_DENSE = 13,   /* prox_adaptive_recompress, dense result kept (nnz, B unused) */
+    L1CSR_OP_MUON = 14,         /* muon_update, L1CSR_F32 (nnz, B unused) */
+    L1CSR_OP_MUON_F16 = 15,     /* muon_update, L1CSR_F16 */
+    L1CSR_OP_TOKEN_LOSS = 16    /* l1csr_token_logp / _policy_loss / _preference_loss: n_rows = C, n_cols = pairs, B */
 };
 
 /* Human-readable name of a status code (static string, never NULL). */
@@ -581,6 +594,84 @@ int l1csr_relu_bwd(int64_t n, const float *x, const float *dy, float *dx, hipStr
 int l1csr_softmax_xent(int32_t C, int32_t B, const float *logits, int64_t ld,
                        const int32_t *labels, float *dlogits, float *loss,
                        void *ws, size_t ws_bytes, hipStream_t stream);
+
+/*
+ * Orthogonalised momentum (the Muon update: K. Jordan et al., 2024), the step
+ * that prox_l1_step / prox_l1_recompress then take as their gradient:
+ *     M' = mu M + G
+ *     U  = G + mu M' (nesterov != 0) or M';  U = G if M is NULL
+ *     X  = U / (|U|_F + eps)         (the transpose if N > K)
+ *     `steps` times: A = X X^T,  X <- a X + (b A + c A^2) X,
+ *         (a, b, c) = (3.4445, -4.7750, 2.0315)
+ *     O  = scale X
+ * G [N][ldg] and O [N][ldo] are of `dtype` (l1csr_dtype), M [N][ldm] and M_out
+ * [N][ldmo] float.  M_out receives M' (NULL: not stored; may be M itself with
+ * the same leading dimension); O may be G itself with the same leading
+ * dimension; the arrays may not overlap otherwise (L1CSR_EINVAL).  0 <= mu < 1
+ * (ignored without M), 1 <= steps <= L1CSR_MUON_MAX_STEPS, eps >= 0, scale finite.
+ * |U|_F is summed in double.  precision L1CSR_F32: operands as two fp16 parts
+ * (22 bits), three exact products, fp32 sums; about 1e-6 of |O|_F off the exact
+ * result after five steps, as fp32 products are.  L1CSR_F16: one part, about
+ * 1.5e-3 off.  The accuracy is that of the whole matrix (relative to |O|_F), not
+ * of single small entries, and it needs a norm that is not lost against eps
+ * (|U|_F >= 1e-4 eps).  A zero U gives zeros; a NaN or an infinity anywhere in
+ * U gives NaN everywhere, as the formula does.  N * K < 2^31 and N, K <= 2^22
+ * (L1CSR_EUNSUPPORTED).  Results are reproducible.  ws as
+ * l1csr_workspace_bytes(L1CSR_OP_MUON or L1CSR_OP_MUON_F16, N, K, 0, 0).
+ */
+#define L1CSR_MUON_MAX_STEPS 32
+int muon_update(int32_t N, int32_t K, int dtype, const void *G, int64_t ldg, const float *M, int64_t ldm,
+                float *M_out, int64_t ldmo, float mu, int nesterov, int steps, float eps, float scale, int precision,
+                void *O, int64_t ldo, void *ws, size_t ws_bytes, hipStream_t stream);
+
+/*
+ * Losses on the log-probabilities of taken tokens, for logits[C][ld] of `dtype`
+ * (class-major, tokens contiguous, as l1csr_softmax_xent) and labels[B]:
+ *     lp_b = z[a_b][b] - log sum_c exp z[c][b],   a_b = labels[b]
+ * A token counts if its label lies in [0, C) and weights[b] != 0 (weights NULL:
+ * all 1).  The logits of a token that does not count are not used, whatever
+ * they hold; its lp is 0 and its column of dlogits is 0.  Logits of -infinity
+ * exclude a class.  Sums over tokens are in double; everything is reproducible.
+ * dlogits [C][ldd], of the type of the logits, receives d loss / d logits (every
+ * column of it; NULL: the loss alone); it may be the logits themselves (with the
+ * same leading dimension), but may not overlap them otherwise (L1CSR_EINVAL).
+ * ws as l1csr_workspace_bytes(L1CSR_OP_TOKEN_LOSS, C, pairs, 0, B), pairs = 0 but
+ * for the preference loss.
+ *
+ * l1csr_token_logp: logp[b] = lp_b (weights do not apply).
+ *
+ * l1csr_policy_loss: the clipped policy loss with a penalty on the distance
+ *   from a reference,
+ *     r = exp(lp - old_logp),  pg = -min(r adv, clip(r, 1 - clip_low, 1 + clip_high) adv)
+ *     kl = exp(ref_logp - lp) - (ref_logp - lp) - 1    (0 without ref_logp)
+ *     loss = sum_b w_b (pg_b + kl_coef kl_b) / sum_b w_b
+ *   old_logp, advantages [B]; ref_logp [B] or NULL.  stats[4] (device) = loss,
+ *   the mean pg, the mean kl and the share of clipped tokens (those whose
+ *   policy gradient is zero: adv > 0 and r > 1 + clip_high, or adv < 0 and
+ *   r < 1 - clip_low), all weighted; zeros if no token counts.  logp [B] (nullable)
+ *   receives lp.  0 <= clip_low <= 1, clip_high >= 0, kl_coef >= 0.
+ *
+ * l1csr_preference_loss: pairs of a preferred and a rejected sequence, tokens
+ *   seq_ptr[2p] .. seq_ptr[2p+1] - 1 and seq_ptr[2p+1] .. seq_ptr[2p+2] - 1
+ *   (seq_ptr[2 pairs + 1], device, not decreasing, within [0, B]; an empty sequence is
+ *   allowed),
+ *     reward_s = beta (sum_{b in s} w_b lp_b - ref_logp[s]),
+ *     D_p = reward_{2p} - reward_{2p+1},
+ *     loss = (1 / pairs) sum_p( -(1 - ls) log sig(D_p) - ls log sig(-D_p) )
+ *   with ls = label_smoothing in [0, 1/2], beta >= 0; ref_logp [2 pairs] or NULL (zeros).
+ *   rewards [2 pairs] (nullable) receives the rewards, *loss (device) the loss, 0 for
+ *   no pairs.  Columns of dlogits that belong to no sequence are 0.
+ */
+int l1csr_token_logp(int32_t C, int32_t B, int dtype, const void *logits, int64_t ld, const int32_t *labels,
+                     float *logp, void *ws, size_t ws_bytes, hipStream_t stream);
+int l1csr_policy_loss(int32_t C, int32_t B, int dtype, const void *logits, int64_t ld, const int32_t *labels,
+                      const float *old_logp, const float *advantages, const float *ref_logp, const float *weights,
+                      float clip_low, float clip_high, float kl_coef, void *dlogits, int64_t ldd, float *logp,
+                      float *stats, void *ws, size_t ws_bytes, hipStream_t stream);
+int l1csr_preference_loss(int32_t C, int32_t B, int dtype, const void *logits, int64_t ld, const int32_t *labels,
+                          int32_t pairs, const int32_t *seq_ptr, const float *ref_logp, const float *weights,
+                          float beta, float label_smoothing, void *dlogits, int64_t ldd, float *rewards, float *loss,
+                          void *ws, size_t ws_bytes, hipStream_t stream);
 
 #ifdef __cplusplus
 }

@@ -24,6 +24,8 @@ __all__ = [
     "l1_step", "side_stream", "prox_l1_recompress_noalloc", "dense_wgrad_prox", "csr_recompress_counted",
     "dense_wgrad_prox_recompress", "csr_bitmap_build", "Bitmap", "SpmmPlan", "csr_spmm_plan", "csr_spmm_planned",
     "csr_spmm_bwd_t_plan", "csr_spmm_bwd_t_planned",
+    "token_logp", "policy_loss", "preference_loss", "F16", "MuonState", "orthogonalize", "prox_muon_step",
+    "prox_muon_recompress",
 ]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libl1csr.so")
@@ -31,7 +33,7 @@ LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libl1csr.so
 OK, EINVAL, ECAPACITY, EBADCSR, EHIP, EUNSUPPORTED, ESCRATCH = 0, -1, -2, -3, -4, -5, -6
 NOALLOC_SCRATCH_BYTES = 16 << 20  # L1CSR_NOALLOC_SCRATCH_BYTES
 PROX_DENSE, PROX_CSR = 0, 1
-F32, BF16, BF16X3 = 0, 1, 2
+F32, BF16, BF16X3, F16 = 0, 1, 2, 3
 SOLVER_RMSPROP, SOLVER_ADAM = 1, 2
 OP_CSC_BUILD, OP_RECOMPRESS, OP_SDDMM, OP_SPMM, OP_COMPACT, OP_SOFTMAX_XENT = 1, 2, 3, 4, 5, 6
 OP_PROX_RECOMPRESS = 7
@@ -41,6 +43,10 @@ OP_WGRAD_PACKED = 10
 OP_SDDMM_PACKED = 11
 OP_SPMM_PACKED = 12
 OP_PROX_DENSE = 13
+OP_MUON = 14
+OP_MUON_F16 = 15
+OP_TOKEN_LOSS = 16
+MUON_MAX_STEPS = 32  # L1CSR_MUON_MAX_STEPS
 
 
 class L1CSRError(RuntimeError):
@@ -109,7 +115,14 @@ def lib():
         L.l1csr_relu_fwd.argtypes = [i64, vp, vp, vp]
         L.l1csr_relu_bwd.argtypes = [i64, vp, vp, vp, vp]
         L.l1csr_softmax_xent.argtypes = [i32, i32, vp, i64, vp, vp, vp, vp, sz, vp]
-        for name in ("csr_spmm_fwd", "csr_spmm_plan", "csr_spmm_planned", "csc_build", "csc_update_vals", "csr_spmm_bwd_t", "dense_wgrad",
+        L.l1csr_token_logp.argtypes = [i32, i32, C.c_int, vp, i64, vp, vp, vp, sz, vp]
+        L.l1csr_policy_loss.argtypes = [i32, i32, C.c_int, vp, i64, vp, vp, vp, vp, vp, f32, f32, f32, vp, i64, vp, vp,
+                                        vp, sz, vp]
+        L.l1csr_preference_loss.argtypes = [i32, i32, C.c_int, vp, i64, vp, i32, vp, vp, vp, f32, f32, vp, i64, vp, vp,
+                                            vp, sz, vp]
+        L.muon_update.argtypes = [i32, i32, C.c_int, vp, i64, vp, i64, vp, i64, f32, C.c_int, C.c_int, f32, f32, C.c_int,
+                                  vp, i64, vp, sz, vp]
+        for name in ("l1csr_token_logp", "l1csr_policy_loss", "l1csr_preference_loss", "muon_update", "csr_spmm_fwd", "csr_spmm_plan", "csr_spmm_planned", "csc_build", "csc_update_vals", "csr_spmm_bwd_t", "dense_wgrad",
                      "sddmm_masked_wgrad", "prox_l1_step", "csr_recompress", "prox_l1_recompress",
                      "prox_l1_recompress_noalloc", "dense_wgrad_prox", "csr_recompress_counted", "csr_bitmap_build",
                      "csr_compact", "csr_validate", "l1csr_relu_fwd", "l1csr_relu_bwd", "l1csr_softmax_xent",
@@ -292,6 +305,58 @@ def _mat(t, name):
     if unit != 1 and cols > 1:
         raise ValueError(f"{name} must have a contiguous last dimension")
     return rows, cols, ld if rows > 1 else max(cols, 1)
+
+
+def _dtype_code(t, name):
+    """l1csr_dtype of a GPU tensor."""
+    torch = _torch()
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must live on the GPU (got {t.device})")
+    code = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{name} must be float32, bfloat16 or float16 (got {t.dtype})")
+    return code
+
+
+def _typed_mat(t, name):
+    """A [rows][ld] matrix of one of the element types; returns (rows, cols, ld, l1csr_dtype)."""
+    code = _dtype_code(t, name)
+    if t.dim() != 2:
+        raise ValueError(f"{name} must be 2-D")
+    rows, cols = t.shape
+    ld, unit = t.stride()
+    if (unit != 1 and cols > 1) or (rows > 1 and ld < cols):
+        raise ValueError(f"{name} must have a contiguous last dimension and rows that do not overlap")
+    return rows, cols, ld if rows > 1 else max(cols, 1), code
+
+
+def _on_one_device(first, *others):
+    """Every tensor given (None: left out) lies on the first one's device, which has to be the current one:
+    a call launches on the current device's stream."""
+    index = first.device.index
+    for t in others:
+        if t is not None and t.device.index != index:
+            raise ValueError(f"tensors on different devices: {first.device} and {t.device}")
+    if index != _torch().cuda.current_device():
+        raise ValueError(f"the tensors live on {first.device}: make it the current device "
+                         "(torch.cuda.device) for the call")
+
+
+def _own_workspace(nbytes, device, stream):
+    """_workspace for the calls below it: under capture the buffer is the call's own (from the graph's pool), so two
+    graphs captured on one stream may be replayed side by side."""
+    return _workspace(nbytes, device, stream, keep=not _torch().cuda.is_current_stream_capturing())
+
+
+def _new(shape, dtype, device, stream):
+    """An output of a call, allocated in the order of the stream that the call runs on."""
+    torch = _torch()
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
 
 
 _ws_cache: dict = {}
@@ -1114,6 +1179,223 @@ def softmax_xent(logits, labels, dlogits=None, loss=None, stream=None):
     _check(lib().l1csr_softmax_xent(Cn, B, _p(logits), ld, _p(labels), _p(dlogits), _p(loss),
                                     _p(ws), wsb, _stream(stream)), "l1csr_softmax_xent")
     return loss, dlogits
+
+
+def _token_args(logits, labels, weights, dlogits, grad, stream):
+    """What the calls over logits[C][B] check alike; returns (C, B, dtype, ld, dlogits, its ld)."""
+    torch = _torch()
+    Cn, B, ld, code = _typed_mat(logits, "logits")
+    _vec(labels, torch.int32, "labels")
+    if labels.numel() != B:
+        raise ValueError("labels must hold one class per token (B)")
+    if weights is not None:
+        _vec(weights, torch.float32, "weights")
+        if weights.numel() != B:
+            raise ValueError("weights must hold one value per token (B)")
+    ldd = 0
+    if dlogits is not None and not grad:
+        raise ValueError("dlogits given to a call without gradient")
+    if grad:
+        if dlogits is None:
+            dlogits = _new((Cn, B), logits.dtype, logits.device, stream)
+        rows, cols, ldd, dcode = _typed_mat(dlogits, "dlogits")
+        if (rows, cols) != (Cn, B) or dcode != code:
+            raise ValueError("dlogits must have the shape and type of logits")
+        if rows == 1 and dlogits.data_ptr() == logits.data_ptr():
+            ldd = ld
+    _on_one_device(logits, labels, weights, dlogits)
+    return Cn, B, code, ld, dlogits, ldd
+
+
+def _per(t, n, name, what):
+    if t is None:
+        return None
+    _vec(t, _torch().float32, name)
+    if t.numel() != n:
+        raise ValueError(f"{name} must hold one value per {what}")
+    return t
+
+
+def token_logp(logits, labels, logp=None, stream=None):
+    """Log-probabilities of the taken tokens: logp[b] = logits[labels[b]][b] - log sum_c exp logits[c][b].
+
+    logits [C][B] float32, bfloat16 or float16 (class-major, tokens contiguous, as softmax_xent's), labels [B] int32;
+    a label outside [0, C) gives 0.  Returns logp (float32 [B])."""
+    torch = _torch()
+    Cn, B, code, ld, _, _ = _token_args(logits, labels, None, None, False, stream)
+    if logp is None:
+        logp = _new((B,), torch.float32, logits.device, stream)
+    _per(logp, B, "logp", "token")
+    _on_one_device(logits, logp)
+    ws, wsb = _own_workspace(workspace_bytes(OP_TOKEN_LOSS, Cn, 0, 0, B), logits.device, stream)
+    _check(lib().l1csr_token_logp(Cn, B, code, _p(logits), ld, _p(labels), _p(logp), _p(ws), wsb, _stream(stream)),
+           "l1csr_token_logp")
+    return logp
+
+
+def policy_loss(logits, labels, old_logp, advantages, ref_logp=None, weights=None, clip_low=0.2, clip_high=0.2,
+                kl_coef=0.0, dlogits=None, logp=None, stats=None, grad=True, stream=None):
+    """Clipped policy loss with a penalty on the distance from a reference, and its gradient.
+
+    With lp the token_logp of logits [C][B], r = exp(lp - old_logp) and the KL estimate
+    k = exp(ref_logp - lp) - (ref_logp - lp) - 1 (0 without ref_logp), the loss is the weighted mean over the tokens of
+    -min(r adv, clip(r, 1 - clip_low, 1 + clip_high) adv) + kl_coef k.  A token counts if its label lies in [0, C) and its
+    weight (weights float32 [B], default 1) is not 0; the logits of the others are not used and their columns of
+    dlogits are 0.  dlogits (the type and shape of logits) may be logits itself; grad=False leaves it out.
+    Returns (stats, dlogits, logp): stats[4] = loss, mean policy term, mean k, share of clipped tokens."""
+    torch = _torch()
+    Cn, B, code, ld, dlogits, ldd = _token_args(logits, labels, weights, dlogits, grad, stream)
+    for t_, name in ((old_logp, "old_logp"), (advantages, "advantages")):
+        _vec(t_, torch.float32, name)
+        _per(t_, B, name, "token")
+    _per(ref_logp, B, "ref_logp", "token")
+    if logp is None:
+        logp = _new((B,), torch.float32, logits.device, stream)
+    if stats is None:
+        stats = _new((4,), torch.float32, logits.device, stream)
+    _per(logp, B, "logp", "token")
+    _per(stats, 4, "stats", "statistic (4)")
+    _on_one_device(logits, old_logp, advantages, ref_logp, logp, stats)
+    ws, wsb = _own_workspace(workspace_bytes(OP_TOKEN_LOSS, Cn, 0, 0, B), logits.device, stream)
+    _check(lib().l1csr_policy_loss(Cn, B, code, _p(logits), ld, _p(labels), _p(old_logp), _p(advantages), _p(ref_logp),
+                                   _p(weights), float(clip_low), float(clip_high), float(kl_coef), _p(dlogits), ldd,
+                                   _p(logp), _p(stats), _p(ws), wsb, _stream(stream)), "l1csr_policy_loss")
+    return stats, dlogits, logp
+
+
+def preference_loss(logits, labels, seq_ptr, ref_logp=None, weights=None, beta=0.1, label_smoothing=0.0, dlogits=None,
+                    rewards=None, loss=None, grad=True, stream=None):
+    """Preference loss over pairs of sequences packed along the tokens, and its gradient.
+
+    seq_ptr (int32 [2 pairs + 1], not decreasing, within [0, B]): sequence 2p is the preferred one of pair p, 2p + 1 the
+    rejected one.  rewards[s] = beta (sum of weights * token_logp over s - ref_logp[s]) (ref_logp float32 [2 pairs],
+    default 0), D = rewards[2p] - rewards[2p + 1], loss = the mean over the pairs of
+    -(1 - ls) log sigmoid(D) - ls log sigmoid(-D) with ls = label_smoothing.  Tokens that do not count and dlogits as in
+    policy_loss; columns in no sequence get 0.  Returns (loss[1], dlogits, rewards)."""
+    torch = _torch()
+    Cn, B, code, ld, dlogits, ldd = _token_args(logits, labels, weights, dlogits, grad, stream)
+    _vec(seq_ptr, torch.int32, "seq_ptr")
+    if seq_ptr.numel() % 2 == 0:
+        raise ValueError("seq_ptr must hold 2 * pairs + 1 offsets")
+    pairs = seq_ptr.numel() // 2
+    _per(ref_logp, 2 * pairs, "ref_logp", "sequence")
+    if rewards is None:
+        rewards = _new((2 * pairs,), torch.float32, logits.device, stream)
+    if loss is None:
+        loss = _new((1,), torch.float32, logits.device, stream)
+    _per(rewards, 2 * pairs, "rewards", "sequence")
+    _per(loss, 1, "loss", "call (1)")
+    _on_one_device(logits, seq_ptr, ref_logp, rewards, loss)
+    ws, wsb = _own_workspace(workspace_bytes(OP_TOKEN_LOSS, Cn, pairs, 0, B), logits.device, stream)
+    _check(lib().l1csr_preference_loss(Cn, B, code, _p(logits), ld, _p(labels), pairs, _p(seq_ptr), _p(ref_logp),
+                                       _p(weights), float(beta), float(label_smoothing), _p(dlogits), ldd, _p(rewards),
+                                       _p(loss), _p(ws), wsb, _stream(stream)), "l1csr_preference_loss")
+    return loss, dlogits, rewards
+
+
+@dataclass
+class MuonState:
+    """Hyper-parameters and momentum of Prox-Muon.  m is a float32 device tensor [N][K] (a leading dimension >= K is
+    allowed) that starts at zero; scale multiplies the orthogonalised update (None: sqrt(max(1, N / K)))."""
+    m: object
+    mu: float = 0.95
+    nesterov: bool = True
+    steps: int = 5
+    eps: float = 1e-7
+    scale: float | None = None
+
+    @staticmethod
+    def zeros(shape, device, **kw):
+        torch = _torch()
+        return MuonState(torch.zeros(shape, dtype=torch.float32, device=device), **kw)
+
+
+def _muon_update(G, O, m, m_out, mu, nesterov, steps, eps, scale, precision, stream):
+    N, K, ldg, code = _typed_mat(G, "G")
+    ro, co, ldo, ocode = _typed_mat(O, "out")
+    if (ro, co) != (N, K) or ocode != code:
+        raise ValueError("the update must have the shape and type of G")
+    if N == 1 and O.data_ptr() == G.data_ptr():
+        ldo = ldg
+    ldm = ldmo = 0
+    for t_, name in ((m, "m"), (m_out, "m_out")):
+        if t_ is not None:
+            rows, cols, ld = _mat(t_, name)
+            if (rows, cols) != (N, K):
+                raise ValueError(f"{name} must be [n_rows][n_cols]")
+            if name == "m":
+                ldm = ld
+            else:
+                ldmo = ld
+    if precision not in (F32, F16):
+        raise ValueError("precision must be F32 or F16")
+    _on_one_device(G, O, m, m_out)
+    ws, wsb = _own_workspace(workspace_bytes(OP_MUON if precision == F32 else OP_MUON_F16, N, K, 0, 0), G.device, stream)
+    _check(lib().muon_update(N, K, code, _p(G), ldg, _p(m), ldm, _p(m_out), ldmo, float(mu), int(bool(nesterov)),
+                             int(steps), float(eps), float(scale), int(precision), _p(O), ldo, _p(ws), wsb,
+                             _stream(stream)), "muon_update")
+    return O
+
+
+def orthogonalize(G, out=None, steps=5, eps=1e-7, scale=1.0, precision=None, stream=None):
+    """scale * NS(G / (|G|_F + eps)): `steps` quintic Newton-Schulz steps (muon_update without momentum).
+
+    G [N][K] float32, bfloat16 or float16; out, of the same shape and type, may be G itself.  precision: F32 (fp32
+    accuracy) or F16 (operands rounded to fp16, about 1.5e-3 of the norm off); by default F32 for a float32 G and F16
+    for the 16-bit types.  Returns out."""
+    if precision is None:
+        precision = F32 if _dtype_code(G, "G") == 0 else F16
+    if out is None:
+        N, K, _, _ = _typed_mat(G, "G")
+        out = _new((N, K), G.dtype, G.device, stream)
+    return _muon_update(G, out, None, None, 0.0, False, steps, eps, scale, precision, stream)
+
+
+def _muon_args(W, G, st, m_out):
+    N, K, _ = _mat(G, "G")
+    if (N, K) != (W.n_rows, W.n_cols):
+        raise ValueError("G must be [n_rows][n_cols]")
+    _mat(st.m, "m")
+    scale = max(1.0, N / K) ** 0.5 if st.scale is None and N and K else st.scale or 0.0
+    return N, K, scale, st.m if m_out is None else m_out
+
+
+def prox_muon_step(W: CSR, G, st: MuonState, eta, lam, Z=None, m_out=None, row_counts=None, precision=F32,
+                   stream=None):
+    """One Prox-Muon step of the l1 phase over all N*K weights: m' = mu m + G, O = scale * NS(G + mu m') (muon_update;
+    without nesterov NS(m')), Z = S_{eta*lam}(W - eta O).  Z may be G itself; st.m is updated in place, or m_out receives
+    m' and st.m is kept.  Returns Z."""
+    torch = _torch()
+    N, K, scale, m_new = _muon_args(W, G, st, m_out)
+    _on_one_device(G, W.row_ptr, W.col_idx, W.vals, row_counts)
+    W.validate_shapes()
+    if Z is None:
+        Z = _new((N, K), torch.float32, G.device, stream)
+    _muon_update(G, Z, st.m, m_new, st.mu, st.nesterov, st.steps, st.eps, scale, precision, stream)
+    return prox_l1_step(PROX_DENSE, W, Z, eta, lam, Z=Z, row_counts=row_counts, stream=stream)
+
+
+def prox_muon_recompress(W: CSR, G, st: MuonState, eta, lam, O=None, capacity=None, out: CSR | None = None,
+                         precision=F32, stream=None):
+    """W' = CSR of the Prox-Muon step (the bits of prox_muon_step and csr_recompress), the recompression fused with the
+    threshold (prox_l1_recompress).  O (float32 [N][K], may be G itself) receives the update; st.m is updated in
+    place, but not by a call that fails for its capacity."""
+    torch = _torch()
+    N, K, scale, m_new = _muon_args(W, G, st, None)
+    _on_one_device(G, W.row_ptr, W.col_idx, W.vals)
+    W.validate_shapes()
+    cap = capacity if capacity is not None else (N * K if out is None else min(out.col_idx.numel(), out.vals.numel()))
+    short = cap < N * K
+    if short:
+        m_new = _new((N, K), torch.float32, G.device, stream)
+    if O is None:
+        O = _new((N, K), torch.float32, G.device, stream)
+    _muon_update(G, O, st.m, m_new, st.mu, st.nesterov, st.steps, st.eps, scale, precision, stream)
+    out = prox_l1_recompress(W, O, eta, lam, capacity=capacity, out=out, stream=stream)
+    if short:
+        with torch.cuda.stream(torch.cuda.current_stream(G.device) if stream is None else stream):
+            st.m.copy_(m_new)
+    return out
 
 
 # the two-stream l1 step over the entry points above

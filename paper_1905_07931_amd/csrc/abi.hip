@@ -49,6 +49,12 @@ bool overlap(const float *p, int64_t ldp, const float *q, int64_t ldq, int64_t r
     return p0 < q1 && q0 < p1;
 }
 
+int64_t dtype_bytes(int dtype) { return dtype == L1CSR_DTYPE_F32 ? 4 : 2; }
+
+bool bad_dtype(int dtype) {
+    return dtype != L1CSR_DTYPE_F32 && dtype != L1CSR_DTYPE_BF16 && dtype != L1CSR_DTYPE_F16;
+}
+
 // byte ranges [a, a + na) and [b, b + nb) intersect (null or empty never does)
 bool bytes_overlap(const void *a, size_t na, const void *b, size_t nb) {
     if (a == nullptr || b == nullptr || na == 0 || nb == 0) return false;
@@ -84,6 +90,28 @@ bool outputs_overlap(int32_t n_rows, int64_t nnz, const int32_t *row_ptr, const 
             if (bytes_overlap(outs[o], out_b[o], dense_in[d], dense_in_bytes[d])) return true;
     }
     return false;
+}
+
+// extent in bytes of a [rows][ld] matrix of `dtype`
+size_t typed_bytes(int64_t rows, int64_t cols, int64_t ld, int dtype) {
+    return rows > 0 && cols > 0 ? (size_t)(((rows - 1) * ld + cols) * dtype_bytes(dtype)) : 0;
+}
+
+// What the calls over logits check alike
+int token_check(const token_loss_args &a, size_t ws_bytes, const void *ws) {
+    if (a.C <= 0 || a.B < 0 || a.pairs < 0 || bad_dtype(a.dtype)) return L1CSR_EINVAL;
+    if (bad_dense(a.logits, a.C, a.B, a.ld)) return L1CSR_EINVAL;
+    if (a.B > 0 && a.labels == nullptr) return L1CSR_EINVAL;
+    if (a.dlogits != nullptr) {
+        if (a.ldd < a.B) return L1CSR_EINVAL;
+        if (a.dlogits == a.logits ? a.ldd != a.ld
+                                  : bytes_overlap(a.dlogits, typed_bytes(a.C, a.B, a.ldd, a.dtype), a.logits,
+                                                  typed_bytes(a.C, a.B, a.ld, a.dtype)))
+            return L1CSR_EINVAL;
+    }
+    const size_t need = token_loss_workspace_bytes(a.C, a.B, a.pairs);
+    if (need > 0 && (ws == nullptr || ws_bytes < need)) return L1CSR_EINVAL;
+    return L1CSR_OK;
 }
 
 // Prox-RMSProp / Prox-ADAM hyper-parameters -> the kernels' double constants;
@@ -289,6 +317,9 @@ size_t l1csr_workspace_bytes(int op, int32_t n_rows, int32_t n_cols, int64_t nnz
         case L1CSR_OP_SDDMM_PACKED: return round_up(packed_sddmm_bytes(n_rows, n_cols, nnz, B));
         case L1CSR_OP_SPMM_PACKED: return round_up(packed_spmm_bytes(n_rows, n_cols, nnz, B));
         case L1CSR_OP_PROX_DENSE: return round_up(prox_dense_carve(n_rows, n_cols, nullptr).bytes);
+        case L1CSR_OP_MUON: return round_up(muon_workspace_bytes(n_rows, n_cols, 2));
+        case L1CSR_OP_MUON_F16: return round_up(muon_workspace_bytes(n_rows, n_cols, 1));
+        case L1CSR_OP_TOKEN_LOSS: return round_up(token_loss_workspace_bytes(n_rows, B, n_cols));
         case L1CSR_OP_SOFTMAX_XENT: return round_up(sizeof(float) * (size_t)(ceil_div(B, 256) + 1));
         default: return 0;
     }
@@ -835,6 +866,86 @@ int l1csr_softmax_xent(int32_t C, int32_t B, const float *logits, int64_t ld,
         return L1CSR_EINVAL;
     return hip_status(
         launch_softmax_xent(C, B, logits, ld, labels, dlogits, loss, static_cast<float *>(ws), stream));
+}
+
+int l1csr_token_logp(int32_t C, int32_t B, int dtype, const void *logits, int64_t ld, const int32_t *labels,
+                     float *logp, void *ws, size_t ws_bytes, hipStream_t stream) {
+    token_loss_args a{};
+    a.C = C; a.B = B; a.dtype = dtype;
+    a.logits = logits; a.ld = ld; a.labels = labels; a.logp = logp;
+    const int rc = token_check(a, ws_bytes, ws);
+    if (rc != L1CSR_OK) return rc;
+    if (B > 0 && logp == nullptr) return L1CSR_EINVAL;
+    return hip_status(launch_token_logp(a, ws, stream));
+}
+
+int l1csr_policy_loss(int32_t C, int32_t B, int dtype, const void *logits, int64_t ld, const int32_t *labels,
+                      const float *old_logp, const float *advantages, const float *ref_logp, const float *weights,
+                      float clip_low, float clip_high, float kl_coef, void *dlogits, int64_t ldd, float *logp,
+                      float *stats, void *ws, size_t ws_bytes, hipStream_t stream) {
+    token_loss_args a{};
+    a.C = C; a.B = B; a.dtype = dtype;
+    a.logits = logits; a.ld = ld; a.labels = labels; a.weights = weights;
+    a.dlogits = dlogits; a.ldd = ldd; a.logp = logp;
+    a.old_logp = old_logp; a.adv = advantages; a.ref_logp = ref_logp;
+    a.clip_low = clip_low; a.clip_high = clip_high; a.kl_coef = kl_coef;
+    a.out = stats;
+    if (!finite_f(clip_low) || !finite_f(clip_high) || !finite_f(kl_coef)) return L1CSR_EINVAL;
+    if (clip_low < 0.f || clip_low > 1.f || clip_high < 0.f || kl_coef < 0.f || stats == nullptr) return L1CSR_EINVAL;
+    const int rc = token_check(a, ws_bytes, ws);
+    if (rc != L1CSR_OK) return rc;
+    if (B > 0 && (old_logp == nullptr || advantages == nullptr)) return L1CSR_EINVAL;
+    return hip_status(launch_policy_loss(a, ws, stream));
+}
+
+int l1csr_preference_loss(int32_t C, int32_t B, int dtype, const void *logits, int64_t ld, const int32_t *labels,
+                          int32_t pairs, const int32_t *seq_ptr, const float *ref_logp, const float *weights,
+                          float beta, float label_smoothing, void *dlogits, int64_t ldd, float *rewards, float *loss,
+                          void *ws, size_t ws_bytes, hipStream_t stream) {
+    token_loss_args a{};
+    a.C = C; a.B = B; a.dtype = dtype;
+    a.logits = logits; a.ld = ld; a.labels = labels; a.weights = weights;
+    a.dlogits = dlogits; a.ldd = ldd;
+    a.pairs = pairs; a.seq_ptr = seq_ptr; a.ref_logp = ref_logp;
+    a.beta = beta; a.smoothing = label_smoothing;
+    a.rewards = rewards; a.out = loss;
+    if (!finite_f(beta) || !(beta >= 0.f) || !(label_smoothing >= 0.f && label_smoothing <= 0.5f)) return L1CSR_EINVAL;
+    if (loss == nullptr || (pairs > 0 && seq_ptr == nullptr) || pairs > INT32_MAX / 2 - 1) return L1CSR_EINVAL;
+    const int rc = token_check(a, ws_bytes, ws);
+    if (rc != L1CSR_OK) return rc;
+    return hip_status(launch_preference_loss(a, ws, stream));
+}
+
+int muon_update(int32_t N, int32_t K, int dtype, const void *G, int64_t ldg, const float *M, int64_t ldm,
+                float *M_out, int64_t ldmo, float mu, int nesterov, int steps, float eps, float scale, int precision,
+                void *O, int64_t ldo, void *ws, size_t ws_bytes, hipStream_t stream) {
+    if (N < 0 || K < 0 || bad_dtype(dtype)) return L1CSR_EINVAL;
+    if (precision != L1CSR_F32 && precision != L1CSR_F16) return L1CSR_EINVAL;
+    if (steps < 1 || steps > L1CSR_MUON_MAX_STEPS) return L1CSR_EINVAL;
+    if (!finite_f(eps) || eps < 0.f || !finite_f(scale)) return L1CSR_EINVAL;
+    if (bad_dense(G, N, K, ldg) || bad_dense(O, N, K, ldo)) return L1CSR_EINVAL;
+    if (M != nullptr && (ldm < K || !(mu >= 0.f && mu < 1.f))) return L1CSR_EINVAL;
+    if (M_out != nullptr && (M == nullptr || ldmo < K)) return L1CSR_EINVAL;
+    const size_t g = typed_bytes(N, K, ldg, dtype), o = typed_bytes(N, K, ldo, dtype);
+    const size_t m = M ? dense_bytes(N, K, ldm) : 0, mo = M_out ? dense_bytes(N, K, ldmo) : 0;
+    if (G == O ? ldg != ldo : bytes_overlap(G, g, O, o)) return L1CSR_EINVAL;
+    if (M != nullptr && M == M_out ? ldm != ldmo : bytes_overlap(M, m, M_out, mo)) return L1CSR_EINVAL;
+    if (bytes_overlap(M, m, G, g) || bytes_overlap(M, m, O, o) || bytes_overlap(M_out, mo, G, g) ||
+        bytes_overlap(M_out, mo, O, o))
+        return L1CSR_EINVAL;
+    const int parts = precision == L1CSR_F32 ? 2 : 1;
+    const size_t need = muon_workspace_bytes(N, K, parts);
+    if (need > 0 && (ws == nullptr || ws_bytes < need)) return L1CSR_EINVAL;
+    // 32-bit chunk numbers and offsets inside a packed group; grid rows
+    if ((int64_t)N * K > INT32_MAX || N > (1 << 22) || K > (1 << 22)) return L1CSR_EUNSUPPORTED;
+    muon_args a{};
+    a.N = N; a.K = K; a.dtype = dtype;
+    a.G = G; a.ldg = ldg;
+    a.M = M; a.ldm = ldm; a.M_out = M_out; a.ldmo = ldmo;
+    a.mu = mu; a.nesterov = nesterov != 0; a.steps = steps;
+    a.eps = eps; a.scale = scale; a.parts = parts;
+    a.O = O; a.ldo = ldo;
+    return hip_status(launch_muon(a, ws, stream));
 }
 
 }  // extern "C"

@@ -259,4 +259,51 @@ hipError_t launch_relu_bwd(int64_t n, const float *x, const float *dy, float *dx
 hipError_t launch_softmax_xent(int C, int B, const float *z, int64_t ld, const int *labels,
                                float *dz, float *loss, float *ws, hipStream_t s);
 
+// token_loss.hip -----------------------------------------------------------
+// element types of the calls that take more than fp32 (the ABI's l1csr_dtype)
+constexpr int kTypeF32 = 0;
+constexpr int kTypeBF16 = 1;
+constexpr int kTypeF16 = 2;
+struct token_loss_args {
+    int C, B, dtype;
+    const void *logits;            // [C][ld]
+    int64_t ld;
+    const int *labels;             // [B]
+    const float *weights;          // [B], nullable
+    void *dlogits;                 // [C][ldd], nullable: the loss alone
+    int64_t ldd;
+    float *logp;                   // [B], nullable
+    const float *ref_logp;         // policy [B], preference [2 pairs]; nullable
+    const float *old_logp, *adv;   // policy: [B]
+    float clip_low, clip_high, kl_coef;
+    int pairs;                     // preference
+    const int *seq_ptr;            // [2 pairs + 1]
+    float beta, smoothing;
+    float *rewards;                // [2 pairs], nullable
+    float *out;                    // policy: 4 values, preference: 1
+};
+size_t token_loss_workspace_bytes(int C, int B, int pairs);
+hipError_t launch_token_logp(const token_loss_args &a, void *ws, hipStream_t s);
+hipError_t launch_policy_loss(const token_loss_args &a, void *ws, hipStream_t s);
+hipError_t launch_preference_loss(const token_loss_args &a, void *ws, hipStream_t s);
+
+// muon.hip -----------------------------------------------------------------
+struct muon_args {
+    int N, K, dtype;
+    const void *G;       // [N][ldg], as O
+    int64_t ldg;
+    const float *M;      // [N][ldm] momentum, null: U = G
+    int64_t ldm;
+    float *M_out;        // [N][ldmo], null: not stored; may be M
+    int64_t ldmo;
+    float mu;
+    int nesterov, steps;
+    float eps, scale;
+    int parts;           // of the operands: 2 (fp32 accuracy) or 1
+    void *O;             // [N][ldo]; may be G
+    int64_t ldo;
+};
+size_t muon_workspace_bytes(int N, int K, int parts);
+hipError_t launch_muon(const muon_args &a, void *ws, hipStream_t s);
+
 }  // namespace l1csr

@@ -36,6 +36,7 @@
 
 #include "common.hpp"
 #include "launch.hpp"
+#include "lds_dma.hpp"
 #include "prox_epilogue.hpp"
 
 namespace l1csr {
@@ -43,7 +44,6 @@ namespace l1csr {
 namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __attribute__((address_space(3))) void sg_lds_void;
 
 constexpr int kGroup = 32;         // rows of a packed group
 constexpr int kStep = 16;          // reduction indices of a packed block
@@ -267,25 +267,6 @@ __device__ __forceinline__ floatx16 mfma16(bf16x8 a, bf16x8 b, floatx16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
 
-// One 1 KB block global -> LDS (16 bytes per lane), base and lds wave-uniform.
-// As an instruction of its own rather than the builtin: the compiler orders the
-// builtin's loads against the reads of the other buffers and waited for the
-// loads just issued (vmcnt(0)) in one step of three.  It writes no register;
-// wait_vm() below counts it.
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"  // m0 is reserved: the clobber orders it, nothing keeps it
-__device__ __forceinline__ void dma16(const char *base, unsigned off, unsigned lds) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base)
-                 : "memory", "m0");
-}
-#pragma clang diagnostic pop
-
-template <int N>
-__device__ __forceinline__ void wait_vm() {  // at most N vector memory operations and no LDS access outstanding
-    static_assert(N < 16, "low field only");
-    __builtin_amdgcn_s_waitcnt(0x0070 | N);
-}
-
 // The tile: 128 x 128, 2 x 2 waves of 64 x 64 (2 x 2 MFMA tiles each), a step of
 // 16 reduction indices a time.  A step is 4 + 4 groups of NP blocks (24 KB with
 // three parts), three steps in LDS (72 KB): two workgroups share a CU, so one's
@@ -377,9 +358,9 @@ __global__ __launch_bounds__(NT, 2) void split_gemm_kernel(gemm_args G) {
                           : G.B.data + min(tn * RGB + (g - RGA), G.B.groups - 1) * gs) +
                  (int64_t)c0 * (NP * kBlockBytes) + q * kBlockBytes;
     }
-    const unsigned l0 = (unsigned)(uintptr_t)(sg_lds_void *)S0 + wave * kBlockBytes;
-    const unsigned l1 = (unsigned)(uintptr_t)(sg_lds_void *)S1 + wave * kBlockBytes;
-    const unsigned l2 = (unsigned)(uintptr_t)(sg_lds_void *)S2 + wave * kBlockBytes;
+    const unsigned l0 = lds_address(S0) + wave * kBlockBytes;
+    const unsigned l1 = lds_address(S1) + wave * kBlockBytes;
+    const unsigned l2 = lds_address(S2) + wave * kBlockBytes;
     auto load = [&](unsigned dst, int c) {
         const unsigned off = (unsigned)c * (NP * kBlockBytes) + lane * 16;
 #pragma unroll

@@ -1,0 +1,473 @@
+// Losses on the log-probabilities of taken tokens and their gradients with
+// respect to the logits z[C][B] (class-major, tokens contiguous):
+//   lp_b = z[a_b][b] - log sum_c exp z[c][b]
+//   policy      r = exp(lp - old), pg = -min(r A, clip(r, 1 - cl, 1 + ch) A),
+//               kl = exp(ref - lp) - (ref - lp) - 1,
+//               loss = sum_b w (pg + beta kl) / sum_b w
+//   preference  S_s = sum_{b in s} w lp, reward_s = beta (S_s - R_s),
+//               D = reward_chosen - reward_rejected,
+//               loss = mean_p( -(1 - ls) log sig(D) - ls log sig(-D) )
+// Both gradients are dz[c][b] = coef_b (1[c = a_b] - softmax(z_.b)_c) with one
+// coefficient a token, coef_b = d loss / d lp_b.
+//
+// Three passes: partial (maximum, sum of exponentials) of every column over
+// ranges of classes; a token pass that joins them and takes the loss and the
+// coefficient; the gradient pass.  (The preference loss has a pass over the
+// pairs before the last.)  Sums over tokens are taken in double in a fixed order.
+#include <algorithm>
+
+#include "common.hpp"
+#include "launch.hpp"
+
+namespace l1csr {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kTokenBlocks = 256;  // most workgroups (and partial sums) of the token pass
+constexpr float kLog2e = 1.44269504088896340736f;
+
+__device__ __forceinline__ float to_f32(float x) { return x; }
+__device__ __forceinline__ float to_f32(_Float16 x) { return (float)x; }
+__device__ __forceinline__ float to_f32(__bf16 x) { return (float)x; }
+
+// exp(x) for x <= 0 (or NaN); results under 2^-126 are zero
+__device__ __forceinline__ float exp_neg(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+
+// V values at any alignment of T: the hardware takes unaligned 16-byte accesses
+template <typename T, int V>
+__device__ __forceinline__ void load_vec(const T *p, T (&x)[V]) {
+    __builtin_memcpy(x, p, sizeof(T) * V);
+}
+
+// How a workgroup lies over [C][B]: 2^tx_shift threads of V columns each side by
+// side, the others over the classes; blockIdx.y a range of classes.
+struct grid_shape {
+    int tx_shift, col_blocks, splits, rows;
+};
+
+template <int V>
+struct columns {
+    int col0;   // the first column of this thread
+    int at;     // where its loads begin: col0, or B - V where the columns end inside the vector
+    bool any;   // it has a column
+    __device__ columns(int tx, int tx_shift, int B) {
+        col0 = (((int)blockIdx.x << tx_shift) + tx) * V;
+        any = col0 < B;
+        at = V == 1 ? col0 : min(col0, B - V);
+    }
+    // element v of the loads is a column of this thread (not its neighbour's)
+    __device__ bool mine(int v) const { return at + v >= col0; }
+};
+
+__device__ __forceinline__ bool live(const int *labels, const float *w, int b, int C) {
+    const int a = labels[b];
+    return a >= 0 && a < C && (w == nullptr || w[b] != 0.f);
+}
+
+template <typename T, int V>
+__global__ __launch_bounds__(kThreads) void column_sums_kernel(int C, int B, const T *__restrict__ z, int64_t ld,
+                                                               const int *__restrict__ labels,
+                                                               const float *__restrict__ w, grid_shape g,
+                                                               float2 *__restrict__ part) {
+    constexpr int U = 4;
+    __shared__ float sm[kThreads * V], ss[kThreads * V];
+    const int TX = 1 << g.tx_shift, TY = kThreads >> g.tx_shift;
+    const int tx = threadIdx.x & (TX - 1), ty = threadIdx.x >> g.tx_shift;
+    const columns<V> k(tx, g.tx_shift, B);
+    bool work = false;  // a column that counts: the others' logits are not read
+    if (k.any)
+#pragma unroll
+        for (int v = 0; v < V; ++v) work |= k.mine(v) && live(labels, w, k.at + v, C);
+    float m[V], s[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        m[v] = -INFINITY;
+        s[v] = 0.f;
+    }
+    const int c0 = blockIdx.y * g.rows, c1 = min(C, c0 + g.rows);
+    if (work)
+        for (int c = c0 + ty; c < c1; c += U * TY) {
+            T x[U][V];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (c + u * TY < c1) load_vec<T, V>(z + (int64_t)(c + u * TY) * ld + k.at, x[u]);
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                float y[U], top = m[v];
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    y[u] = c + u * TY < c1 ? to_f32(x[u][v]) : -INFINITY;
+                    top = fmaxf(top, y[u]);
+                }
+                const float base = top == -INFINITY ? 0.f : top;  // only excluded classes so far
+                float sum = s[v] * exp_neg(m[v] - base);
+#pragma unroll
+                for (int u = 0; u < U; ++u) sum += exp_neg(y[u] - base);
+                m[v] = top;
+                s[v] = sum;
+            }
+        }
+    const int first = ((int)blockIdx.x << g.tx_shift) * V;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const int col = k.at + v - first;
+        if (k.any && k.mine(v)) {
+            sm[ty * TX * V + col] = m[v];
+            ss[ty * TX * V + col] = s[v];
+        }
+    }
+    __syncthreads();
+    const int n = min(TX * V, B - first);
+    for (int col = threadIdx.x; col < n; col += kThreads) {
+        float top = -INFINITY, sum = 0.f;
+        for (int t = 0; t < TY; ++t) top = fmaxf(top, sm[t * TX * V + col]);
+        const float base = top == -INFINITY ? 0.f : top;
+        for (int t = 0; t < TY; ++t) sum += ss[t * TX * V + col] * exp_neg(sm[t * TX * V + col] - base);
+        part[(int64_t)(first + col) * g.splits + blockIdx.y] = make_float2(top, sum);
+    }
+}
+
+// What the token pass leaves for the others
+struct token_out {
+    float *m, *inv;   // the column's maximum and 1 / (sum of exponentials)
+    float *coef;      // d loss / d lp (policy: times the sum of weights)
+    float *lp;        // log-probability; 0 where the token does not count
+    double *sums;     // [4][kTokenBlocks] weights, and weighted loss, kl, clipped
+};
+
+struct policy_args {
+    const float *old_lp, *adv, *ref_lp;
+    float low, high, kl_coef;  // 1 - clip_low, 1 + clip_high
+};
+
+enum { kLogp = 0, kPolicy = 1, kPreference = 2 };
+
+__device__ __forceinline__ double block_sum(double x, double *lds) {
+#pragma unroll
+    for (int d = kWave / 2; d >= 1; d >>= 1) x += __shfl_xor(x, d, kWave);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
+    __syncthreads();
+    double t = 0;
+    for (int i = 0; i < kThreads / kWave; ++i) t += lds[i];
+    return t;
+}
+
+// 2^lane_shift lanes a token join its partial sums
+template <typename T, int KIND>
+__global__ __launch_bounds__(kThreads) void token_kernel(int C, int B, const T *__restrict__ z, int64_t ld,
+                                                         const int *__restrict__ labels, const float *__restrict__ w,
+                                                         int splits, int lane_shift, const float2 *__restrict__ part,
+                                                         policy_args P, token_out o) {
+    __shared__ double lds[kThreads / kWave];
+    const int L = 1 << lane_shift, per = kThreads >> lane_shift;
+    const int lane = threadIdx.x & (L - 1);
+    double sw = 0, sl = 0, sk = 0, sc = 0;
+    for (int64_t b0 = (int64_t)blockIdx.x * per; b0 < B; b0 += (int64_t)gridDim.x * per) {
+        const int64_t b = b0 + (threadIdx.x >> lane_shift);
+        const bool on = b < B && live(labels, w, (int)b, C);
+        float top = -INFINITY;
+        if (on)
+            for (int i = lane; i < splits; i += L) top = fmaxf(top, part[b * splits + i].x);
+        for (int d = L / 2; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, kWave));
+        const float base = top == -INFINITY ? 0.f : top;
+        float s = 0.f;
+        if (on)
+            for (int i = lane; i < splits; i += L) {
+                const float2 p = part[b * splits + i];
+                s += p.y * exp_neg(p.x - base);
+            }
+        for (int d = L / 2; d >= 1; d >>= 1) s += __shfl_xor(s, d, kWave);
+        if (lane != 0 || b >= B) continue;
+        const float lp = on ? (to_f32(z[(int64_t)labels[b] * ld + b]) - top) - logf(s) : 0.f;
+        if (o.lp) o.lp[b] = lp;
+        if constexpr (KIND == kLogp) continue;
+        o.m[b] = top;
+        o.inv[b] = on ? 1.f / s : 0.f;
+        float coef = 0.f;
+        if constexpr (KIND == kPolicy) {
+            if (on) {
+                const float wt = w ? w[b] : 1.f, A = P.adv[b], r = expf(lp - P.old_lp[b]);
+                const bool off = (A > 0.f && r > P.high) || (A < 0.f && r < P.low);
+                const float used = off ? (A > 0.f ? P.high : P.low) : r;
+                float kl = 0.f, dlp = off ? 0.f : -A * r;
+                if (P.ref_lp) {
+                    const float q = P.ref_lp[b] - lp, e = expm1f(q);
+                    kl = e - q;
+                    dlp -= P.kl_coef * e;
+                }
+                coef = wt * dlp;
+                sw += wt;
+                sl += (double)wt * (-A * used);
+                sk += (double)wt * kl;
+                sc += off ? wt : 0.f;
+            }
+        }
+        o.coef[b] = coef;
+    }
+    if constexpr (KIND == kPolicy) {
+        const double t[4] = {block_sum(sw, lds), block_sum(sl, lds), block_sum(sk, lds), block_sum(sc, lds)};
+        if (threadIdx.x < 4) o.sums[threadIdx.x * kTokenBlocks + blockIdx.x] = t[threadIdx.x];
+    }
+}
+
+// A workgroup a pair: the sums over its two sequences, the loss, the tokens' coefficients.
+__global__ __launch_bounds__(kThreads) void pair_kernel(int C, int B, int pairs, const int *__restrict__ labels,
+                                                        const float *__restrict__ w, const int *__restrict__ seq,
+                                                        const float *__restrict__ ref, float beta, float smoothing,
+                                                        const float *__restrict__ lp, float *__restrict__ coef,
+                                                        float *__restrict__ rewards, double *__restrict__ loss) {
+    __shared__ double lds[kThreads / kWave];
+    const int p = blockIdx.x;
+    const int lo = min(max(seq[2 * p], 0), B), mid = min(max(seq[2 * p + 1], lo), B), hi = min(max(seq[2 * p + 2], mid), B);
+    double s0 = 0, s1 = 0;
+    for (int b = lo + (int)threadIdx.x; b < hi; b += kThreads) {
+        if (!live(labels, w, b, C)) continue;
+        const double x = (double)lp[b] * (w ? w[b] : 1.f);
+        if (b < mid) s0 += x; else s1 += x;
+    }
+    s0 = beta * (block_sum(s0, lds) - (ref ? ref[2 * p] : 0.f));
+    s1 = beta * (block_sum(s1, lds) - (ref ? ref[2 * p + 1] : 0.f));
+    const double D = s0 - s1, e = exp(-fabs(D)), up = D >= 0 ? 1 / (1 + e) : e / (1 + e);  // sig(D)
+    const double down = D >= 0 ? e / (1 + e) : 1 / (1 + e);
+    if (threadIdx.x == 0) {
+        if (rewards) {
+            rewards[2 * p] = (float)s0;
+            rewards[2 * p + 1] = (float)s1;
+        }
+        // -log sig(D) = log(1 + e) + max(-D, 0)
+        loss[p] = log1p(e) + (1 - (double)smoothing) * fmax(-D, 0.0) + smoothing * fmax(D, 0.0);
+    }
+    const double dS = (smoothing * up - (1 - (double)smoothing) * down) * beta / pairs;
+    for (int b = lo + (int)threadIdx.x; b < hi; b += kThreads)
+        if (live(labels, w, b, C)) coef[b] = (float)((b < mid ? dS : -dS) * (w ? w[b] : 1.f));
+}
+
+// The loss from the partial sums, by one workgroup: out[0..3] = loss, policy part, kl, clipped share,
+// or out[0] = the mean over the pairs.  Returns what the policy's coefficients are scaled with.
+template <int KIND>
+__device__ double finish(int n, const double *__restrict__ sums, float kl_coef, double *lds, bool write, float *out) {
+    if constexpr (KIND == kPolicy) {
+        const double sw = block_sum((int)threadIdx.x < n ? sums[threadIdx.x] : 0.0, lds);
+        const double inv = sw != 0 ? 1 / sw : 0.0;
+        if (!write) return inv;
+        double t[3];
+        for (int q = 0; q < 3; ++q)
+            t[q] = block_sum((int)threadIdx.x < n ? sums[(q + 1) * kTokenBlocks + threadIdx.x] : 0.0, lds) * inv;
+        if (threadIdx.x == 0) {
+            out[0] = (float)(t[0] + kl_coef * t[1]);
+            out[1] = (float)t[0];
+            out[2] = (float)t[1];
+            out[3] = (float)t[2];
+        }
+        return inv;
+    } else {
+        if (!write) return 1;
+        double x = 0;
+        for (int i = threadIdx.x; i < n; i += kThreads) x += sums[i];
+        x = block_sum(x, lds);
+        if (threadIdx.x == 0) out[0] = n > 0 ? (float)(x / n) : 0.f;
+        return 1;
+    }
+}
+
+template <int KIND>
+__global__ __launch_bounds__(kThreads) void finish_kernel(int n, const double *__restrict__ sums, float kl_coef,
+                                                          float *__restrict__ out) {
+    __shared__ double lds[kThreads / kWave];
+    finish<KIND>(n, sums, kl_coef, lds, true, out);
+}
+
+// dz, over the layout of column_sums_kernel; z and dz may be the same matrix (every
+// element is read by the thread that writes it; a thread's loads of its
+// neighbour's columns are not used).  A token's own class comes last, from lp.
+template <typename T, int V, int KIND>
+__global__ __launch_bounds__(kThreads) void gradient_kernel(int C, int B, const T *z, int64_t ld,
+                                                            const int *__restrict__ labels, grid_shape g, token_out t,
+                                                            T *dz, int64_t ldd, int n_sums, float kl_coef,
+                                                            float *__restrict__ out) {
+    constexpr int U = 4;
+    __shared__ double lds[kThreads / kWave];
+    const float scale =
+        (float)finish<KIND>(n_sums, t.sums, kl_coef, lds, blockIdx.x == 0 && blockIdx.y == 0, out);
+    const int TX = 1 << g.tx_shift, TY = kThreads >> g.tx_shift;
+    const int tx = threadIdx.x & (TX - 1), ty = threadIdx.x >> g.tx_shift;
+    const columns<V> k(tx, g.tx_shift, B);
+    if (!k.any) return;
+    float m[V], f[V];  // dz = -f exp(z - m)
+    bool work = false;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const float coef = t.coef[k.at + v] * scale;
+        m[v] = t.m[k.at + v];
+        f[v] = coef * t.inv[k.at + v];
+        work |= k.mine(v) && coef != 0.f;
+        if (coef == 0.f) f[v] = 0.f;
+    }
+    const int c0 = blockIdx.y * g.rows, c1 = min(C, c0 + g.rows);
+    const bool whole = k.at == k.col0;
+    for (int c = c0 + ty; c < c1; c += U * TY) {
+        T x[U][V];
+        if (work) {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (c + u * TY < c1) load_vec<T, V>(z + (int64_t)(c + u * TY) * ld + k.at, x[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (c + u * TY >= c1) continue;
+            T y[V];
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                y[v] = f[v] == 0.f || !work ? (T)0.f : (T)(-f[v] * exp_neg(to_f32(x[u][v]) - m[v]));
+            T *d = dz + (int64_t)(c + u * TY) * ldd + k.at;
+            if (whole) {
+                __builtin_memcpy(d, y, sizeof(T) * V);
+            } else {
+#pragma unroll
+                for (int v = 0; v < V; ++v)
+                    if (k.mine(v)) d[v] = y[v];
+            }
+        }
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const int b = k.at + v, a = labels[b];
+        if (!k.mine(v) || a < c0 || a >= c1 || (a - c0) % TY != ty) continue;
+        const float coef = t.coef[b] * scale;
+        if (coef != 0.f) dz[(int64_t)a * ldd + b] = (T)(-coef * expm1f(t.lp[b]));
+    }
+}
+
+template <typename T>
+constexpr int kVec = 16 / sizeof(T);
+
+// 2048 workgroups of ranges with four rounds of loads at least
+grid_shape shape_of(int C, int B, int V) {
+    grid_shape g;
+    const int64_t threads = ceil_div(B, V);
+    g.tx_shift = 0;
+    while ((1 << g.tx_shift) < threads && (V << g.tx_shift) < kThreads) ++g.tx_shift;
+    g.col_blocks = (int)ceil_div(threads, 1 << g.tx_shift);
+    const int TY = kThreads >> g.tx_shift;
+    int64_t s = ceil_div(2048, g.col_blocks);
+    const int64_t most = ceil_div(C, 16 * TY);
+    s = s < most ? s : most;
+    g.rows = (int)ceil_div(C, s);
+    g.splits = (int)ceil_div(C, g.rows);
+    return g;
+}
+
+struct carved {
+    float2 *part;
+    token_out t;
+    double *pair_loss;
+    size_t bytes;
+};
+
+carved carve(int C, int B, int pairs, void *ws) {
+    carved r;
+    char *p = static_cast<char *>(ws);
+    auto take = [&](size_t n) {
+        char *q = p;
+        p += (n + 255) / 256 * 256;
+        return q;
+    };
+    // room for either vector width: the scalar one has the most ranges
+    int splits = 0;
+    for (int v : {1, 4, 8})
+        if (B >= v) splits = std::max(splits, shape_of(C, B, v).splits);
+    r.part = reinterpret_cast<float2 *>(take(sizeof(float2) * (size_t)B * splits));
+    r.t.m = reinterpret_cast<float *>(take(sizeof(float) * B));
+    r.t.inv = reinterpret_cast<float *>(take(sizeof(float) * B));
+    r.t.coef = reinterpret_cast<float *>(take(sizeof(float) * B));
+    r.t.lp = reinterpret_cast<float *>(take(sizeof(float) * B));
+    r.t.sums = reinterpret_cast<double *>(take(sizeof(double) * 4 * kTokenBlocks));
+    r.pair_loss = reinterpret_cast<double *>(take(sizeof(double) * pairs));
+    r.bytes = (size_t)(p - static_cast<char *>(ws));
+    return r;
+}
+
+template <typename T, int V, int KIND>
+hipError_t run(const token_loss_args &a, const policy_args &P, void *ws, hipStream_t s) {
+    const grid_shape g = shape_of(a.C, a.B, V);
+    carved w = carve(a.C, a.B, a.pairs, ws);
+    token_out t = w.t;
+    if (a.logp) t.lp = a.logp;
+    const T *z = static_cast<const T *>(a.logits);
+    const dim3 grid((unsigned)g.col_blocks, (unsigned)g.splits);
+    column_sums_kernel<T, V><<<grid, kThreads, 0, s>>>(a.C, a.B, z, a.ld, a.labels, a.weights, g, w.part);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    int shift = 0;
+    while ((1 << shift) < g.splits && shift < 6) ++shift;
+    int blocks = (int)ceil_div(a.B, kThreads >> shift);
+    if (blocks > kTokenBlocks) blocks = kTokenBlocks;
+    token_kernel<T, KIND><<<blocks, kThreads, 0, s>>>(a.C, a.B, z, a.ld, a.labels, a.weights, g.splits, shift, w.part,
+                                                      P, t);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    if constexpr (KIND == kLogp) return hipSuccess;
+    else {
+        int n = blocks;
+        if (KIND == kPreference) {
+            n = a.pairs;
+            if (n > 0) {
+                pair_kernel<<<n, kThreads, 0, s>>>(a.C, a.B, n, a.labels, a.weights, a.seq_ptr, a.ref_logp, a.beta,
+                                                   a.smoothing, t.lp, t.coef, a.rewards, w.pair_loss);
+                e = hipGetLastError();
+                if (e != hipSuccess) return e;
+            }
+            t.sums = w.pair_loss;
+        }
+        if (a.dlogits == nullptr)
+            finish_kernel<KIND><<<1, kThreads, 0, s>>>(n, t.sums, P.kl_coef, a.out);
+        else
+            gradient_kernel<T, V, KIND><<<grid, kThreads, 0, s>>>(a.C, a.B, z, a.ld, a.labels, g, t,
+                                                                  static_cast<T *>(a.dlogits), a.ldd, n, P.kl_coef, a.out);
+        return hipGetLastError();
+    }
+}
+
+template <typename T, int KIND>
+hipError_t run_vec(const token_loss_args &a, const policy_args &P, void *ws, hipStream_t s) {
+    return a.B >= kVec<T> ? run<T, kVec<T>, KIND>(a, P, ws, s) : run<T, 1, KIND>(a, P, ws, s);
+}
+
+template <int KIND>
+hipError_t run_type(const token_loss_args &a, const policy_args &P, void *ws, hipStream_t s) {
+    if (a.dtype == kTypeF32) return run_vec<float, KIND>(a, P, ws, s);
+    if (a.dtype == kTypeBF16) return run_vec<__bf16, KIND>(a, P, ws, s);
+    return run_vec<_Float16, KIND>(a, P, ws, s);
+}
+
+}  // namespace
+
+size_t token_loss_workspace_bytes(int C, int B, int pairs) {
+    return C > 0 && B >= 0 && pairs >= 0 ? carve(C, B, pairs, nullptr).bytes : 0;
+}
+
+hipError_t launch_token_logp(const token_loss_args &a, void *ws, hipStream_t s) {
+    return a.B == 0 ? hipSuccess : run_type<kLogp>(a, policy_args{}, ws, s);
+}
+
+hipError_t launch_policy_loss(const token_loss_args &a, void *ws, hipStream_t s) {
+    if (a.B == 0) return launch_fill_f32(a.out, 4, 0.f, s);
+    return run_type<kPolicy>(a, policy_args{a.old_logp, a.adv, a.ref_logp, 1.f - a.clip_low, 1.f + a.clip_high, a.kl_coef},
+                             ws, s);
+}
+
+hipError_t launch_preference_loss(const token_loss_args &a, void *ws, hipStream_t s) {
+    if (a.B == 0) {  // empty sequences: the loss of the reference alone
+        const carved w = carve(a.C, 0, a.pairs, ws);
+        if (a.pairs > 0)
+            pair_kernel<<<a.pairs, kThreads, 0, s>>>(a.C, 0, a.pairs, a.labels, a.weights, a.seq_ptr, a.ref_logp,
+                                                     a.beta, a.smoothing, nullptr, nullptr, a.rewards, w.pair_loss);
+        finish_kernel<kPreference><<<1, kThreads, 0, s>>>(a.pairs, w.pair_loss, 0.f, a.out);
+        return hipGetLastError();
+    }
+    return run_type<kPreference>(a, policy_args{}, ws, s);
+}
+
+}  // namespace l1csr

@@ -14,7 +14,9 @@ threshold to its own result and counts the survivors per 32-column word) and
 csr_recompress_counted, so the dense Z = S_t(W - eta G) is written once and
 read once by the recompression, and G itself is never stored.  With an adaptive solver
 (Algorithms 1-2) G is stored and the preconditioned step is fused with the
-recompression instead (prox_adaptive_recompress).
+recompression instead (prox_adaptive_recompress); with Prox-Muon G is stored, the
+orthogonalised update written over it and its prox step fused with the
+recompression (prox_muon_recompress).
 
 Only the forward product has to finish before the rest: dY is the upstream
 gradient of Y.  The calls keep the dependencies of a training loop and run on
@@ -50,9 +52,9 @@ for every entry point under capture, W's nnz must be known on the host
 """
 from __future__ import annotations
 
-from . import (CSC, CSR, F32, OP_SPMM, OP_SPMM_PACKED, AdaptiveState, Bitmap, SpmmPlan, csc_build, csr_bitmap_build,
+from . import (CSC, CSR, F32, OP_SPMM, OP_SPMM_PACKED, AdaptiveState, Bitmap, MuonState, SpmmPlan, csc_build, csr_bitmap_build,
                csr_recompress_counted, csr_spmm_bwd_t, csr_spmm_bwd_t_plan, csr_spmm_bwd_t_planned, csr_spmm_fwd,
-               dense_wgrad, dense_wgrad_prox, prox_adaptive_recompress, workspace_bytes)
+               dense_wgrad, dense_wgrad_prox, prox_adaptive_recompress, prox_muon_recompress, workspace_bytes)
 
 _side_streams: dict = {}
 _plans: dict = {}
@@ -109,14 +111,15 @@ def two_stream_pays(W: CSR, B: int) -> bool:
 
 def l1_step(W: CSR, X, dY, eta: float, lam: float, *, Y, dX, dW, csc: CSC, out: CSR,
             precision: int = F32, side=None, events: dict | None = None,
-            schedule: str = "auto", adaptive: AdaptiveState | None = None,
+            schedule: str = "auto", adaptive: AdaptiveState | MuonState | None = None,
             bitmap: Bitmap | None = None) -> CSR:
     """Run one l1 step on the caller's current stream plus a side stream.
 
     W is the N x K layer (CSR, nnz known on the host or read from the device),
     X the K x B input, dY the N x B upstream gradient.  Results go to the
     caller's buffers: Y (N x B), dX (K x B), dW (N x K: the dense prox result
-    Z = S_t(W - eta G) of the plain step, the gradient G of an adaptive one),
+    Z = S_t(W - eta G) of the plain step, the gradient G of an adaptive one, the update O of a
+    Prox-Muon one),
     csc (the CSC copy of W, capacity >= nnz) and out (W' in CSR, capacity N*K).
     precision selects the dense weight gradient's arithmetic (F32 or BF16X3).
     side: the stream to fork onto (default: one per device).  events: optional
@@ -125,11 +128,12 @@ def l1_step(W: CSR, X, dY, eta: float, lam: float, *, Y, dX, dW, csc: CSC, out: 
     "csr_spmm_bwd_t_plan" (two streams only), "csr_spmm_bwd_t",
     "dense_wgrad_prox", "csr_recompress_counted"; adaptive:
     "dense_wgrad",
-    "prox_adaptive_recompress").  schedule: "two_stream", "serial" (every call on the
+    "prox_adaptive_recompress" or "prox_muon_recompress").  schedule: "two_stream", "serial" (every call on the
     caller's stream) or "auto" (two_stream where two_stream_pays()).
     adaptive: Prox-RMSProp / Prox-ADAM state with dense [N][K] m, v; the step
     then ends with prox_adaptive_recompress (state updated in place, t
-    advanced) instead of dense_wgrad_prox + csr_recompress_counted.  bitmap: buffers for
+    advanced) instead of dense_wgrad_prox + csr_recompress_counted; a MuonState ends it with
+    prox_muon_recompress (st.m updated in place).  bitmap: buffers for
     W's bitmap index (Bitmap.empty(N, K), shared by the CSC build and the weight
     update); allocated per call if None.  All
     outputs are ready on the
@@ -193,6 +197,10 @@ def l1_step(W: CSR, X, dY, eta: float, lam: float, *, Y, dX, dW, csc: CSC, out: 
              lambda: counts.setdefault("wc", dense_wgrad_prox(W, dY, X, eta, lam, bitmap, Z=dW, precision=precision,
                                                               stream=main)[1]))
         call("csr_recompress_counted", main, lambda: csr_recompress_counted(dW, counts["wc"], out=out, stream=main))
+    elif isinstance(adaptive, MuonState):
+        call("dense_wgrad", main, lambda: dense_wgrad(dY, X, dW, precision=precision, stream=main))
+        call("prox_muon_recompress", main,
+             lambda: prox_muon_recompress(W, dW, adaptive, eta, lam, O=dW, out=out, stream=main))
     else:
         call("dense_wgrad", main, lambda: dense_wgrad(dY, X, dW, precision=precision, stream=main))
         call("prox_adaptive_recompress", main,
