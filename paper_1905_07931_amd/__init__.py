@@ -1341,10 +1341,10 @@ def orthogonalize(G, out=None, steps=5, eps=1e-7, scale=1.0, precision=None, str
     """scale * NS(G / (|G|_F + eps)): `steps` quintic Newton-Schulz steps (muon_update without momentum).
 
     G [N][K] float32, bfloat16 or float16; out, of the same shape and type, may be G itself.  precision: F32 (fp32
-    accuracy) or F16 (operands rounded to fp16, about 1.5e-3 of the norm off); by default F32 for a float32 G and F16
-    for the 16-bit types.  Returns out."""
+    accuracy) or F16 (operands rounded to fp16, about 1.5e-3 of the norm off, less than a bfloat16 result's own
+    rounding); by default F16 for a bfloat16 G and F32 for the others.  Returns out."""
     if precision is None:
-        precision = F32 if _dtype_code(G, "G") == 0 else F16
+        precision = F16 if _dtype_code(G, "G") == 1 else F32
     if out is None:
         N, K, _, _ = _typed_mat(G, "G")
         out = _new((N, K), G.dtype, G.device, stream)

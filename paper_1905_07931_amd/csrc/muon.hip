@@ -26,6 +26,7 @@
 // two: a X is added from both, or the rounding of X, which spreads into
 // directions that U lacks, would grow 3.4-fold a step (1.4e-2 off at rank 64 of
 // 300 x 784 against 8e-4).
+#include <algorithm>
 #include <cmath>
 #include <utility>
 
@@ -66,13 +67,17 @@ __device__ __forceinline__ float to_f32(float x) { return x; }
 __device__ __forceinline__ float to_f32(_Float16 x) { return (float)x; }
 __device__ __forceinline__ float to_f32(__bf16 x) { return (float)x; }
 
-__device__ __forceinline__ double block_sum(double x, double *lds) {  // 256 threads
+template <int waves>
+__device__ __forceinline__ double block_sum(double x, double *lds) {
 #pragma unroll
     for (int d = kWave / 2; d >= 1; d >>= 1) x += __shfl_xor(x, d, kWave);
     __syncthreads();
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
     __syncthreads();
-    return (lds[0] + lds[1]) + (lds[2] + lds[3]);
+    double t = lds[0];
+#pragma unroll
+    for (int w = 1; w < waves; ++w) t += lds[w];
+    return t;
 }
 
 // ---------------------------------------------------------------------------
@@ -91,7 +96,6 @@ struct update_src {
     int N, K;
 };
 
-template <typename T>
 __device__ __forceinline__ float update_at(const update_src &u, float g, float m_new) {
     return u.M == nullptr ? g : (u.nesterov ? fmaf(u.mu, m_new, g) : m_new);
 }
@@ -125,7 +129,7 @@ __global__ __launch_bounds__(256) void momentum_kernel(update_src u, double *__r
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             mv[e] = fmaf(u.mu, mv[e], to_f32(gv[e]));
-            const double x = (double)update_at<T>(u, to_f32(gv[e]), mv[e]);
+            const double x = (double)update_at(u, to_f32(gv[e]), mv[e]);
             if (e < n) sum = fma(x, x, sum);
         }
         if (o == nullptr) continue;
@@ -136,7 +140,7 @@ __global__ __launch_bounds__(256) void momentum_kernel(update_src u, double *__r
             for (int e = 0; e < 4; ++e)
                 if (e < n) o[e] = mv[e];
     }
-    sum = block_sum(sum, lds);
+    sum = block_sum<4>(sum, lds);
     if (threadIdx.x == 0) part[blockIdx.x] = sum;
 }
 
@@ -154,18 +158,14 @@ struct parts_of {
     }
 };
 
-// 2^14 2^e U packed by rows (X) and by columns (X^T); 2^e |U|_F in [1/2, 1).
-// scal[0] = s, scal[1] = s^2 with s = 1 / (2^e (|U|_F + eps)).  A workgroup takes 64 x 64 of X.
-template <typename T>
-__global__ __launch_bounds__(256) void pack_update_kernel(update_src u, int tall, const double *__restrict__ part,
-                                                          int n_part, float eps, packed_half X, packed_half Xt,
-                                                          float *__restrict__ scal) {
-    constexpr int LD = 65;
-    __shared__ float tile[64 * LD];
-    __shared__ double lds[4];
+// e with 2^e |U|_F in [1/2, 1), returned negated; scal[0] = s, scal[1] = s^2 with
+// s = 1 / (2^e (|U|_F + eps))
+template <int waves>
+__device__ __forceinline__ int scale_of(const double *part, int n_part, float eps, float *scal, bool write,
+                                        double *lds) {
     double sum = 0;
-    for (int i = threadIdx.x; i < n_part; i += 256) sum += part[i];
-    const double norm = sqrt(block_sum(sum, lds));
+    for (int i = threadIdx.x; i < n_part; i += waves * kWave) sum += part[i];
+    const double norm = sqrt(block_sum<waves>(sum, lds));
     int e = 0;
     double s;
     if (norm < INFINITY) {
@@ -175,46 +175,388 @@ __global__ __launch_bounds__(256) void pack_update_kernel(update_src u, int tall
     } else {
         s = NAN;  // an infinity or a NaN in U, or a norm past double: nothing to give
     }
-    if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) {
+    if (write && threadIdx.x == 0) {
         scal[0] = (float)s;
         scal[1] = (float)(s * s);
     }
+    return e;
+}
+
+// V elements of U (0 past its ends): every load in flight before the first is used
+template <typename T, int V, typename At>
+__device__ __forceinline__ void load_update(const update_src &u, At at, float (&x)[V]) {
+    const T *G = static_cast<const T *>(u.G);
+    T g[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        int r, c;
+        at(v, r, c);
+        g[v] = G[(int64_t)min(r, u.N - 1) * u.ldg + min(c, u.K - 1)];
+    }
+    float m[V] = {};
+    if (u.M) {
+        const float *M = u.M_out ? u.M_out : u.M;
+        const int64_t ld = u.M_out ? u.ldo : u.ldm;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            int r, c;
+            at(v, r, c);
+            m[v] = M[(int64_t)min(r, u.N - 1) * ld + min(c, u.K - 1)];
+        }
+        if (u.M_out == nullptr)
+#pragma unroll
+            for (int v = 0; v < V; ++v) m[v] = fmaf(u.mu, m[v], to_f32(g[v]));
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        int r, c;
+        at(v, r, c);
+        x[v] = r < u.N && c < u.K ? update_at(u, to_f32(g[v]), m[v]) : 0.f;
+    }
+}
+
+// 2^14 2^e U packed by rows (X) and by columns (X^T).  A workgroup takes 64 x 64 of X.
+template <typename T>
+__global__ __launch_bounds__(256) void pack_update_kernel(update_src u, int tall, const double *__restrict__ part,
+                                                          int n_part, float eps, packed_half X, packed_half Xt,
+                                                          float *__restrict__ scal) {
+    constexpr int LD = 65;
+    __shared__ float tile[64 * LD];
+    __shared__ double lds[4];
     const int i0 = blockIdx.y * 64, j0 = blockIdx.x * 64;  // of X
     const int r0 = tall ? j0 : i0, c0 = tall ? i0 : j0;    // of U
-    const T *G = static_cast<const T *>(u.G);
     const int col = threadIdx.x & 63, q = threadIdx.x >> 6;
-#pragma unroll 4
-    for (int r = q; r < 64; r += 4) {
-        float x = 0.f;
-        if (r0 + r < u.N && c0 + col < u.K) {
-            const float g = to_f32(G[(int64_t)(r0 + r) * u.ldg + c0 + col]);
-            float m = 0.f;
-            if (u.M)
-                m = u.M_out ? u.M_out[(int64_t)(r0 + r) * u.ldo + c0 + col]
-                            : fmaf(u.mu, u.M[(int64_t)(r0 + r) * u.ldm + c0 + col], g);
-            x = ldexpf(update_at<T>(u, g, m), kScaleX - e);
-        }
-        tile[tall ? col * LD + r : r * LD + col] = x;
+    float x[16];
+    load_update<T>(u, [&](int v, int &r, int &c) { r = r0 + q + 4 * v; c = c0 + col; }, x);
+    const int e = scale_of<4>(part, n_part, eps, scal, blockIdx.x == 0 && blockIdx.y == 0, lds);
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+        const int r = q + 4 * v;
+        tile[tall ? col * LD + r : r * LD + col] = ldexpf(x[v], kScaleX - e);
     }
     __syncthreads();
     const int lane = threadIdx.x & 63, l = lane & 31, h = lane >> 5;
-    for (int b = q; b < 16; b += 4) {  // blocks of X, then of X^T
+#pragma unroll
+    for (int b = 0; b < 16; b += 4) {  // blocks of X, then of X^T
         const bool t = b >= 8;
         const packed_half &o = t ? Xt : X;
-        const int gg = b >> 2 & 1, ss = b & 3;
+        const int gg = b >> 2 & 1, ss = q;
         const int g = (t ? j0 : i0) / kGroup + gg, st = (t ? i0 : j0) / kStep + ss;
         if (g >= o.groups || st >= o.steps) continue;
-        float x[8];
+        float y[8];
 #pragma unroll
         for (int v = 0; v < 8; ++v) {
             const int row = gg * 32 + l, k = ss * 16 + h * 8 + v;
-            x[v] = t ? tile[k * LD + row] : tile[row * LD + k];
+            y[v] = t ? tile[k * LD + row] : tile[row * LD + k];
         }
-        const parts_of<8> p(x);
+        const parts_of<8> p(y);
         char *d = o.data + ((int64_t)g * o.steps + st) * (o.parts * kBlock) + lane * 16;
         *reinterpret_cast<halfx8 *>(d) = p.hi;
         if (o.parts == 2) *reinterpret_cast<halfx8 *>(d + kBlock) = p.lo;
     }
+}
+
+// ---------------------------------------------------------------------------
+// m <= 128: a step in one launch
+// ---------------------------------------------------------------------------
+//
+// Such matrices are bound by the launches' own time.  A workgroup holds all of A (the
+// sums over the column ranges of X, added up by every workgroup) and a slice of
+// 64 columns of X: it takes Y = A X, X' = a X + b Y + c A Y and, with X' still in LDS,
+// the slice's part of X' X'^T.  One product more than with the polynomial of A made
+// ahead, on a slice that one workgroup multiplies in a microsecond.  Many ranges are
+// summed by a launch of their own first.
+
+constexpr int kSmall = 128;       // most rows of X
+constexpr int kSlice = 64;        // columns of X a workgroup takes at a time
+constexpr int kSliceSteps = kSlice / kStep;
+constexpr int kMostRanges = 192;  // partial sums of A
+constexpr int kSumRanges = 8;     // more are summed ahead
+
+// partial sums of A: [range][32 x 32 tile, ti <= tj by columns][register][lane]
+__host__ __device__ constexpr int tiles_of(int g) { return g * (g + 1) / 2; }
+__device__ __forceinline__ void tile_of(int t, int &ti, int &tj) {
+    tj = t >= 6 ? 3 : (t >= 3 ? 2 : (t >= 1 ? 1 : 0));
+    ti = t - tj * (tj + 1) / 2;
+}
+
+// byte of element (row, k) of a two-part operand, first part
+__device__ __forceinline__ int element_at(int row, int k, int steps) {
+    return ((row >> 5) * steps + (k >> 4)) * (2 * kBlock) + ((row & 31) + 32 * ((k >> 3) & 1)) * 16 + (k & 7) * 2;
+}
+
+__device__ __forceinline__ void product_step(const char *pa, const char *pb, floatx16 &acc, floatx16 &low) {
+    const halfx8 ah = *reinterpret_cast<const halfx8 *>(pa), al = *reinterpret_cast<const halfx8 *>(pa + kBlock);
+    const halfx8 bh = *reinterpret_cast<const halfx8 *>(pb), bl = *reinterpret_cast<const halfx8 *>(pb + kBlock);
+    acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(ah, bh, acc, 0, 0, 0);
+    low = __builtin_amdgcn_mfma_f32_32x32x16_f16(al, bh, low, 0, 0, 0);
+    low = __builtin_amdgcn_mfma_f32_32x32x16_f16(ah, bl, low, 0, 0, 0);
+}
+
+// The products of this wave's tiles of X X^T over a slice, packed by rows in LDS
+template <int g, int waves, int per>
+__device__ __forceinline__ void gram_slice(const char *X, int wave, int lane, floatx16 (&acc)[per], floatx16 (&low)[per]) {
+#pragma unroll
+    for (int x = 0; x < per; ++x) {
+        const int t = wave + waves * x;
+        if (t >= tiles_of(g)) continue;
+        int ti, tj;
+        tile_of(t, ti, tj);
+#pragma unroll
+        for (int st = 0; st < kSliceSteps; ++st)
+            product_step(X + (ti * kSliceSteps + st) * (2 * kBlock) + lane * 16,
+                         X + (tj * kSliceSteps + st) * (2 * kBlock) + lane * 16, acc[x], low[x]);
+    }
+}
+
+template <int g, int waves, int per>
+__device__ __forceinline__ void store_gram(float *partial, int wave, int lane, const floatx16 (&acc)[per],
+                                           const floatx16 (&low)[per]) {
+#pragma unroll
+    for (int x = 0; x < per; ++x) {
+        const int t = wave + waves * x;
+        if (t >= tiles_of(g)) continue;
+        float *d = partial + ((int64_t)blockIdx.x * tiles_of(g) + t) * (16 * kWave) + lane;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) d[r * kWave] = acc[x][r] + low[x][r];
+    }
+}
+
+// 2^14 2^e U by slices: X^T packed, and the first A's partial sums
+template <int g>
+constexpr int kPackWaves = g > 2 ? 8 : 4;
+
+template <typename T, int g>
+__global__ __launch_bounds__(kPackWaves<g> *kWave) void small_pack_kernel(update_src u, int tall,
+                                                         const double *__restrict__ part, int n_part, float eps, packed_half Xt, int m, int n,
+                                                         float *__restrict__ scal, float *__restrict__ partial) {
+    constexpr int LD = kSlice + 1, rows = 32 * g, waves = kPackWaves<g>, each = rows / waves;
+    __shared__ float tile[rows * LD];
+    __shared__ __attribute__((aligned(16))) char X[g * kSliceSteps * 2 * kBlock];
+    __shared__ double lds[waves];
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+    const int l = lane & 31, h = lane >> 5;
+    constexpr int per = (tiles_of(g) + waves - 1) / waves;
+    floatx16 acc[per] = {}, low[per] = {};
+    int e = 0;
+    for (int j0 = blockIdx.x * kSlice; j0 < n; j0 += gridDim.x * kSlice) {
+        // along U's rows; element v of a thread is (i, j) of X
+        float x[each];
+        auto at = [&](int v, int &i, int &j) {
+            const int f = threadIdx.x + waves * kWave * v;
+            i = tall ? f % rows : f / kSlice;
+            j = tall ? f / rows : f % kSlice;
+        };
+        load_update<T>(u, [&](int v, int &r, int &c) {
+            int i, j;
+            at(v, i, j);
+            r = tall ? j0 + j : i;
+            c = tall ? i : j0 + j;
+        }, x);
+        if (j0 == (int)blockIdx.x * kSlice) e = scale_of<waves>(part, n_part, eps, scal, blockIdx.x == 0, lds);
+        __syncthreads();  // the last slice is read
+#pragma unroll
+        for (int v = 0; v < each; ++v) {
+            int i, j;
+            at(v, i, j);
+            tile[i * LD + j] = ldexpf(x[v], kScaleX - e);
+        }
+        __syncthreads();
+        for (int b = wave; b < 8 * g; b += waves) {  // blocks of X^T, then of X
+            const bool t = b < 4 * g;
+            const int c = t ? b : b - 4 * g;
+            const int gr = t ? c & 1 : c / kSliceSteps, st = t ? c >> 1 : c % kSliceSteps;
+            float y[8];
+#pragma unroll
+            for (int v = 0; v < 8; ++v) {
+                const int k = st * kStep + 8 * h + v, r = gr * 32 + l;
+                y[v] = t ? tile[k * LD + r] : tile[r * LD + k];
+            }
+            const parts_of<8> p(y);
+            char *d = X + (gr * kSliceSteps + st) * (2 * kBlock) + lane * 16;
+            if (t) {
+                const int row = j0 / kGroup + gr;
+                if (row >= Xt.groups) continue;
+                d = Xt.data + ((int64_t)row * Xt.steps + st) * (2 * kBlock) + lane * 16;
+            }
+            *reinterpret_cast<halfx8 *>(d) = p.hi;
+            *reinterpret_cast<halfx8 *>(d + kBlock) = p.lo;
+        }
+        __syncthreads();
+        gram_slice<g, waves, per>(X, wave, lane, acc, low);
+    }
+    store_gram<g, waves, per>(partial, wave, lane, acc, low);
+}
+
+// s[q] = the sum over the ranges of the four floats at p + q * apart, a range every
+// `stride` floats, U ranges in flight (past the last the last again, not added)
+template <int n, int U>
+__device__ __forceinline__ void sum_ranges(const float *p, int apart, int ranges, int64_t stride, float4 (&s)[n]) {
+#pragma unroll
+    for (int q = 0; q < n; ++q) s[q] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int r = 0; r < ranges; r += U) {
+        float4 v[U][n];
+#pragma unroll
+        for (int w = 0; w < U; ++w)
+#pragma unroll
+            for (int q = 0; q < n; ++q)
+                v[w][q] = *reinterpret_cast<const float4 *>(p + min(r + w, ranges - 1) * stride + q * apart);
+#pragma unroll
+        for (int w = 0; w < U; ++w)
+#pragma unroll
+            for (int q = 0; q < n; ++q) {
+                const bool on = r + w < ranges;
+                s[q].x += on ? v[w][q].x : 0.f;
+                s[q].y += on ? v[w][q].y : 0.f;
+                s[q].z += on ? v[w][q].z : 0.f;
+                s[q].w += on ? v[w][q].w : 0.f;
+            }
+    }
+}
+
+// four neighbours (one row i, columns j ..) of a symmetric operand's tile to both their places
+__device__ __forceinline__ void place_sums(char *A, int steps, int index, float4 s, float scale) {
+    int ti, tj;
+    tile_of(index >> 10, ti, tj);
+    const int reg = index >> 6 & 15, ln = index & 63;
+    const int i = ti * 32 + 8 * (reg >> 2) + 4 * (ln >> 5) + (reg & 3), j = tj * 32 + (ln & 31);
+    const float x[4] = {s.x * scale, s.y * scale, s.z * scale, s.w * scale};
+    const parts_of<4> p(x);
+    if (ti != tj) {
+        char *d = A + element_at(i, j, steps);
+        *reinterpret_cast<halfx4 *>(d) = p.hi;
+        *reinterpret_cast<halfx4 *>(d + kBlock) = p.lo;
+    }
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+        char *d = A + element_at(j + v, i, steps);
+        *reinterpret_cast<_Float16 *>(d) = p.hi[v];
+        *reinterpret_cast<_Float16 *>(d + kBlock) = p.lo[v];
+    }
+}
+
+__global__ __launch_bounds__(256) void small_sum_kernel(const float *__restrict__ partial, int ranges, int tiles,
+                                                        const float *__restrict__ scal, packed_half A) {
+    const int i = (blockIdx.x * 256 + threadIdx.x) * 4;
+    if (i >= tiles * 1024) return;
+    float4 s[1];
+    sum_ranges<1, 16>(partial + i, 0, ranges, (int64_t)tiles * 1024, s);
+    place_sums(A.data, A.steps, i, s[0], (scal ? scal[1] : 1.f) * 0x1p-14f);
+}
+
+// One step; A from its ranges' sums, or packed where they were summed ahead (ranges = 0).
+// LAST: O, else X^T packed and the next A's partial sums.  2 g waves: a 32 x 32 tile of the slice each.
+template <typename T, bool LAST, int g>
+__global__ __launch_bounds__(2 * g *kWave) void small_step_kernel(const float *__restrict__ sums, int ranges,
+                                                                  packed_half A, packed_half Xt, int m, int n,
+                                                                  const float *__restrict__ scal, packed_half out,
+                                                                  float *__restrict__ partial, T *__restrict__ O,
+                                                                  int64_t ldo, int tall, float scale) {
+    constexpr int steps = 2 * g, waves = 2 * g, per = (tiles_of(g) + waves - 1) / waves;
+    __shared__ __attribute__((aligned(16))) char LA[g * steps * 2 * kBlock];
+    __shared__ __attribute__((aligned(16))) char LY[2 * steps * 2 * kBlock];
+    __shared__ __attribute__((aligned(16))) char LX[LAST ? 16 : g * kSliceSteps * 2 * kBlock];
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+    const int l = lane & 31, h = lane >> 5;
+    const int gi = wave >> 1, wj = wave & 1;
+    const float dev = scal ? scal[0] : 1.f, f = dev * scale;
+    halfx8 xh[steps], xl[steps];  // the slice's fragments, ahead of what the products wait for
+    auto load = [&](int j0) {
+        // (a group past the end: the last one's, not stored and zeroed where it would count)
+        const char *p = Xt.data + (int64_t)min(j0 / kGroup + wj, Xt.groups - 1) * steps * (2 * kBlock) + lane * 16;
+#pragma unroll
+        for (int st = 0; st < steps; ++st) {
+            xh[st] = *reinterpret_cast<const halfx8 *>(p + st * (2 * kBlock));
+            xl[st] = *reinterpret_cast<const halfx8 *>(p + st * (2 * kBlock) + kBlock);
+        }
+    };
+    load(blockIdx.x * kSlice);
+    if (ranges > 0) {
+        constexpr int items = tiles_of(g) * 256, threads = waves * kWave, each = items / threads;
+        static_assert(items % threads == 0, "whole rounds");
+        float4 a[each];
+        sum_ranges<each, 4>(sums + threadIdx.x * 4, threads * 4, ranges, tiles_of(g) * 1024, a);
+#pragma unroll
+        for (int q = 0; q < each; ++q)
+            place_sums(LA, steps, (threadIdx.x + q * threads) * 4, a[q], dev * dev * 0x1p-14f);
+    } else {
+        for (int i = threadIdx.x * 16; i < g * steps * 2 * kBlock; i += waves * kWave * 16)
+            *reinterpret_cast<float4 *>(LA + i) = *reinterpret_cast<const float4 *>(A.data + i);
+    }
+    __syncthreads();
+    floatx16 acc[per] = {}, low[per] = {};
+    for (int j0 = blockIdx.x * kSlice; j0 < n; j0 += gridDim.x * kSlice) {
+        const int gj = j0 / kGroup + wj;
+        const bool on = gj < Xt.groups;
+        const char *xt = Xt.data + (int64_t)min(gj, Xt.groups - 1) * steps * (2 * kBlock);
+        floatx16 y = {}, z = {}, s = {};
+#pragma unroll
+        for (int st = 0; st < steps; ++st) {
+            const char *p = LA + (gi * steps + st) * (2 * kBlock) + lane * 16;
+            const halfx8 ah = *reinterpret_cast<const halfx8 *>(p), al = *reinterpret_cast<const halfx8 *>(p + kBlock);
+            y = __builtin_amdgcn_mfma_f32_32x32x16_f16(ah, xh[st], y, 0, 0, 0);
+            s = __builtin_amdgcn_mfma_f32_32x32x16_f16(al, xh[st], s, 0, 0, 0);
+            s = __builtin_amdgcn_mfma_f32_32x32x16_f16(ah, xl[st], s, 0, 0, 0);
+        }
+        const int mine = 2 * gi * (2 * kBlock) + l * 16 + 8 * h;  // this tile in the rows of X^T and Y^T
+        halfx4 th[4], tl[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const char *p = xt + mine + (q >> 1) * (2 * kBlock) + (q & 1) * 512;
+            th[q] = *reinterpret_cast<const halfx4 *>(p);
+            tl[q] = *reinterpret_cast<const halfx4 *>(p + kBlock);
+        }
+        if (j0 + (int)gridDim.x * kSlice < n) load(j0 + gridDim.x * kSlice);
+        y = (y + s) * 0x1p-14f;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const float v[4] = {y[4 * q], y[4 * q + 1], y[4 * q + 2], y[4 * q + 3]};
+            const parts_of<4> p(v);
+            char *d = LY + wj * steps * (2 * kBlock) + mine + (q >> 1) * (2 * kBlock) + (q & 1) * 512;
+            *reinterpret_cast<halfx4 *>(d) = p.hi;
+            *reinterpret_cast<halfx4 *>(d + kBlock) = p.lo;
+        }
+        __syncthreads();
+        s = floatx16{};
+#pragma unroll
+        for (int st = 0; st < steps; ++st)
+            product_step(LA + (gi * steps + st) * (2 * kBlock) + lane * 16,
+                         LY + (wj * steps + st) * (2 * kBlock) + lane * 16, z, s);
+        z = (z + s) * 0x1p-14f;
+        const int j = gj * 32 + l;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int to = mine + (q >> 1) * (2 * kBlock) + (q & 1) * 512;
+            float v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float x = (float)th[q][e] + (float)tl[q][e];
+                v[e] = on ? f * fmaf(kC, z[4 * q + e], fmaf(kB, y[4 * q + e], kA * x)) : 0.f;
+            }
+            const int i = gi * 32 + 8 * q + 4 * h;
+            if constexpr (LAST) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (i + e < m && j < n) O[tall ? j * ldo + i + e : (i + e) * ldo + j] = (T)v[e];
+            } else {
+                const parts_of<4> p(v);
+                if (on) {
+                    char *d = out.data + (int64_t)gj * steps * (2 * kBlock) + to;
+                    *reinterpret_cast<halfx4 *>(d) = p.hi;
+                    *reinterpret_cast<halfx4 *>(d + kBlock) = p.lo;
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    char *d = LX + element_at(i + e, wj * 32 + l, kSliceSteps);
+                    *reinterpret_cast<_Float16 *>(d) = p.hi[e];
+                    *reinterpret_cast<_Float16 *>(d + kBlock) = p.lo[e];
+                }
+            }
+        }
+        __syncthreads();  // Y is read (and X' stored)
+        if constexpr (!LAST) gram_slice<g, waves, per>(LX, wave, lane, acc, low);
+    }
+    if constexpr (!LAST) store_gram<g, waves, per>(partial, wave, lane, acc, low);
 }
 
 // ---------------------------------------------------------------------------
@@ -233,7 +575,8 @@ struct tile_shape {
 struct product_args {
     packed_half A, B;           // D[i][j] = sum_k A[i][k] B[j][k]
     int rows, cols;             // of D
-    int tiles_m, tiles_n, symmetric;  // symmetric: D = D^T, tiles with tm <= tn only
+    int tiles_m, tiles_n;
+    int symmetric;              // D = D^T: only tiles with a 32 x 32 block on or above the diagonal
     // v = dev (al D + be E) + ga [i == j]
     float al, be, ga;
     const float *dev;           // nullable: 1
@@ -242,13 +585,132 @@ struct product_args {
     void *O;                    // or v as a matrix: O[i][j], flipped: O[j][i]
     int64_t ldo;
     int flip;
-    float *partial;             // ranges of the reduction: [range][tile][lane order]
-    int ranges, range_stages;   // 1: the whole reduction
+    // The first `whole` of `tiles` tiles take a workgroup each, the others `ranges`:
+    // partial sums [range][tile - whole][lane order], joined by a second launch.
+    int tiles, whole, ranges, range_stages;
+    float *partial;
 };
 
-enum { kWhole = 0, kRange = 1, kJoin = 2 };  // one launch; the ranges' sums; their sum and the epilogue
+// Tiles of a symmetric product: tile column tn has those tm with a 32 x 32 block on or above the diagonal.
+template <typename S>
+__host__ __device__ __forceinline__ int column_tiles(int tn, int tiles_m) {
+    const int c = (tn * S::GB + S::GB - 1) / S::GA + 1;
+    return c < tiles_m ? c : tiles_m;
+}
+template <typename S>
+__host__ __device__ __forceinline__ int band_tiles(int first, int tiles_m, int tiles_n) {
+    int c = 0;
+    for (int tn = first; tn < first + 8 && tn < tiles_n; ++tn) c += column_tiles<S>(tn, tiles_m);
+    return c;
+}
+// Tile number t to its place: bands of 8 tile columns (other products: rows) walked across the band.
+template <typename S>
+__host__ __device__ __forceinline__ void place_of(int t, int symmetric, int tiles_m, int tiles_n, int &tm, int &tn) {
+    if (!symmetric) {
+        const int band = t / (8 * tiles_n), r = t - band * 8 * tiles_n;
+        const int h = tiles_m - band * 8 < 8 ? tiles_m - band * 8 : 8;
+        tn = r / h;
+        tm = band * 8 + (r - tn * h);
+        return;
+    }
+    int first = 0, r = t;
+    for (int c = band_tiles<S>(0, tiles_m, tiles_n); r >= c; c = band_tiles<S>(first, tiles_m, tiles_n)) {
+        r -= c;
+        first += 8;
+    }
+    const int h = tiles_n - first < 8 ? tiles_n - first : 8, all = column_tiles<S>(first, tiles_m);
+    if (r < all * h) {
+        tm = r / h;
+        tn = first + r - tm * h;
+        return;
+    }
+    r -= all * h;
+    for (tm = all;; ++tm) {  // the rows that only the band's later columns have
+        int f = first;
+        while (column_tiles<S>(f, tiles_m) <= tm) ++f;
+        const int k = first + h - f;
+        if (r < k) {
+            tn = f + r;
+            return;
+        }
+        r -= k;
+    }
+}
 
-template <int NP, typename S, int PHASE, typename O>
+constexpr int kTurned = 32 * 33;  // floats of a turned block
+
+// The epilogue of a 32 x 32 block.  Lane l, register 4 q + e holds row 8 q + 4 (l / 32) + e,
+// column l % 32: four consecutive indices of a packed row j (8 bytes a part), so
+// the matrix packed by rows j is stored from the registers, the one by rows i through LDS.
+template <typename O>
+__device__ __forceinline__ void finish_block(const product_args &P, int gi, int gj, int lane, const floatx16 &acc,
+                                             float *buf) {
+    if (gi >= P.A.groups || gj >= P.B.groups || (P.symmetric && gi > gj)) return;
+    const float dev = P.dev ? *P.dev : 1.f;
+    const int l = lane & 31, h = lane >> 5;
+    const int i0 = gi * kGroup, j = gj * kGroup + l;
+    float v[16];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        float e4[4] = {0.f, 0.f, 0.f, 0.f};
+        if (P.E.data) {
+            const char *p = P.E.data + ((int64_t)gj * P.E.steps + 2 * gi + (q >> 1)) * (P.E.parts * kBlock) +
+                            (l + 32 * (q & 1)) * 16 + 8 * h;
+            const halfx4 hi = *reinterpret_cast<const halfx4 *>(p);
+            halfx4 lo = {};
+            if (P.E.parts == 2) lo = *reinterpret_cast<const halfx4 *>(p + kBlock);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) e4[e] = (float)hi[e] + (float)lo[e];
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int i = i0 + 8 * q + 4 * h + e;
+            float x = dev * fmaf(P.al, acc[4 * q + e], P.be * e4[e]);
+            if (i == j && i < P.rows) x += P.ga;
+            v[4 * q + e] = x;
+        }
+    }
+    if (P.O) {
+        O *out = static_cast<O *>(P.O);
+        if (j < P.cols)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int i = i0 + 8 * (r >> 2) + 4 * h + (r & 3);
+                if (i < P.rows) out[P.flip ? j * P.ldo + i : i * P.ldo + j] = (O)v[r];
+            }
+        return;
+    }
+    {
+        const packed_half &o = P.out_n;
+        char *d = o.data + ((int64_t)gj * o.steps + 2 * gi) * (o.parts * kBlock) + l * 16 + 8 * h;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const float x[4] = {v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+            const parts_of<4> p(x);
+            char *to = d + (q >> 1) * (o.parts * kBlock) + (q & 1) * 512;
+            *reinterpret_cast<halfx4 *>(to) = p.hi;
+            if (o.parts == 2) *reinterpret_cast<halfx4 *>(to + kBlock) = p.lo;
+        }
+    }
+    if (P.out_t.data == nullptr || (P.symmetric && gi == gj)) return;
+    const packed_half &o = P.out_t;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) buf[(8 * (r >> 2) + 4 * h + (r & 3)) * 33 + l] = v[r];
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    char *d = o.data + ((int64_t)gi * o.steps + 2 * gj) * (o.parts * kBlock) + lane * 16;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = buf[l * 33 + 16 * s + 8 * h + e];
+        const parts_of<8> p(x);
+        *reinterpret_cast<halfx8 *>(d + s * (o.parts * kBlock)) = p.hi;
+        if (o.parts == 2) *reinterpret_cast<halfx8 *>(d + s * (o.parts * kBlock) + kBlock) = p.lo;
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+}
+
+template <int NP, typename S, typename O>
 __global__ __launch_bounds__(S::threads, 2) void product_kernel(product_args P) {
     constexpr int PIECES = (S::GA + S::GB) * NP * S::KS;  // 1 KB blocks of a stage
     constexpr int LPW = PIECES / S::waves;
@@ -258,33 +720,20 @@ __global__ __launch_bounds__(S::threads, 2) void product_kernel(product_args P) 
     __shared__ __attribute__((aligned(16))) char S0[SB];
     __shared__ __attribute__((aligned(16))) char S1[SB];
     __shared__ __attribute__((aligned(16))) char S2[SB];
-    // Tiles in bands of 8 tile rows (symmetric: tile columns) walked across the band; each XCD (blocks
-    // are dealt round-robin) takes one contiguous range, whose operand rows its L2 then holds.
-    const int T = P.symmetric ? P.tiles_n * (P.tiles_n + 1) / 2 : P.tiles_m * P.tiles_n, per = (T + 7) / 8;
-    const int t = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
-    if ((int)(blockIdx.x >> 3) >= per || t >= T) return;
-    int tm, tn;
-    if (P.symmetric) {
-        int b = 0;  // bands of 8 columns: 32 b^2 + 4 b tiles lie before band b
-        while (32 * (b + 1) * (b + 1) + 4 * (b + 1) <= t) ++b;
-        int r = t - (32 * b * b + 4 * b);
-        const int h = min(8, P.tiles_n - 8 * b);
-        if (r < 8 * b * h) {
-            tm = r / h;
-            tn = 8 * b + r - tm * h;
-        } else {
-            r -= 8 * b * h;
-            int x = 0;
-            while (r >= h - x) r -= h - x++;
-            tm = 8 * b + x;
-            tn = tm + r;
-        }
+    // Each XCD (blocks are dealt round-robin) takes one contiguous range of the whole tiles, whose
+    // operand rows its L2 then holds.
+    const int per = (P.whole + 7) / 8;
+    int t, range = -1;
+    if ((int)blockIdx.x < 8 * per) {
+        t = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
+        if (t >= P.whole) return;
     } else {
-        const int band = t / (8 * P.tiles_n), r = t - band * 8 * P.tiles_n;
-        const int h = min(8, P.tiles_m - band * 8);
-        tn = r / h;
-        tm = band * 8 + (r - tn * h);
+        const int r = (int)blockIdx.x - 8 * per;
+        t = P.whole + r / P.ranges;
+        range = r % P.ranges;
     }
+    int tm, tn;
+    place_of<S>(t, P.symmetric, P.tiles_m, P.tiles_n, tm, tn);
     const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int wk = wave / (S::WM * S::WN), wp = wave % (S::WM * S::WN);
     const int wgm = wp / S::WN * TM, wgn = wp % S::WN * TN;  // the wave's first groups in the tile
@@ -295,11 +744,11 @@ __global__ __launch_bounds__(S::threads, 2) void product_kernel(product_args P) 
 #pragma unroll
         for (int b = 0; b < TN; ++b) acc[a][b] = small[a][b] = floatx16{};
 
-    if constexpr (PHASE != kJoin) {
+    {
         const int steps = P.A.steps;
-        const int st0 = PHASE == kRange ? (int)blockIdx.y * P.range_stages : 0;
+        const int st0 = range < 0 ? 0 : range * P.range_stages;
         const int all = (steps + KS - 1) / KS;
-        const int stages = PHASE == kRange ? min(P.range_stages, all - st0) : all;
+        const int stages = range < 0 ? all : min(P.range_stages, all - st0);
         // this wave's blocks of a stage: piece p = wave + j * waves, a group's blocks side by side
         const char *src[LPW];
         int at[LPW];     // the piece's step in the stage
@@ -404,163 +853,123 @@ __global__ __launch_bounds__(S::threads, 2) void product_kernel(product_args P) 
                         for (int r = 0; r < 16; ++r)
                             acc[a][b][r] += buf[(w * S::WM * S::WN + wp) * n + ((a * TN + b) * 16 + r) * kWave + lane];
         }
-    } else if (wk > 0) {
+    }
+    if (range >= 0) {
+        float *d = P.partial + ((int64_t)range * (P.tiles - P.whole) + t - P.whole) * (GA * GB * 16 * kWave) +
+                   wp * (TM * TN * 16 * kWave) + lane;
+#pragma unroll
+        for (int a = 0; a < TM; ++a)
+#pragma unroll
+            for (int b = 0; b < TN; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) d[((a * TN + b) * 16 + r) * kWave] = acc[a][b][r];
         return;
     }
-    if constexpr (PHASE != kWhole) {
-        constexpr int n = TM * TN * 16 * kWave, per_tile = S::WM * S::WN * n;
-        float *d = P.partial + (int64_t)t * per_tile + wp * n + lane;
-        const int64_t range = (int64_t)T * per_tile;
-        if constexpr (PHASE == kRange) {
-            d += blockIdx.y * range;
-#pragma unroll
-            for (int a = 0; a < TM; ++a)
-#pragma unroll
-                for (int b = 0; b < TN; ++b)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) d[((a * TN + b) * 16 + r) * kWave] = acc[a][b][r];
-            return;
-        }
-        for (int w = 0; w < P.ranges; ++w, d += range)
-#pragma unroll
-            for (int a = 0; a < TM; ++a)
-#pragma unroll
-                for (int b = 0; b < TN; ++b)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) acc[a][b][r] += d[((a * TN + b) * 16 + r) * kWave];
-    }
 
-    // The epilogue.  Lane l, register 4 q + e of a 32 x 32 tile holds row 8 q + 4 (l / 32) + e,
-    // column l % 32: four consecutive indices of a packed row j (8 bytes a part), so
-    // the matrix packed by rows j is stored from the registers, the one by rows i through LDS.
-    const float dev = P.dev ? *P.dev : 1.f;
-    const int l = lane & 31, h = lane >> 5;
-    const bool both = P.out_t.data != nullptr && !(P.symmetric && tm == tn);
     float *buf = nullptr;
-    if (both) {
+    if (P.out_t.data != nullptr) {
         // two positions in each of two buffers that every wave has read its last
         // fragments from (behind the barrier in front of the shared sums, if there are any)
         if constexpr (S::WK == 1) __syncthreads();
-        static_assert(S::WM * S::WN <= 4 && 2 * 32 * 33 * 4 <= SB, "room for the turned tiles");
-        buf = reinterpret_cast<float *>(S::WK > 1 ? (wp < 2 ? S1 : S2) : (wp < 2 ? S0 : S1)) + (wp & 1) * (32 * 33);
+        static_assert(S::WM * S::WN <= 4 && 2 * kTurned * 4 <= SB, "room for the turned blocks");
+        buf = reinterpret_cast<float *>(S::WK > 1 ? (wp < 2 ? S1 : S2) : (wp < 2 ? S0 : S1)) + (wp & 1) * kTurned;
     }
 #pragma unroll
     for (int a = 0; a < TM; ++a)
 #pragma unroll
-        for (int b = 0; b < TN; ++b) {
-            const int gi = tm * GA + wgm + a, gj = tn * GB + wgn + b;
-            if (gi >= P.A.groups || gj >= P.B.groups) continue;
-            const int i0 = gi * kGroup, j = gj * kGroup + l;
-            float v[16];
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                float e4[4] = {0.f, 0.f, 0.f, 0.f};
-                if (P.E.data) {
-                    const char *p = P.E.data + ((int64_t)gj * P.E.steps + 2 * gi + (q >> 1)) * (P.E.parts * kBlock) +
-                                    (l + 32 * (q & 1)) * 16 + 8 * h;
-                    const halfx4 hi = *reinterpret_cast<const halfx4 *>(p);
-                    halfx4 lo = {};
-                    if (P.E.parts == 2) lo = *reinterpret_cast<const halfx4 *>(p + kBlock);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) e4[e] = (float)hi[e] + (float)lo[e];
-                }
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int i = i0 + 8 * q + 4 * h + e;
-                    float x = dev * fmaf(P.al, acc[a][b][4 * q + e], P.be * e4[e]);
-                    if (i == j && i < P.rows) x += P.ga;
-                    v[4 * q + e] = x;
-                }
-            }
-            if (P.O) {
-                O *out = static_cast<O *>(P.O);
-                if (j < P.cols)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int i = i0 + 8 * (r >> 2) + 4 * h + (r & 3);
-                        if (i < P.rows) out[P.flip ? j * P.ldo + i : i * P.ldo + j] = (O)v[r];
-                    }
-                continue;
-            }
-            {
-                const packed_half &o = P.out_n;
-                char *d = o.data + ((int64_t)gj * o.steps + 2 * gi) * (o.parts * kBlock) + l * 16 + 8 * h;
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const float x[4] = {v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
-                    const parts_of<4> p(x);
-                    char *to = d + (q >> 1) * (o.parts * kBlock) + (q & 1) * 512;
-                    *reinterpret_cast<halfx4 *>(to) = p.hi;
-                    if (o.parts == 2) *reinterpret_cast<halfx4 *>(to + kBlock) = p.lo;
-                }
-            }
-            if (both) {
-                const packed_half &o = P.out_t;
-#pragma unroll
-                for (int r = 0; r < 16; ++r) buf[(8 * (r >> 2) + 4 * h + (r & 3)) * 33 + l] = v[r];
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                char *d = o.data + ((int64_t)gi * o.steps + 2 * gj) * (o.parts * kBlock) + lane * 16;
-#pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    float x[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] = buf[l * 33 + 16 * s + 8 * h + e];
-                    const parts_of<8> p(x);
-                    *reinterpret_cast<halfx8 *>(d + s * (o.parts * kBlock)) = p.hi;
-                    if (o.parts == 2) *reinterpret_cast<halfx8 *>(d + s * (o.parts * kBlock) + kBlock) = p.lo;
-                }
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            }
-        }
+        for (int b = 0; b < TN; ++b) finish_block<O>(P, tm * GA + wgm + a, tn * GB + wgn + b, lane, acc[a][b], buf);
 }
 
-// Large products: 128 x 128 tiles.  Products of few tiles: 64 x 64, two waves a
-// position, four steps between two barriers.
+// The blocks of the tiles that were cut: a wave adds the ranges of a 32 x 32 block and finishes it.
+template <typename S, typename O>
+__global__ __launch_bounds__(256) void join_kernel(product_args P) {
+    constexpr int blocks = S::GA * S::GB;
+    __shared__ float turned[4][kTurned];
+    const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int id = blockIdx.x * 4 + wave;
+    static_assert(blocks % 4 == 0, "whole workgroups");
+    const int t = P.whole + id / blocks, n = id % blocks;
+    int tm, tn;
+    place_of<S>(t, P.symmetric, P.tiles_m, P.tiles_n, tm, tn);
+    // block n of a tile in the order of the partial sums: position, then (a, b)
+    constexpr int each = S::TM * S::TN;
+    const int wp = n / each, ab = n % each;
+    const int gi = tm * S::GA + wp / S::WN * S::TM + ab / S::TN, gj = tn * S::GB + wp % S::WN * S::TN + ab % S::TN;
+    const float *p = P.partial + ((int64_t)(t - P.whole) * blocks + n) * (16 * kWave) + lane;
+    const int64_t stride = (int64_t)(P.tiles - P.whole) * blocks * (16 * kWave);
+    floatx16 sum = {};
+    for (int w = 0; w < P.ranges; w += 2) {
+        floatx16 x, y;
+        const int64_t second = w + 1 < P.ranges ? stride : 0;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) x[r] = p[r * kWave];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) y[r] = p[second + r * kWave];
+        sum += x;
+        if (second) sum += y;
+        p += 2 * stride;
+    }
+    finish_block<O>(P, gi, gj, lane, sum, turned[wave]);
+}
+
+// Large products: 128 x 128 tiles.  Products of fewer tiles: 128 x 64, or 64 x 64 with two waves a
+// position and four steps between two barriers.
 template <int NP>
 using large_tile = tile_shape<2, 2, 2, 2, 1, NP == 2 ? 1 : 2>;
+template <int NP>
+using medium_tile = tile_shape<2, 1, 2, 2, 1, NP == 2 ? 2 : 4>;
 using small_tile = tile_shape<1, 1, 2, 2, 2, 4>;
 
 template <typename S>
-int64_t tile_count(const product_args &P, int *tm, int *tn) {
-    *tm = (int)ceil_div(P.A.groups, S::GA);
-    *tn = (int)ceil_div(P.B.groups, S::GB);
-    return P.symmetric ? (int64_t)*tn * (*tn + 1) / 2 : (int64_t)*tm * *tn;
+void count_tiles(product_args &P) {
+    P.tiles_m = (int)ceil_div(P.A.groups, S::GA);
+    P.tiles_n = (int)ceil_div(P.B.groups, S::GB);
+    P.tiles = P.tiles_m * P.tiles_n;
+    if (!P.symmetric) return;
+    P.tiles = 0;
+    for (int first = 0; first < P.tiles_n; first += 8) P.tiles += band_tiles<S>(first, P.tiles_m, P.tiles_n);
 }
 
-constexpr int kRangeTiles = 512;  // most (tile, range) pairs of a product cut into ranges
-constexpr size_t kPartialBytes = (size_t)kRangeTiles * 64 * 64 * sizeof(float);
+constexpr int kCus = 256;
+// (also twice the partial sums of a small matrix's A)
+constexpr size_t kPartialBytes = (size_t)16 << 20;
+static_assert(kPartialBytes >= (size_t)kCus * 128 * 128 * sizeof(float) &&
+                  kPartialBytes / 2 >= (size_t)kMostRanges * tiles_of(4) * 1024 * sizeof(float), "partial sums");
 
-template <int NP, typename O>
-hipError_t launch_product(product_args P, hipStream_t s) {
-    int tm, tn;
-    int64_t T = tile_count<large_tile<NP>>(P, &tm, &tn);
-    if (T >= 256) {
-        P.tiles_m = tm;
-        P.tiles_n = tn;
-        product_kernel<NP, large_tile<NP>, kWhole, O><<<(unsigned)(ceil_div(T, 8) * 8), large_tile<NP>::threads, 0, s>>>(P);
-        return hipGetLastError();
-    }
-    T = tile_count<small_tile>(P, &tm, &tn);
-    P.tiles_m = tm;
-    P.tiles_n = tn;
-    const unsigned grid = (unsigned)(ceil_div(T, 8) * 8);
-    const int stages = (int)ceil_div(P.A.steps, small_tile::KS);
-    int ranges = P.partial ? (int)(kRangeTiles / 2 / T) : 1;
-    if (ranges > stages / 4) ranges = stages / 4;
-    if (ranges < 2) {
-        product_kernel<NP, small_tile, kWhole, O><<<grid, small_tile::threads, 0, s>>>(P);
-        return hipGetLastError();
-    }
-    if constexpr (sizeof(O) == sizeof(float)) {
+// The tiles past the last whole round of the CUs are cut into up to `most` ranges that fill
+// one, where that saves `least` stages of a tile: the join costs a launch of 5 us.
+template <int NP, typename S, typename O>
+hipError_t launch_tiles(product_args P, int most, int least, hipStream_t s) {
+    count_tiles<S>(P);
+    const int stages = (int)ceil_div(P.A.steps, S::KS), rest = P.tiles % kCus;
+    const int ranges = rest > 0 ? std::min(std::min(kCus / rest, most), stages / 4) : 1;
+    P.whole = P.tiles;
+    if (ranges > 1 && stages - stages / ranges >= least) {
+        P.whole = P.tiles - rest;
         P.range_stages = (int)ceil_div(stages, ranges);
         P.ranges = (int)ceil_div(stages, P.range_stages);
-        product_kernel<NP, small_tile, kRange, float><<<dim3(grid, (unsigned)P.ranges), small_tile::threads, 0, s>>>(P);
-        hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-        product_kernel<NP, small_tile, kJoin, float><<<grid, small_tile::threads, 0, s>>>(P);
-        return hipGetLastError();
     }
-    return hipErrorInvalidValue;
+    const int cut = (P.tiles - P.whole) * P.ranges;
+    const unsigned grid = (unsigned)(ceil_div(P.whole, 8) * 8 + cut);
+    product_kernel<NP, S, O><<<grid, S::threads, 0, s>>>(P);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || cut == 0) return e;
+    join_kernel<S, O><<<(unsigned)((P.tiles - P.whole) * S::GA * S::GB / 4), 256, 0, s>>>(P);
+    return hipGetLastError();
+}
+
+// By the number of large tiles.  us for five steps, symmetric and other products both with small,
+// medium and large tiles, two parts: 700 x 700 166, 237, 352; 1001 x 1777 268, 347, 539; 1500 x 1500 515, 456, 616;
+// 2048 x 2048 968, 752, 823; 2500 x 2500 (symmetric ones medium, 210 large tiles, the others
+// large, 400) 1159, all large 1204; 3500 x 3500 3920, 3075, 2858.  One part: 1001 x 1777 173, 229, 314; 1500 x 1500
+// 250, 261, 334; 2048 x 2048 440, 387, 444; 4096 x 4096 2255, 2071, 1839.  Cut tiles: large 4096 x 4096 4254 -> 3781
+// (528 symmetric tiles: 16 past the second round), 3500 x 3500 2858 -> 2710.
+template <int NP, typename O>
+hipError_t launch_product(product_args P, hipStream_t s) {
+    count_tiles<large_tile<NP>>(P);
+    if (P.tiles >= kCus) return launch_tiles<NP, large_tile<NP>, O>(P, 4, 40, s);
+    if (P.tiles >= kCus / 4) return launch_tiles<NP, medium_tile<NP>, O>(P, 4, 100, s);
+    return launch_tiles<NP, small_tile, O>(P, 32, 24, s);
 }
 
 struct muon_ws {
@@ -574,6 +983,7 @@ struct muon_ws {
 // parts of X and the m x m operands; X^T always has two (the residual of one part)
 muon_ws carve(int N, int K, int np, void *ws) {
     const int m = N < K ? N : K, n = N < K ? K : N;
+    if (m <= kSmall) np = 2;
     muon_ws w{};
     char *p = static_cast<char *>(ws);
     auto take = [&](size_t b) {
@@ -603,13 +1013,61 @@ muon_ws carve(int N, int K, int np, void *ws) {
 
 float exp2i(int e) { return std::ldexp(1.f, e); }
 
+int norm_blocks(const muon_args &a) {
+    const int64_t chunks = (int64_t)a.N * ceil_div(a.K, 4);
+    return (int)(chunks < kNormBlocks * 256 ? ceil_div(chunks, 256) : kNormBlocks);
+}
+
+// Steps between two products with X: the m x m products that stand for them pay where X is
+// wider than square and they are not bound by their launches.  us, one step and three, two parts:
+// 300 x 784 127 and 131, 512 x 512 136 and 155, 600 x 2000 219 and 194, 1001 x 1777 271 and 261, 2048 x 2048
+// 867 and 987, 2048 x 4096 1230 and 1146, 4096 x 9216 7181 and 5366.
+int most_steps(int m, int n) { return m > 512 && 2 * (int64_t)n >= 3 * (int64_t)m ? kMaxGroup : 1; }
+
+template <typename T, int g>
+hipError_t run_small(const muon_args &a, const update_src &u, void *ws, hipStream_t s) {
+    const bool tall = a.N > a.K;
+    const int m = tall ? a.K : a.N, n = tall ? a.N : a.K;
+    muon_ws w = carve(a.N, a.K, 2, ws);
+    const int nb = norm_blocks(a), slices = (int)ceil_div(n, kSlice);
+    const int ranges = slices < kMostRanges ? slices : kMostRanges;
+    momentum_kernel<T><<<nb, 256, 0, s>>>(u, w.norm);
+    small_pack_kernel<T, g><<<ranges, kPackWaves<g> * kWave, 0, s>>>(u, tall, w.norm, nb, a.eps, w.Xt[0], m, n, w.scal, w.partial);
+    hipError_t e = hipGetLastError();
+    for (int k = 0; k < a.steps && e == hipSuccess; ++k) {
+        const float *scal = k == 0 ? w.scal : nullptr;
+        // (a launch reads the sums of one half and writes those of the other)
+        float *sums = w.partial + (k & 1) * (kPartialBytes / 8), *next = w.partial + (~k & 1) * (kPartialBytes / 8);
+        if (ranges > kSumRanges)
+            small_sum_kernel<<<tiles_of(g), 256, 0, s>>>(sums, ranges, tiles_of(g), scal, w.A);
+        const int given = ranges > kSumRanges ? 0 : ranges;
+        if (k + 1 < a.steps)
+            small_step_kernel<float, false, g><<<ranges, 2 * g * kWave, 0, s>>>(
+                sums, given, w.A, w.Xt[k & 1], m, n, scal, w.Xt[~k & 1], next, nullptr, 0, 0, 1.f);
+        else
+            small_step_kernel<T, true, g><<<slices, 2 * g * kWave, 0, s>>>(
+                sums, given, w.A, w.Xt[k & 1], m, n, scal, packed_half{}, nullptr, static_cast<T *>(a.O), a.ldo, tall,
+                a.scale * exp2i(-kScaleX));
+        e = hipGetLastError();
+    }
+    return e;
+}
+
+template <typename T>
+hipError_t run_small(const muon_args &a, const update_src &u, void *ws, hipStream_t s) {
+    const int m = std::min(a.N, a.K);
+    if (m <= 32) return run_small<T, 1>(a, u, ws, s);
+    if (m <= 64) return run_small<T, 2>(a, u, ws, s);
+    if (m <= 96) return run_small<T, 3>(a, u, ws, s);
+    return run_small<T, 4>(a, u, ws, s);
+}
+
 template <int NP, typename T>
 hipError_t run(const muon_args &a, const update_src &u, void *ws, hipStream_t s) {
     const bool tall = a.N > a.K;
     const int m = tall ? a.K : a.N, n = tall ? a.N : a.K;
     muon_ws w = carve(a.N, a.K, NP, ws);
-    const int64_t chunks = (int64_t)a.N * ceil_div(a.K, 4);
-    const int nb = (int)(chunks < kNormBlocks * 256 ? ceil_div(chunks, 256) : kNormBlocks);
+    const int nb = norm_blocks(a);
     momentum_kernel<T><<<nb, 256, 0, s>>>(u, w.norm);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
@@ -637,7 +1095,7 @@ hipError_t run(const muon_args &a, const update_src &u, void *ws, hipStream_t s)
     int left = a.steps, cur = 0;
     bool first = true;
     while (left > 0 && e == hipSuccess) {
-        const int g = NP == 1 ? 1 : (left < kMaxGroup ? left : kMaxGroup);
+        const int g = NP == 1 ? 1 : std::min(left, most_steps(m, n));
         left -= g;
         e = symmetric(w.X, kScaleX, w.X, kScaleX, w.A, kScaleX, 1.f, 0.f, 0.f, none, 0, first ? w.scal + 1 : nullptr);
         packed_half *Q = &w.P, *Q2 = &w.Q[1];
@@ -659,6 +1117,7 @@ hipError_t run(const muon_args &a, const update_src &u, void *ws, hipStream_t s)
         }
         if (e != hipSuccess) break;
         product_args P{};
+        P.partial = w.partial;
         P.A = *Q;
         P.B = w.Xt[cur];
         P.rows = m; P.cols = n;
@@ -689,6 +1148,7 @@ hipError_t run(const muon_args &a, const update_src &u, void *ws, hipStream_t s)
 template <typename T>
 hipError_t run_type(const muon_args &a, void *ws, hipStream_t s) {
     const update_src u{a.G, a.ldg, a.M, a.ldm, a.M_out, a.ldmo, a.mu, a.nesterov, a.N, a.K};
+    if (std::min(a.N, a.K) <= kSmall) return run_small<T>(a, u, ws, s);
     return a.parts == 1 ? run<1, T>(a, u, ws, s) : run<2, T>(a, u, ws, s);
 }
 
