@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes as C
 import functools
+import math
 import os
 from dataclasses import dataclass
 
@@ -307,14 +308,19 @@ def _mat(t, name):
     return rows, cols, ld if rows > 1 else max(cols, 1)
 
 
+_DTYPES: dict = {}  # torch dtype -> l1csr_dtype
+
+
 def _dtype_code(t, name):
     """l1csr_dtype of a GPU tensor."""
-    torch = _torch()
+    torch = _torch_module or _torch()
+    if not _DTYPES:
+        _DTYPES.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if not t.is_cuda:
         raise ValueError(f"{name} must live on the GPU (got {t.device})")
-    code = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}.get(t.dtype)
+    code = _DTYPES.get(t.dtype)
     if code is None:
         raise TypeError(f"{name} must be float32, bfloat16 or float16 (got {t.dtype})")
     return code
@@ -323,25 +329,41 @@ def _dtype_code(t, name):
 def _typed_mat(t, name):
     """A [rows][ld] matrix of one of the element types; returns (rows, cols, ld, l1csr_dtype)."""
     code = _dtype_code(t, name)
-    if t.dim() != 2:
+    shape = t.shape
+    if len(shape) != 2:
         raise ValueError(f"{name} must be 2-D")
-    rows, cols = t.shape
+    rows, cols = shape
     ld, unit = t.stride()
     if (unit != 1 and cols > 1) or (rows > 1 and ld < cols):
         raise ValueError(f"{name} must have a contiguous last dimension and rows that do not overlap")
     return rows, cols, ld if rows > 1 else max(cols, 1), code
 
 
-def _on_one_device(first, *others):
-    """Every tensor given (None: left out) lies on the first one's device, which has to be the current one:
-    a call launches on the current device's stream."""
-    index = first.device.index
-    for t in others:
-        if t is not None and t.device.index != index:
-            raise ValueError(f"tensors on different devices: {first.device} and {t.device}")
-    if index != _torch().cuda.current_device():
+def _device_of(first):
+    """The device index of a call's first tensor, which has to be the current one: a call launches on the
+    current device's stream."""
+    index = first.get_device()
+    if index != _torch_module.cuda.current_device():
         raise ValueError(f"the tensors live on {first.device}: make it the current device "
                          "(torch.cuda.device) for the call")
+    return index
+
+
+def _same_device(index, t, name):
+    if t.get_device() != index:
+        raise ValueError(f"{name} lives on {t.device}, another tensor on device {index}")
+    return t
+
+
+def _vec_of(t, dtype, n, index, name, what):
+    """A contiguous vector of n values on device `index`."""
+    if isinstance(t, _torch_module.Tensor) and t.dtype is dtype and t.shape == (n,) and t.get_device() == index and \
+            t.is_contiguous():
+        return t
+    _vec(t, dtype, name)
+    if t.numel() != n:
+        raise ValueError(f"{name} must hold one value per {what}")
+    return _same_device(index, t, name)
 
 
 def _own_workspace(nbytes, device, stream):
@@ -1182,38 +1204,33 @@ def softmax_xent(logits, labels, dlogits=None, loss=None, stream=None):
 
 
 def _token_args(logits, labels, weights, dlogits, grad, stream):
-    """What the calls over logits[C][B] check alike; returns (C, B, dtype, ld, dlogits, its ld)."""
-    torch = _torch()
+    """What the calls over logits[C][B] check alike; returns (C, B, dtype, ld, dlogits, its ld, device index)."""
     Cn, B, ld, code = _typed_mat(logits, "logits")
-    _vec(labels, torch.int32, "labels")
-    if labels.numel() != B:
-        raise ValueError("labels must hold one class per token (B)")
+    torch = _torch_module
+    index = _device_of(logits)
+    _vec_of(labels, torch.int32, B, index, "labels", "token (B)")
     if weights is not None:
-        _vec(weights, torch.float32, "weights")
-        if weights.numel() != B:
-            raise ValueError("weights must hold one value per token (B)")
+        _vec_of(weights, torch.float32, B, index, "weights", "token (B)")
     ldd = 0
-    if dlogits is not None and not grad:
-        raise ValueError("dlogits given to a call without gradient")
     if grad:
         if dlogits is None:
             dlogits = _new((Cn, B), logits.dtype, logits.device, stream)
         rows, cols, ldd, dcode = _typed_mat(dlogits, "dlogits")
-        if (rows, cols) != (Cn, B) or dcode != code:
+        if rows != Cn or cols != B or dcode != code:
             raise ValueError("dlogits must have the shape and type of logits")
+        _same_device(index, dlogits, "dlogits")
         if rows == 1 and dlogits.data_ptr() == logits.data_ptr():
             ldd = ld
-    _on_one_device(logits, labels, weights, dlogits)
-    return Cn, B, code, ld, dlogits, ldd
+    elif dlogits is not None:
+        raise ValueError("dlogits given to a call without gradient")
+    return Cn, B, code, ld, dlogits, ldd, index
 
 
-def _per(t, n, name, what):
+def _result(t, n, logits, index, name, what, stream):
+    """A call's float32 output of n values: the caller's, or a new one."""
     if t is None:
-        return None
-    _vec(t, _torch().float32, name)
-    if t.numel() != n:
-        raise ValueError(f"{name} must hold one value per {what}")
-    return t
+        return _new((n,), _torch_module.float32, logits.device, stream)
+    return _vec_of(t, _torch_module.float32, n, index, name, what)
 
 
 def token_logp(logits, labels, logp=None, stream=None):
@@ -1221,15 +1238,11 @@ def token_logp(logits, labels, logp=None, stream=None):
 
     logits [C][B] float32, bfloat16 or float16 (class-major, tokens contiguous, as softmax_xent's), labels [B] int32;
     a label outside [0, C) gives 0.  Returns logp (float32 [B])."""
-    torch = _torch()
-    Cn, B, code, ld, _, _ = _token_args(logits, labels, None, None, False, stream)
-    if logp is None:
-        logp = _new((B,), torch.float32, logits.device, stream)
-    _per(logp, B, "logp", "token")
-    _on_one_device(logits, logp)
+    Cn, B, code, ld, _, _, index = _token_args(logits, labels, None, None, False, stream)
+    logp = _result(logp, B, logits, index, "logp", "token (B)", stream)
     ws, wsb = _own_workspace(workspace_bytes(OP_TOKEN_LOSS, Cn, 0, 0, B), logits.device, stream)
-    _check(lib().l1csr_token_logp(Cn, B, code, _p(logits), ld, _p(labels), _p(logp), _p(ws), wsb, _stream(stream)),
-           "l1csr_token_logp")
+    _check(lib().l1csr_token_logp(Cn, B, code, logits.data_ptr(), ld, labels.data_ptr(), logp.data_ptr(), _p(ws), wsb,
+                                  _stream(stream)), "l1csr_token_logp")
     return logp
 
 
@@ -1243,23 +1256,19 @@ def policy_loss(logits, labels, old_logp, advantages, ref_logp=None, weights=Non
     weight (weights float32 [B], default 1) is not 0; the logits of the others are not used and their columns of
     dlogits are 0.  dlogits (the type and shape of logits) may be logits itself; grad=False leaves it out.
     Returns (stats, dlogits, logp): stats[4] = loss, mean policy term, mean k, share of clipped tokens."""
-    torch = _torch()
-    Cn, B, code, ld, dlogits, ldd = _token_args(logits, labels, weights, dlogits, grad, stream)
-    for t_, name in ((old_logp, "old_logp"), (advantages, "advantages")):
-        _vec(t_, torch.float32, name)
-        _per(t_, B, name, "token")
-    _per(ref_logp, B, "ref_logp", "token")
-    if logp is None:
-        logp = _new((B,), torch.float32, logits.device, stream)
-    if stats is None:
-        stats = _new((4,), torch.float32, logits.device, stream)
-    _per(logp, B, "logp", "token")
-    _per(stats, 4, "stats", "statistic (4)")
-    _on_one_device(logits, old_logp, advantages, ref_logp, logp, stats)
+    Cn, B, code, ld, dlogits, ldd, index = _token_args(logits, labels, weights, dlogits, grad, stream)
+    f32 = _torch_module.float32
+    _vec_of(old_logp, f32, B, index, "old_logp", "token (B)")
+    _vec_of(advantages, f32, B, index, "advantages", "token (B)")
+    if ref_logp is not None:
+        _vec_of(ref_logp, f32, B, index, "ref_logp", "token (B)")
+    logp = _result(logp, B, logits, index, "logp", "token (B)", stream)
+    stats = _result(stats, 4, logits, index, "stats", "statistic (4)", stream)
     ws, wsb = _own_workspace(workspace_bytes(OP_TOKEN_LOSS, Cn, 0, 0, B), logits.device, stream)
-    _check(lib().l1csr_policy_loss(Cn, B, code, _p(logits), ld, _p(labels), _p(old_logp), _p(advantages), _p(ref_logp),
-                                   _p(weights), float(clip_low), float(clip_high), float(kl_coef), _p(dlogits), ldd,
-                                   _p(logp), _p(stats), _p(ws), wsb, _stream(stream)), "l1csr_policy_loss")
+    _check(lib().l1csr_policy_loss(Cn, B, code, logits.data_ptr(), ld, labels.data_ptr(), old_logp.data_ptr(),
+                                   advantages.data_ptr(), _p(ref_logp), _p(weights), clip_low, clip_high, kl_coef,
+                                   _p(dlogits), ldd, logp.data_ptr(), stats.data_ptr(), _p(ws), wsb, _stream(stream)),
+           "l1csr_policy_loss")
     return stats, dlogits, logp
 
 
@@ -1272,24 +1281,22 @@ def preference_loss(logits, labels, seq_ptr, ref_logp=None, weights=None, beta=0
     default 0), D = rewards[2p] - rewards[2p + 1], loss = the mean over the pairs of
     -(1 - ls) log sigmoid(D) - ls log sigmoid(-D) with ls = label_smoothing.  Tokens that do not count and dlogits as in
     policy_loss; columns in no sequence get 0.  Returns (loss[1], dlogits, rewards)."""
-    torch = _torch()
-    Cn, B, code, ld, dlogits, ldd = _token_args(logits, labels, weights, dlogits, grad, stream)
+    Cn, B, code, ld, dlogits, ldd, index = _token_args(logits, labels, weights, dlogits, grad, stream)
+    torch = _torch_module
     _vec(seq_ptr, torch.int32, "seq_ptr")
-    if seq_ptr.numel() % 2 == 0:
-        raise ValueError("seq_ptr must hold 2 * pairs + 1 offsets")
     pairs = seq_ptr.numel() // 2
-    _per(ref_logp, 2 * pairs, "ref_logp", "sequence")
-    if rewards is None:
-        rewards = _new((2 * pairs,), torch.float32, logits.device, stream)
-    if loss is None:
-        loss = _new((1,), torch.float32, logits.device, stream)
-    _per(rewards, 2 * pairs, "rewards", "sequence")
-    _per(loss, 1, "loss", "call (1)")
-    _on_one_device(logits, seq_ptr, ref_logp, rewards, loss)
+    if seq_ptr.numel() != 2 * pairs + 1:
+        raise ValueError("seq_ptr must hold 2 * pairs + 1 offsets")
+    _same_device(index, seq_ptr, "seq_ptr")
+    if ref_logp is not None:
+        _vec_of(ref_logp, torch.float32, 2 * pairs, index, "ref_logp", "sequence (2 * pairs)")
+    rewards = _result(rewards, 2 * pairs, logits, index, "rewards", "sequence (2 * pairs)", stream)
+    loss = _result(loss, 1, logits, index, "loss", "call (1)", stream)
     ws, wsb = _own_workspace(workspace_bytes(OP_TOKEN_LOSS, Cn, pairs, 0, B), logits.device, stream)
-    _check(lib().l1csr_preference_loss(Cn, B, code, _p(logits), ld, _p(labels), pairs, _p(seq_ptr), _p(ref_logp),
-                                       _p(weights), float(beta), float(label_smoothing), _p(dlogits), ldd, _p(rewards),
-                                       _p(loss), _p(ws), wsb, _stream(stream)), "l1csr_preference_loss")
+    _check(lib().l1csr_preference_loss(Cn, B, code, logits.data_ptr(), ld, labels.data_ptr(), pairs, seq_ptr.data_ptr(),
+                                       _p(ref_logp), _p(weights), beta, label_smoothing, _p(dlogits), ldd,
+                                       rewards.data_ptr(), loss.data_ptr(), _p(ws), wsb, _stream(stream)),
+           "l1csr_preference_loss")
     return loss, dlogits, rewards
 
 
@@ -1310,30 +1317,35 @@ class MuonState:
         return MuonState(torch.zeros(shape, dtype=torch.float32, device=device), **kw)
 
 
-def _muon_update(G, O, m, m_out, mu, nesterov, steps, eps, scale, precision, stream):
+def _muon_update(G, O, m, m_out, st, scale, precision, stream):
+    """muon_update of G [N][K] into O; m None: no momentum."""
     N, K, ldg, code = _typed_mat(G, "G")
-    ro, co, ldo, ocode = _typed_mat(O, "out")
-    if (ro, co) != (N, K) or ocode != code:
-        raise ValueError("the update must have the shape and type of G")
-    if N == 1 and O.data_ptr() == G.data_ptr():
+    index = _device_of(G)
+    if O is G:
         ldo = ldg
+    else:
+        ro, co, ldo, ocode = _typed_mat(O, "the update")
+        if ro != N or co != K or ocode != code:
+            raise ValueError("the update must have the shape and type of G")
+        _same_device(index, O, "the update")
+        if N == 1 and O.data_ptr() == G.data_ptr():
+            ldo = ldg
     ldm = ldmo = 0
-    for t_, name in ((m, "m"), (m_out, "m_out")):
-        if t_ is not None:
-            rows, cols, ld = _mat(t_, name)
-            if (rows, cols) != (N, K):
-                raise ValueError(f"{name} must be [n_rows][n_cols]")
-            if name == "m":
-                ldm = ld
-            else:
-                ldmo = ld
-    if precision not in (F32, F16):
+    if m is not None:
+        rows, cols, ldm = _mat(_same_device(index, m, "m"), "m")
+        if rows != N or cols != K:
+            raise ValueError("m must be [n_rows][n_cols]")
+        ldmo = ldm
+        if m_out is not m:
+            rows, cols, ldmo = _mat(_same_device(index, m_out, "m_out"), "m_out")
+            if rows != N or cols != K:
+                raise ValueError("m_out must be [n_rows][n_cols]")
+    if precision != F32 and precision != F16:
         raise ValueError("precision must be F32 or F16")
-    _on_one_device(G, O, m, m_out)
     ws, wsb = _own_workspace(workspace_bytes(OP_MUON if precision == F32 else OP_MUON_F16, N, K, 0, 0), G.device, stream)
-    _check(lib().muon_update(N, K, code, _p(G), ldg, _p(m), ldm, _p(m_out), ldmo, float(mu), int(bool(nesterov)),
-                             int(steps), float(eps), float(scale), int(precision), _p(O), ldo, _p(ws), wsb,
-                             _stream(stream)), "muon_update")
+    _check(lib().muon_update(N, K, code, G.data_ptr(), ldg, _p(m), ldm, _p(m_out), ldmo, st.mu, 1 if st.nesterov else 0,
+                             st.steps, st.eps, scale, precision, O.data_ptr(), ldo, _p(ws), wsb, _stream(stream)),
+           "muon_update")
     return O
 
 
@@ -1348,16 +1360,23 @@ def orthogonalize(G, out=None, steps=5, eps=1e-7, scale=1.0, precision=None, str
     if out is None:
         N, K, _, _ = _typed_mat(G, "G")
         out = _new((N, K), G.dtype, G.device, stream)
-    return _muon_update(G, out, None, None, 0.0, False, steps, eps, scale, precision, stream)
+    return _muon_update(G, out, None, None, MuonState(None, 0.0, False, steps, eps), scale, precision, stream)
 
 
-def _muon_args(W, G, st, m_out):
+def _muon_args(W, G, st):
+    """What the Prox-Muon calls check of the layer and its gradient; returns (N, K, scale)."""
     N, K, _ = _mat(G, "G")
-    if (N, K) != (W.n_rows, W.n_cols):
+    if N != W.n_rows or K != W.n_cols:
         raise ValueError("G must be [n_rows][n_cols]")
-    _mat(st.m, "m")
-    scale = max(1.0, N / K) ** 0.5 if st.scale is None and N and K else st.scale or 0.0
-    return N, K, scale, st.m if m_out is None else m_out
+    if st.m is None:
+        raise ValueError("Prox-Muon needs the momentum m")
+    index = G.get_device()
+    for t_, name in ((W.row_ptr, "row_ptr"), (W.col_idx, "col_idx"), (W.vals, "vals")):
+        _same_device(index, t_, name)
+    scale = st.scale
+    if scale is None:
+        scale = math.sqrt(N / K) if N > K > 0 else 1.0
+    return N, K, scale
 
 
 def prox_muon_step(W: CSR, G, st: MuonState, eta, lam, Z=None, m_out=None, row_counts=None, precision=F32,
@@ -1365,13 +1384,11 @@ def prox_muon_step(W: CSR, G, st: MuonState, eta, lam, Z=None, m_out=None, row_c
     """One Prox-Muon step of the l1 phase over all N*K weights: m' = mu m + G, O = scale * NS(G + mu m') (muon_update;
     without nesterov NS(m')), Z = S_{eta*lam}(W - eta O).  Z may be G itself; st.m is updated in place, or m_out receives
     m' and st.m is kept.  Returns Z."""
-    torch = _torch()
-    N, K, scale, m_new = _muon_args(W, G, st, m_out)
-    _on_one_device(G, W.row_ptr, W.col_idx, W.vals, row_counts)
+    N, K, scale = _muon_args(W, G, st)
     W.validate_shapes()
     if Z is None:
-        Z = _new((N, K), torch.float32, G.device, stream)
-    _muon_update(G, Z, st.m, m_new, st.mu, st.nesterov, st.steps, st.eps, scale, precision, stream)
+        Z = _new((N, K), _torch().float32, G.device, stream)
+    _muon_update(G, Z, st.m, st.m if m_out is None else m_out, st, scale, precision, stream)
     return prox_l1_step(PROX_DENSE, W, Z, eta, lam, Z=Z, row_counts=row_counts, stream=stream)
 
 
@@ -1381,16 +1398,14 @@ def prox_muon_recompress(W: CSR, G, st: MuonState, eta, lam, O=None, capacity=No
     threshold (prox_l1_recompress).  O (float32 [N][K], may be G itself) receives the update; st.m is updated in
     place, but not by a call that fails for its capacity."""
     torch = _torch()
-    N, K, scale, m_new = _muon_args(W, G, st, None)
-    _on_one_device(G, W.row_ptr, W.col_idx, W.vals)
+    N, K, scale = _muon_args(W, G, st)
     W.validate_shapes()
     cap = capacity if capacity is not None else (N * K if out is None else min(out.col_idx.numel(), out.vals.numel()))
-    short = cap < N * K
-    if short:
-        m_new = _new((N, K), torch.float32, G.device, stream)
+    short = cap < N * K  # the count may not fit: the momentum is stored behind the recompression
+    m_new = _new((N, K), torch.float32, G.device, stream) if short else st.m
     if O is None:
         O = _new((N, K), torch.float32, G.device, stream)
-    _muon_update(G, O, st.m, m_new, st.mu, st.nesterov, st.steps, st.eps, scale, precision, stream)
+    _muon_update(G, O, st.m, m_new, st, scale, precision, stream)
     out = prox_l1_recompress(W, O, eta, lam, capacity=capacity, out=out, stream=stream)
     if short:
         with torch.cuda.stream(torch.cuda.current_stream(G.device) if stream is None else stream):
