@@ -27,16 +27,14 @@ constexpr int kThreads = 256;
 constexpr int kTokenBlocks = 1024;  // most workgroups (and partial sums) of the token pass
 constexpr int kJoin = 8;            // partial sums that a lane of it has in flight
 constexpr float kLog2e = 1.44269504088896340736f;
-constexpr double kLn2 = 1 / (double)kLog2e;  // of the rounded factor
 
 __device__ __forceinline__ float to_f32(float x) { return x; }
 __device__ __forceinline__ float to_f32(_Float16 x) { return (float)x; }
 __device__ __forceinline__ float to_f32(__bf16 x) { return (float)x; }
 
-// 2^x for x <= 0 (or NaN); results under 2^-126 are zero.  The columns' statistics are those of
-// z log2 e: 2^(fma(z, log2 e, -m)) is one rounding and m, the rounded largest
-// z log2 e, cancels from the probabilities.
-__device__ __forceinline__ float exp2_neg(float x) { return __builtin_amdgcn_exp2f(x); }
+// exp(x) for x <= 0 (or NaN); results under 2^-126 are zero.  (The difference z - m is taken first: z log2 e
+// overflows for masks of the type's lowest value.)
+__device__ __forceinline__ float exp_neg(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 
 // V values at any alignment of T: the hardware takes unaligned 16-byte accesses
 template <typename T, int V>
@@ -137,11 +135,11 @@ __global__ __launch_bounds__(kThreads) void column_sums_kernel(int C, int B, con
                 y[u] = u < n ? to_f32(x[u][v]) : -INFINITY;
                 top = fmaxf(top, y[u]);
             }
-            top = fmaxf(top * kLog2e, m[v]);
+            top = fmaxf(top, m[v]);
             const float base = top == -INFINITY ? 0.f : top;  // only excluded classes so far
-            float sum = s[v] * exp2_neg(m[v] - base);
+            float sum = s[v] * exp_neg(m[v] - base);
 #pragma unroll
-            for (int u = 0; u < U; ++u) sum += exp2_neg(fmaf(y[u], kLog2e, -base));
+            for (int u = 0; u < U; ++u) sum += exp_neg(y[u] - base);
             m[v] = top;
             s[v] = sum;
         }
@@ -179,14 +177,14 @@ __global__ __launch_bounds__(kThreads) void column_sums_kernel(int C, int B, con
         float top = -INFINITY, sum = 0.f;
         for (int t = 0; t < TY; ++t) top = fmaxf(top, sm[t * TX * V + col]);
         const float base = top == -INFINITY ? 0.f : top;
-        for (int t = 0; t < TY; ++t) sum += ss[t * TX * V + col] * exp2_neg(sm[t * TX * V + col] - base);
+        for (int t = 0; t < TY; ++t) sum += ss[t * TX * V + col] * exp_neg(sm[t * TX * V + col] - base);
         part[(int64_t)(first + col) * g.splits + blockIdx.y] = make_float2(top, sum);
     }
 }
 
 // What the token pass leaves for the others
 struct token_out {
-    float *m, *inv;   // the column's largest z log2 e and 1 / (sum of exponentials)
+    float *m, *inv;   // the column's maximum and 1 / (sum of exponentials)
     float *coef;      // d loss / d lp (policy: times the sum of weights)
     float *lp;        // log-probability; 0 where the token does not count
     double *sums;     // [4][kTokenBlocks] weights, and weighted loss, kl, clipped
@@ -233,19 +231,17 @@ __global__ __launch_bounds__(kThreads) void token_kernel(int C, int B, const T *
 #pragma unroll
                 for (int u = 0; u < kJoin; ++u) t = fmaxf(t, p[u].x);  // (past the end the last again)
                 const float base = t == -INFINITY ? 0.f : t;
-                s *= exp2_neg(top - base);
+                s *= exp_neg(top - base);
 #pragma unroll
-                for (int u = 0; u < kJoin; ++u) s += i0 + u * L < splits ? p[u].y * exp2_neg(p[u].x - base) : 0.f;
+                for (int u = 0; u < kJoin; ++u) s += i0 + u * L < splits ? p[u].y * exp_neg(p[u].x - base) : 0.f;
                 top = t;
             }
         const float mine = top;
         for (int d = L / 2; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, kWave));
-        s *= exp2_neg(mine - (top == -INFINITY ? 0.f : top));
+        s *= exp_neg(mine - (top == -INFINITY ? 0.f : top));
         for (int d = L / 2; d >= 1; d >>= 1) s += __shfl_xor(s, d, kWave);
         if (lane != 0 || b >= B) continue;
-        float lp = 0.f;  // (z log2 e - m) ln 2 - log s, its first term in double: m is not small against it
-        if (on)
-            lp = (float)(((double)to_f32(z[(int64_t)labels[b] * ld + b]) * kLog2e - (double)top) * kLn2) - logf(s);
+        const float lp = on ? (to_f32(z[(int64_t)labels[b] * ld + b]) - top) - logf(s) : 0.f;
         if (o.lp) o.lp[b] = lp;
         if constexpr (KIND == kLogp) continue;
         o.m[b] = top;
@@ -361,7 +357,7 @@ __global__ __launch_bounds__(kThreads) void gradient_kernel(int C, int B, const 
     const int tx = threadIdx.x & (TX - 1), ty = threadIdx.x >> g.tx_shift;
     const columns<V> k(tx, g.tx_shift, B);
     if (!k.any) return;
-    float m[V], f[V];  // dz = f 2^(z log2 e - m)
+    float m[V], f[V];  // dz = f exp(z - m)
     constexpr int words = sizeof(T) * V / 4;
     unsigned keep[words > 0 ? words : 1];  // the bits of the columns that count: the others' may hold anything
     T ones[V];
@@ -394,7 +390,7 @@ __global__ __launch_bounds__(kThreads) void gradient_kernel(int C, int B, const 
             if (u >= n) continue;
             T y[V] = {};
             if (work) {
-                auto value = [&](float x, int v) { return f[v] * exp2_neg(fmaf(x, kLog2e, -m[v])); };
+                auto value = [&](float x, int v) { return f[v] * exp_neg(x - m[v]); };
                 if constexpr (words > 0) {
                     unsigned b[words];
                     __builtin_memcpy(b, x[u], sizeof(b));

@@ -1,0 +1,351 @@
+"""Token log-probabilities, the clipped policy loss and the preference loss on the GPU against the formulas in 64 bits.
+
+Tolerances.  A column's sum of exponentials has C positive terms, each within (|t| + 4) 2^-24 of its value (one rounding of
+the exponent t = (z - max) log2 e, one of the exponential, one of a rescaling), and is added in some order with at most
+C - 1 roundings and as many rescalings: its relative error is below (2 C + 16) 2^-24 =: ES, the terms with a large |t| being
+too small to count.  lp adds roundings of itself and of the logarithm: |lp error| <= ES + 2^-22 (1 + |lp|) =: EL.  A
+probability is within ES + (|log p| + 4) 2^-22 =: EP of its value, a coefficient within 4 (EL + 2^-22) of its scale (the
+ratio's or the reference's exponential, a few products), and dz rounds once to its type.
+"""
+import math
+
+import numpy as np
+import pytest
+
+import paper_1905_07931_amd as L1
+
+from _helpers import cuda, h
+
+pytestmark = pytest.mark.gpu
+
+HALF_STEP = {"float32": 2.0 ** -24, "bfloat16": 2.0 ** -8, "float16": 2.0 ** -11}
+TINY = {"float32": 2.0 ** -126, "bfloat16": 2.0 ** -126, "float16": 2.0 ** -24}  # a result below rounds by an absolute step
+TYPES = ["float32", "bfloat16", "float16"]
+
+
+def _torch():
+    import torch
+    return torch
+
+
+def es(C):
+    return (2 * C + 16) * 2.0 ** -24
+
+
+def el(C, lp):
+    return es(C) + 2.0 ** -22 * (1 + np.abs(lp))
+
+
+def logits(C, B, dtype, seed, pad=0, off=0):
+    """A [C][B] view with a leading dimension of B + pad, starting `off` elements into its buffer."""
+    torch = _torch()
+    rng = np.random.default_rng(seed)
+    z = rng.standard_normal((C, B)) * 2
+    labels = rng.integers(0, C, B)
+    z[labels, np.arange(B)] += rng.uniform(0, 2 + math.log(C), B)
+    buf = torch.full((C * (B + pad) + off,), float("nan"), dtype=getattr(torch, dtype), device=cuda())
+    v = buf[off:].view(C, B + pad)[:, :B]
+    v.copy_(torch.from_numpy(z).to(getattr(torch, dtype)))
+    return v, torch.from_numpy(labels.astype(np.int32)).to(cuda()), v.cpu().double().numpy(), labels
+
+
+def vec(a):
+    return _torch().from_numpy(np.ascontiguousarray(a, dtype=np.float32)).to(cuda())
+
+
+def ref_logp(z, labels, counts):
+    """(lp, softmax) in 64 bits; the columns that do not count are 0."""
+    lp, p = np.zeros(z.shape[1]), np.zeros(z.shape)
+    for b in np.nonzero(counts)[0]:
+        m = z[:, b].max()
+        e = np.exp(z[:, b] - m)
+        lp[b] = z[labels[b], b] - m - math.log(e.sum())
+        p[:, b] = e / e.sum()
+    return lp, p
+
+
+def ref_policy(lp, counts, w, old, adv, ref, lo, hi, beta):
+    w = np.where(counts, w, 0.0)
+    sw = w.sum()
+    pg, kl, off, d = (np.zeros_like(lp) for _ in range(4))
+    for b in np.nonzero(counts)[0]:
+        r = math.exp(lp[b] - old[b])
+        off[b] = (adv[b] > 0 and r > 1 + hi) or (adv[b] < 0 and r < 1 - lo)
+        pg[b] = -min(r * adv[b], min(max(r, 1 - lo), 1 + hi) * adv[b])
+        d[b] = 0.0 if off[b] else -adv[b] * r
+        if ref is not None:
+            q = ref[b] - lp[b]
+            kl[b] = math.expm1(q) - q
+            d[b] -= beta * math.expm1(q)
+    share = w / sw if sw else w
+    stats = [(share * x).sum() for x in (pg + beta * kl, pg, kl, off)]
+    return stats, share * d
+
+
+def ref_dz(p, labels, coef):
+    dz = -p * coef
+    dz[labels.clip(0, p.shape[0] - 1), np.arange(p.shape[1])] += coef
+    return np.where(coef == 0, 0.0, dz)
+
+
+def check_dz(got, p, labels, coef, scale, C, lp, dtype):
+    """scale: the coefficients' scale that their error is relative to."""
+    want = ref_dz(p, labels, coef)
+    got = got.detach().cpu().double().numpy()
+    with np.errstate(divide="ignore"):
+        ep = es(C) + (np.abs(np.log(np.maximum(p, 1e-300))) + 4) * 2.0 ** -22
+    own = np.zeros_like(p)
+    own[labels.clip(0, C - 1), np.arange(p.shape[1])] = 1.0
+    size = np.abs(own - p)
+    tol = size * scale * 4 * (el(C, lp) + 2.0 ** -22) + np.abs(coef) * (p * ep + own * el(C, lp))
+    tol = tol + np.abs(want) * HALF_STEP[dtype] * 1.001 + TINY[dtype]
+    bad = np.abs(got - want) > tol
+    assert not bad.any(), (int(bad.sum()), np.argwhere(bad)[0], got[bad][0], want[bad][0], tol[bad][0])
+    assert not got[:, coef == 0].any()
+
+
+SHAPES = [(1, 1), (2, 1), (10, 128), (7, 3), (10, 9), (33, 8), (100, 65), (257, 7), (1000, 333), (4097, 130), (5000, 1),
+          (50257, 5), (64, 2051), (9, 9000)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("C,B", SHAPES)
+def test_token_logp(C, B, dtype):
+    z, labels, z64, lab = logits(C, B, dtype, seed=C + B)
+    lp, _ = ref_logp(z64, lab, np.ones(B, bool))
+    got = h(L1.token_logp(z, labels)).astype(np.float64)
+    assert (np.abs(got - lp) <= el(C, lp)).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("C,B,pad,off", [(1, 1, 0, 0), (10, 128, 0, 0), (7, 3, 2, 1), (33, 8, 3, 5), (257, 7, 0, 0),
+                                         (1000, 333, 1, 3), (4097, 130, 6, 0), (20, 2051, 0, 1), (50257, 5, 0, 0)])
+@pytest.mark.parametrize("kl", [False, True])
+def test_policy_loss(C, B, pad, off, dtype, kl):
+    torch = _torch()
+    z, labels, z64, lab = logits(C, B, dtype, seed=3 * C + B, pad=pad, off=off)
+    rng = np.random.default_rng(B)
+    w = np.where(rng.random(B) < 0.3, 0.0, rng.uniform(0.5, 2.0, B)).astype(np.float32)
+    w[B // 2] = 1.0
+    lab = lab.copy()
+    lab[rng.random(B) < 0.1] = -100  # ignored
+    lab[B // 2] = C - 1
+    labels.copy_(torch.from_numpy(lab.astype(np.int32)))
+    counts = (w != 0) & (lab >= 0)
+    z[:, torch.from_numpy(~counts).to(z.device)] = float("nan")  # whatever the others hold
+    lp, p = ref_logp(z64, lab, counts)
+    step = 0.3 * rng.standard_normal(B)
+    for border in (math.log(0.8), math.log(1.3)):  # no ratio where one rounding decides
+        step = np.where(np.abs(step - border) < 0.02, border + 0.03, step)
+    old, adv = (lp - step).astype(np.float32), rng.standard_normal(B).astype(np.float32)
+    old[~counts], adv[~counts] = np.nan, np.inf
+    ref = (lp + 0.5 * rng.standard_normal(B)).astype(np.float32) if kl else None
+    stats, coef = ref_policy(lp, counts, w.astype(np.float64), old.astype(np.float64), adv.astype(np.float64),
+                             None if ref is None else ref.astype(np.float64), 0.2, 0.3, 0.1)
+    dbuf = torch.full((C, B + pad + 3), 7.0, dtype=z.dtype, device=z.device)
+    st, dz, got = L1.policy_loss(z, labels, vec(old), vec(adv), ref_logp=None if ref is None else vec(ref), weights=vec(w),
+                                 clip_low=0.2, clip_high=0.3, kl_coef=0.1, dlogits=dbuf[:, :B])
+    assert (np.abs(h(got).astype(np.float64) - lp) <= el(C, lp)).all()
+    share = np.where(counts, w, 0) / w[counts].sum()
+    size = np.where(counts, np.exp(np.clip(lp - np.nan_to_num(old), -9, 9)) * np.abs(np.nan_to_num(adv, posinf=0)), 0)
+    if kl:
+        size = size + np.where(counts, 0.1 * (np.abs(np.expm1(ref - lp)) + 1), 0)
+    # a mean's error: its terms' (1 + |q| for the kl, whose parts cancel), and one rounding
+    tol = (share * (size + 3) * 4 * (el(C, lp) + 2.0 ** -22)).sum() + 2.0 ** -22 * (1 + np.abs(stats))
+    assert (np.abs(h(st).astype(np.float64) - stats) <= tol).all(), (h(st), stats)
+    check_dz(dz, p, lab, coef, share * size, C, lp, dtype)
+    assert bool((dbuf[:, B:] == 7).all())  # the padding is not touched
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("C,B,pairs", [(1, 4, 1), (10, 40, 3), (1000, 333, 4), (257, 7, 2), (300, 600, 100)])
+@pytest.mark.parametrize("smoothing", [0.0, 0.2])
+def test_preference_loss(C, B, pairs, dtype, smoothing):
+    torch = _torch()
+    z, labels, z64, lab = logits(C, B, dtype, seed=C * B)
+    rng = np.random.default_rng(pairs)
+    w = (rng.random(B) < 0.8).astype(np.float32)
+    # empty sequences among them; tokens before the first and behind the last
+    ptr = np.sort(rng.integers(1 if B > 8 else 0, B - B // 8 + 1, 2 * pairs + 1)).astype(np.int32)
+    ptr[1] = ptr[0]
+    inside = (np.arange(B) >= ptr[0]) & (np.arange(B) < ptr[-1])
+    lp, p = ref_logp(z64, lab, w != 0)
+    beta = 0.1
+    sums = np.array([(w * lp)[ptr[q]:ptr[q + 1]].sum() for q in range(2 * pairs)])
+    ref = (sums + rng.standard_normal(2 * pairs) * 5).astype(np.float32)
+    rew = beta * (sums - ref.astype(np.float64))
+    D = rew[0::2] - rew[1::2]
+    ls = lambda x: -np.logaddexp(0, -x)  # noqa: E731
+    sig = lambda x: 1 / (1 + np.exp(-x))  # noqa: E731
+    loss = (-(1 - smoothing) * ls(D) - smoothing * ls(-D)).mean()
+    dD = beta / pairs * (sig(D) - (1 - smoothing))
+    coef = np.zeros(B)
+    for q in range(2 * pairs):
+        coef[ptr[q]:ptr[q + 1]] = (dD[q // 2] if q % 2 == 0 else -dD[q // 2]) * w[ptr[q]:ptr[q + 1]]
+    dz = torch.full_like(z, 7.0)
+    lo, dz, got = L1.preference_loss(z, labels, torch.from_numpy(ptr).to(z.device), ref_logp=vec(ref), weights=vec(w),
+                                     beta=beta, label_smoothing=smoothing, dlogits=dz)
+    err = np.array([(w * el(C, lp))[ptr[q]:ptr[q + 1]].sum() for q in range(2 * pairs)])
+    assert (np.abs(h(got).astype(np.float64) - rew) <= beta * (err + 2.0 ** -23 * np.abs(sums)) + 2.0 ** -23 * np.abs(rew)).all()
+    eD = beta * (err[0::2] + err[1::2])
+    assert abs(float(lo) - loss) <= eD.max() + 2.0 ** -22 * (1 + abs(loss))  # |d loss / d D| <= 1
+    scale = np.zeros(B)
+    for q in range(2 * pairs):
+        scale[ptr[q]:ptr[q + 1]] = beta / pairs * w[ptr[q]:ptr[q + 1]] * (1 + (err[q] + err[q ^ 1]) * beta / 4 / el(C, 0.0))
+    check_dz(dz, p, lab, coef, scale, C, lp, dtype)
+    assert not bool(dz[:, torch.from_numpy(~inside).to(z.device)].any())
+
+
+def test_gradients_against_differences():
+    # central differences of the losses' own values: step 2^-4, third derivatives below 1 (a loss of softmax probabilities
+    # with |adv| <= 1, ratios near 1), so the truncation is below 2^-8 / 6 and the values' rounding 2^-22 / 2^-4
+    torch = _torch()
+    C, B = 11, 6
+    z, labels, z64, lab = logits(C, B, "float32", seed=5)
+    lp, _ = ref_logp(z64, lab, np.ones(B, bool))
+    old, adv, ref = vec(lp - 0.05), vec(np.linspace(-1, 1, B)), vec(lp + 0.2)
+    ptr = torch.tensor([0, 2, 3, 5, 6], dtype=torch.int32, device=z.device)
+    policy = lambda x, g: L1.policy_loss(x, labels, old, adv, ref_logp=ref, kl_coef=0.5, clip_low=0.9, clip_high=9.0, grad=g)  # noqa: E731
+    prefer = lambda x, g: L1.preference_loss(x, labels, ptr, beta=0.5, label_smoothing=0.1, grad=g)  # noqa: E731
+    for f in (policy, prefer):
+        dz = h(f(z, True)[1])
+        step = 2.0 ** -4
+        for c, b in ((0, 0), (3, 1), (int(lab[2]), 2), (10, 3), (int(lab[4]), 4), (5, 5)):
+            v = []
+            for s in (step, -step):
+                x = z.clone()
+                x[c, b] += s
+                v.append(float(f(x, False)[0][0]))
+            assert abs((v[0] - v[1]) / (2 * step) - dz[c, b]) <= step * step / 6 + 2.0 ** -22 / step, (c, b)
+
+
+def test_masked_classes_and_empty_batches():
+    torch = _torch()
+    z, labels, z64, lab = logits(50, 12, "float32", seed=9)
+    z[20:, ::2] = float("-inf")  # classes excluded; whole ranges of them
+    lab = np.minimum(lab, 19)
+    labels = torch.from_numpy(lab.astype(np.int32)).to(z.device)
+    z[:, 3] = torch.finfo(torch.float32).min  # the type's lowest value everywhere: uniform
+    z64 = z.cpu().double().numpy()
+    with np.errstate(invalid="ignore"):
+        lp, p = ref_logp(z64, lab, np.ones(12, bool))
+    got = h(L1.token_logp(z, labels)).astype(np.float64)
+    assert abs(got[3] + math.log(50)) <= el(50, lp[3])
+    assert (np.abs(got - lp) <= el(50, lp)).all()
+    st, dz, _ = L1.policy_loss(z, labels, vec(lp), vec(np.ones(12)))
+    assert not bool(dz[20:, ::2].any()) and bool(torch.isfinite(dz).all())
+    # no token counts: zeros
+    st, dz, got = L1.policy_loss(z, labels, vec(lp), vec(np.ones(12)), weights=vec(np.zeros(12)))
+    assert not bool(st.any()) and not bool(dz.any()) and not bool(got.any())
+    # no tokens, no pairs
+    e = torch.empty((50, 0), device=z.device)
+    none = torch.empty(0, device=z.device)
+    nolab = torch.empty(0, dtype=torch.int32, device=z.device)
+    st, dz, got = L1.policy_loss(e, nolab, none, none)
+    assert not bool(st.any()) and dz.shape == (50, 0) and got.numel() == 0
+    assert L1.token_logp(e, nolab).numel() == 0
+    loss, dz, rew = L1.preference_loss(z, labels, torch.zeros(1, dtype=torch.int32, device=z.device))
+    assert float(loss) == 0.0 and not bool(dz.any()) and rew.numel() == 0
+    loss, _, rew = L1.preference_loss(e, nolab, torch.zeros(3, dtype=torch.int32, device=z.device), ref_logp=vec([1.0, 2.0]))
+    assert h(rew) == pytest.approx([-0.1, -0.2]) and float(loss) == pytest.approx(math.log1p(math.exp(-0.1)))
+
+
+def test_offsets_outside_the_tokens_stay_in_bounds():
+    # offsets beyond [0, B] or falling back are read as clamped ones: no token outside, no write outside dlogits
+    torch = _torch()
+    z, labels, _, _ = logits(20, 16, "float32", seed=2)
+    bad = torch.tensor([-5, 4, 2, 99, 7], dtype=torch.int32, device=z.device)
+    good = torch.tensor([0, 4, 4, 16, 16], dtype=torch.int32, device=z.device)
+    first = torch.tensor([0, 4, 4], dtype=torch.int32, device=z.device)
+    _, _, r = L1.preference_loss(z, labels, bad)
+    _, _, want = L1.preference_loss(z, labels, first)
+    assert h(r)[:2].tolist() == h(want).tolist()
+    assert bool(torch.isfinite(r).all()) and good.numel() == 5
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_gradient_in_place_and_repeatable(dtype):
+    torch = _torch()
+    z, labels, _, _ = logits(700, 77, dtype, seed=1)
+    old, adv = vec(np.full(77, -5.0)), vec(np.linspace(-1, 1, 77))
+    st, dz, lp = L1.policy_loss(z, labels, old, adv)
+    st2, dz2, lp2 = L1.policy_loss(z.clone(), labels, old, adv)
+    assert torch.equal(dz, dz2) and torch.equal(st, st2) and torch.equal(lp, lp2)
+    own = z.clone()
+    _, back, _ = L1.policy_loss(own, labels, old, adv, dlogits=own)
+    assert back is own and torch.equal(own, dz)
+    ptr = torch.tensor([0, 30, 77], dtype=torch.int32, device=z.device)
+    a = L1.preference_loss(z, labels, ptr)
+    own = z.clone()
+    b = L1.preference_loss(own, labels, ptr, dlogits=own)
+    assert all(torch.equal(x, y) for x, y in zip(a, b))
+    only = L1.policy_loss(z, labels, old, adv, grad=False)
+    assert only[1] is None and torch.equal(only[0], st)
+
+
+def test_streams_and_graphs():
+    torch = _torch()
+    z, labels, _, _ = logits(300, 129, "bfloat16", seed=4)
+    old, adv = vec(np.full(129, -4.0)), vec(np.linspace(-1, 1, 129))
+    ptr = torch.tensor([0, 60, 129], dtype=torch.int32, device=z.device)
+    want = [L1.policy_loss(z, labels, old, adv), L1.preference_loss(z, labels, ptr)]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    got = [L1.policy_loss(z, labels, old, adv, stream=side), L1.preference_loss(z, labels, ptr, stream=side)]
+    side.synchronize()
+    for a, b in zip(want, got):
+        assert all(torch.equal(x, y) for x, y in zip(a, b))
+    # two graphs captured one after the other, replayed beside each other with other inputs between
+    zs, graphs, outs = [z.clone(), z.clone()], [], []
+    for x in zs:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append((L1.policy_loss(x, labels, old, adv), L1.preference_loss(x, labels, ptr)))
+        graphs.append(g)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for k in range(3):
+        for i, x in enumerate(zs):
+            x.copy_(torch.randn(300, 129, device=z.device) * (1 + i + k))
+        torch.cuda.synchronize()
+        for s, g in zip(streams, graphs):
+            with torch.cuda.stream(s):
+                g.replay()
+        torch.cuda.synchronize()
+        for x, o in zip(zs, outs):
+            for a, b in zip(o, (L1.policy_loss(x, labels, old, adv), L1.preference_loss(x, labels, ptr))):
+                assert all(torch.equal(u, v) for u, v in zip(a, b))
+
+
+def test_refusals():
+    torch = _torch()
+    z, labels, _, _ = logits(20, 16, "float32", seed=2)
+    old = vec(np.zeros(16))
+    with pytest.raises(ValueError):
+        L1.token_logp(z.t(), labels)
+    with pytest.raises(ValueError):
+        L1.token_logp(z, labels[:8])
+    with pytest.raises(TypeError):
+        L1.token_logp(z, labels.long())
+    with pytest.raises(TypeError):
+        L1.token_logp(z.double(), labels)
+    with pytest.raises(ValueError):
+        L1.policy_loss(z, labels, old[:4], old)
+    with pytest.raises(ValueError):
+        L1.policy_loss(z, labels, old, old, dlogits=torch.empty(20, 15, device=z.device))
+    with pytest.raises(ValueError):
+        L1.policy_loss(z, labels, old, old, dlogits=torch.empty_like(z).to(torch.bfloat16))
+    with pytest.raises(ValueError):
+        L1.policy_loss(z, labels, old, old, dlogits=z, grad=False)
+    with pytest.raises(L1.L1CSRError):  # overlapping, not the same matrix
+        buf = torch.zeros(21, 16, device=z.device)
+        L1.policy_loss(buf[:20], labels, old, old, dlogits=buf[1:])
+    with pytest.raises(L1.L1CSRError):
+        L1.policy_loss(z, labels, old, old, clip_low=1.5)
+    with pytest.raises(L1.L1CSRError):
+        L1.policy_loss(z, labels, old, old, kl_coef=float("nan"))
+    with pytest.raises(ValueError):
+        L1.preference_loss(z, labels, torch.zeros(4, dtype=torch.int32, device=z.device))
+    with pytest.raises(L1.L1CSRError):
+        L1.preference_loss(z, labels, torch.zeros(3, dtype=torch.int32, device=z.device), label_smoothing=0.7)
+    with pytest.raises(ValueError):
+        L1.token_logp(z, labels.cpu())
