@@ -534,7 +534,7 @@ hipError_t run_type(const token_loss_args &a, const policy_args &P, void *ws, hi
 }  // namespace
 
 size_t token_loss_workspace_bytes(int C, int B, int pairs) {
-    return C > 0 && B >= 0 && pairs >= 0 ? carve(C, B, pairs, nullptr).bytes : 0;
+    return C > 0 && B >= 0 && pairs >= 0 && (B > 0 || pairs > 0) ? carve(C, B, pairs, nullptr).bytes : 0;
 }
 
 hipError_t launch_token_logp(const token_loss_args &a, void *ws, hipStream_t s) {

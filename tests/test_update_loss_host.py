@@ -1,0 +1,117 @@
+"""Host-side checks (CPU) of muon_update and the losses over logits: workspace sizes, and bad arguments that the C entry
+points refuse before any launch; the binding's own checks of tensors."""
+import ctypes as C
+import os
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+LIB = os.path.join(ROOT, "paper_1905_07931_amd", "libl1csr.so")
+OK, EINVAL, EUNSUPPORTED = 0, -1, -5
+OP_MUON, OP_MUON_F16, OP_TOKEN_LOSS = 14, 15, 16
+NO_GPU = not os.path.exists("/dev/kfd")
+P, Q, R, W = (C.c_void_p(1 << 20), C.c_void_p(1 << 30), C.c_void_p(1 << 33), C.c_void_p(1 << 36))  # never dereferenced
+BIG = 1 << 40
+nan, inf = float("nan"), float("inf")
+
+
+@pytest.fixture(scope="module")
+def lib():
+    import paper_1905_07931_amd as L1
+    if not os.path.exists(LIB):
+        from paper_1905_07931_amd import build
+        build.build(verbose=False)
+    return L1.lib()
+
+
+def test_workspace_sizes(lib):
+    ws = lib.l1csr_workspace_bytes
+    for n, k in [(1, 1), (100, 300), (129, 129), (4096, 9216), (46340, 46340)]:
+        for op in (OP_MUON, OP_MUON_F16):
+            b = ws(op, n, k, 0, 0)
+            assert b > 0 and b % 256 == 0 and b == ws(op, k, n, 0, 0)
+        assert ws(OP_MUON, n, k, 0, 0) >= ws(OP_MUON_F16, n, k, 0, 0)
+    assert ws(OP_MUON, 0, 5, 0, 0) == 0 and ws(OP_MUON, 5, 0, 0, 0) == 0 and ws(OP_MUON, -1, 5, 0, 0) == 0
+    for c, b in [(1, 1), (10, 128), (131072, 7), (32768, 8192), (1, 1 << 20)]:
+        n = ws(OP_TOKEN_LOSS, c, 0, 0, b)
+        assert n % 256 == 0 and n >= 16 * b
+        assert ws(OP_TOKEN_LOSS, c, 1000, 0, b) >= n + 8 * 900
+    assert ws(OP_TOKEN_LOSS, 0, 0, 0, 5) == 0
+
+
+def muon(lib, N=8, K=8, dtype=0, G=P, ldg=8, M=Q, ldm=8, M_out=Q, ldmo=8, mu=0.9, nesterov=1, steps=5, eps=1e-7, scale=1.0,
+         precision=0, O=R, ldo=8, ws=W, ws_bytes=BIG):
+    return lib.muon_update(N, K, dtype, G, ldg, M, ldm, M_out, ldmo, mu, nesterov, steps, eps, scale, precision, O, ldo, ws,
+                           ws_bytes, None)
+
+
+@pytest.mark.skipif(not NO_GPU, reason="validation calls use placeholder pointers; run without a GPU")
+def test_muon_arguments_are_rejected_before_launch(lib):
+    bad = [dict(N=-1), dict(K=-1), dict(dtype=3), dict(dtype=-1), dict(precision=1), dict(precision=2), dict(precision=4),
+           dict(steps=0), dict(steps=33), dict(eps=-1e-9), dict(eps=nan), dict(eps=inf), dict(scale=nan), dict(scale=inf),
+           dict(mu=1.0), dict(mu=-0.1), dict(mu=nan), dict(G=None), dict(O=None), dict(ldg=7), dict(ldo=7), dict(ldm=7),
+           dict(ldmo=7), dict(M=None), dict(ws=None), dict(ws_bytes=1000),
+           dict(O=C.c_void_p((1 << 20) + 4)), dict(O=P, ldo=9), dict(M=P), dict(M_out=P), dict(M_out=R), dict(M=R),
+           dict(M_out=C.c_void_p((1 << 30) + 4)), dict(ldmo=9)]
+    for kw in bad:
+        assert muon(lib, **kw) == EINVAL, kw
+    big = dict(ldg=1 << 23, ldm=1 << 23, ldmo=1 << 23, ldo=1 << 23, M=None, M_out=None)
+    assert muon(lib, N=1, K=(1 << 22) + 1, **big) == EUNSUPPORTED
+    assert muon(lib, N=65536, K=32768, M=None, M_out=None, ldg=32768, ldo=32768, O=C.c_void_p(1 << 44)) == EUNSUPPORTED
+    for n, k in ((0, 8), (8, 0), (0, 0)):  # nothing to do
+        assert muon(lib, N=n, K=k, ws=None, ws_bytes=0) == OK
+
+
+def policy(lib, Cn=8, B=8, dtype=0, z=P, ld=8, labels=Q, old=Q, adv=Q, ref=None, w=None, lo=0.2, hi=0.2, kl=0.1, dz=R,
+           ldd=8, logp=None, stats=Q, ws=W, ws_bytes=BIG):
+    return lib.l1csr_policy_loss(Cn, B, dtype, z, ld, labels, old, adv, ref, w, lo, hi, kl, dz, ldd, logp, stats, ws, ws_bytes,
+                                 None)
+
+
+def preference(lib, Cn=8, B=8, dtype=0, z=P, ld=8, labels=Q, pairs=2, ptr=Q, ref=None, w=None, beta=0.1, ls=0.0, dz=R, ldd=8,
+               rewards=None, loss=Q, ws=W, ws_bytes=BIG):
+    return lib.l1csr_preference_loss(Cn, B, dtype, z, ld, labels, pairs, ptr, ref, w, beta, ls, dz, ldd, rewards, loss, ws,
+                                     ws_bytes, None)
+
+
+@pytest.mark.skipif(not NO_GPU, reason="validation calls use placeholder pointers; run without a GPU")
+def test_loss_arguments_are_rejected_before_launch(lib):
+    common = [dict(Cn=0), dict(Cn=-1), dict(B=-1), dict(dtype=3), dict(z=None), dict(ld=7), dict(ldd=7), dict(labels=None),
+              dict(ws=None), dict(ws_bytes=100), dict(dz=C.c_void_p((1 << 20) + 4)), dict(dz=P, ldd=9)]
+    for kw in common + [dict(old=None), dict(adv=None), dict(stats=None), dict(lo=-0.1), dict(lo=1.1), dict(lo=nan),
+                        dict(hi=-0.1), dict(hi=inf), dict(kl=-0.1), dict(kl=nan)]:
+        assert policy(lib, **kw) == EINVAL, kw
+    for kw in common + [dict(pairs=-1), dict(ptr=None), dict(loss=None), dict(beta=-1.0), dict(beta=nan), dict(ls=-0.1),
+                        dict(ls=0.6), dict(ls=nan), dict(pairs=(1 << 30))]:
+        assert preference(lib, **kw) == EINVAL, kw
+    logp = lambda **k: lib.l1csr_token_logp(*(k.get(n, d) for n, d in (  # noqa: E731
+        ("Cn", 8), ("B", 8), ("dtype", 0), ("z", P), ("ld", 8), ("labels", Q), ("logp", R), ("ws", W), ("ws_bytes", BIG))), None)
+    for kw in [dict(Cn=0), dict(B=-1), dict(dtype=7), dict(z=None), dict(ld=7), dict(labels=None), dict(logp=None),
+               dict(ws=None), dict(ws_bytes=10)]:
+        assert logp(**kw) == EINVAL, kw
+    assert logp(B=0, logp=None, labels=None, ws=None, ws_bytes=0, z=None) == OK
+
+
+def test_binding_refuses_host_tensors_and_wrong_shapes():
+    torch = pytest.importorskip("torch")
+    import paper_1905_07931_amd as L1
+    z, lab = torch.zeros(4, 3), torch.zeros(3, dtype=torch.int32)
+    with pytest.raises(ValueError):
+        L1.token_logp(z, lab)
+    with pytest.raises(ValueError):
+        L1.policy_loss(z, lab, z[0], z[0])
+    with pytest.raises(ValueError):
+        L1.preference_loss(z, lab, lab)
+    with pytest.raises(TypeError):
+        L1.token_logp([[0.0]], lab)
+    with pytest.raises(ValueError):
+        L1.orthogonalize(z)
+    with pytest.raises(TypeError):
+        L1.orthogonalize(z.numpy())
+    W = L1.CSR(4, 3, torch.zeros(5, dtype=torch.int32), torch.zeros(1, dtype=torch.int32), torch.zeros(1), 0)
+    for f in (L1.prox_muon_step, L1.prox_muon_recompress):
+        with pytest.raises(ValueError):
+            f(W, z, L1.MuonState(torch.zeros(4, 3)), 0.1, 0.1)
+    for name in ("token_logp", "policy_loss", "preference_loss", "orthogonalize", "MuonState", "prox_muon_step",
+                 "prox_muon_recompress", "F16"):
+        assert name in L1.__all__ and hasattr(L1, name)
