@@ -1020,9 +1020,12 @@ int norm_blocks(const muon_args &a) {
 
 // Steps between two products with X: the m x m products that stand for them pay where X is
 // wider than square and they are not bound by their launches.  us, one step and three, two parts:
-// 300 x 784 127 and 131, 512 x 512 136 and 155, 600 x 2000 219 and 194, 1001 x 1777 271 and 261, 2048 x 2048
-// 867 and 987, 2048 x 4096 1230 and 1146, 4096 x 9216 7181 and 5366.
-int most_steps(int m, int n) { return m > 512 && 2 * (int64_t)n >= 3 * (int64_t)m ? kMaxGroup : 1; }
+// 512 x 512 137 and 157, 300 x 784 128 and 133, 200 x 2000 128 and 127, 400 x 2000 174 and 164, 512 x 4096 219 and 188,
+// 200 x 9216 193 and 152; 600 x 2000 219 and 194, 1001 x 1777 271 and 261, 2048 x 2048 867 and 987, 2048 x 4096 1230 and
+// 1146, 4096 x 9216 7181 and 5366.
+int most_steps(int m, int n) {
+    return 2 * (int64_t)n >= 3 * (int64_t)m && (m > 512 || n >= 5 * (int64_t)m) ? kMaxGroup : 1;
+}
 
 template <typename T, int g>
 hipError_t run_small(const muon_args &a, const update_src &u, void *ws, hipStream_t s) {

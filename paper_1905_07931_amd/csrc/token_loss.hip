@@ -197,6 +197,47 @@ struct policy_args {
 
 enum { kLogp = 0, kPolicy = 1, kPreference = 2 };
 
+struct policy_sums {
+    double weight = 0, pg = 0, kl = 0, off = 0;  // the last three weighted
+};
+
+// w d loss / d lp of a token (times the sum of weights), its loss added to the sums
+__device__ __forceinline__ float policy_token(const policy_args &P, const float *w, int b, float lp, policy_sums &s) {
+    const float wt = w ? w[b] : 1.f, A = P.adv[b], r = expf(lp - P.old_lp[b]);
+    const bool off = (A > 0.f && r > P.high) || (A < 0.f && r < P.low);
+    const float used = off ? (A > 0.f ? P.high : P.low) : r;
+    float kl = 0.f, dlp = off ? 0.f : -A * r;
+    if (P.ref_lp) {
+        const float q = P.ref_lp[b] - lp, e = expm1f(q);
+        kl = e - q;
+        dlp -= P.kl_coef * e;
+    }
+    s.weight += wt;
+    s.pg += (double)wt * (-A * used);
+    s.kl += (double)wt * kl;
+    s.off += off ? wt : 0.f;
+    return wt * dlp;
+}
+
+// A pair's loss, its rewards given, and d loss / d (sum of the preferred sequence), which is minus the other's
+struct pair_terms {
+    double loss, slope;
+    __device__ __forceinline__ pair_terms(double chosen, double rejected, float smoothing, float beta, int pairs) {
+        const double D = chosen - rejected, e = exp(-fabs(D)), up = D >= 0 ? 1 / (1 + e) : e / (1 + e);  // sig(D)
+        const double down = D >= 0 ? e / (1 + e) : 1 / (1 + e);
+        // -log sig(D) = log(1 + e) + max(-D, 0)
+        loss = log1p(e) + (1 - (double)smoothing) * fmax(-D, 0.0) + smoothing * fmax(D, 0.0);
+        slope = (smoothing * up - (1 - (double)smoothing) * down) * beta / pairs;
+    }
+};
+
+// tokens lo .. mid - 1 and mid .. hi - 1 of a pair, within [0, B] whatever the offsets are
+__device__ __forceinline__ void pair_range(const int *seq, int p, int B, int &lo, int &mid, int &hi) {
+    lo = min(max(seq[2 * p], 0), B);
+    mid = min(max(seq[2 * p + 1], lo), B);
+    hi = min(max(seq[2 * p + 2], mid), B);
+}
+
 __device__ __forceinline__ double block_sum(double x, double *lds) {
 #pragma unroll
     for (int d = kWave / 2; d >= 1; d >>= 1) x += __shfl_xor(x, d, kWave);
@@ -217,7 +258,7 @@ __global__ __launch_bounds__(kThreads) void token_kernel(int C, int B, const T *
     __shared__ double lds[kThreads / kWave];
     const int L = 1 << lane_shift, per = kThreads >> lane_shift;
     const int lane = threadIdx.x & (L - 1);
-    double sw = 0, sl = 0, sk = 0, sc = 0;
+    policy_sums sums;
     for (int64_t b0 = (int64_t)blockIdx.x * per; b0 < B; b0 += (int64_t)gridDim.x * per) {
         const int64_t b = b0 + (threadIdx.x >> lane_shift);
         const bool on = b < B && live(labels, w, (int)b, C);
@@ -246,29 +287,10 @@ __global__ __launch_bounds__(kThreads) void token_kernel(int C, int B, const T *
         if constexpr (KIND == kLogp) continue;
         o.m[b] = top;
         o.inv[b] = on ? 1.f / s : 0.f;
-        float coef = 0.f;
-        if constexpr (KIND == kPolicy) {
-            if (on) {
-                const float wt = w ? w[b] : 1.f, A = P.adv[b], r = expf(lp - P.old_lp[b]);
-                const bool off = (A > 0.f && r > P.high) || (A < 0.f && r < P.low);
-                const float used = off ? (A > 0.f ? P.high : P.low) : r;
-                float kl = 0.f, dlp = off ? 0.f : -A * r;
-                if (P.ref_lp) {
-                    const float q = P.ref_lp[b] - lp, e = expm1f(q);
-                    kl = e - q;
-                    dlp -= P.kl_coef * e;
-                }
-                coef = wt * dlp;
-                sw += wt;
-                sl += (double)wt * (-A * used);
-                sk += (double)wt * kl;
-                sc += off ? wt : 0.f;
-            }
-        }
-        o.coef[b] = coef;
+        o.coef[b] = KIND == kPolicy && on ? policy_token(P, w, (int)b, lp, sums) : 0.f;
     }
     if constexpr (KIND == kPolicy) {
-        const double t[4] = {block_sum(sw, lds), block_sum(sl, lds), block_sum(sk, lds), block_sum(sc, lds)};
+        const double t[4] = {block_sum(sums.weight, lds), block_sum(sums.pg, lds), block_sum(sums.kl, lds), block_sum(sums.off, lds)};
         if (threadIdx.x < 4) o.sums[threadIdx.x * kTokenBlocks + blockIdx.x] = t[threadIdx.x];
     }
 }
@@ -281,7 +303,8 @@ __global__ __launch_bounds__(kThreads) void pair_kernel(int C, int B, int pairs,
                                                         float *__restrict__ rewards, double *__restrict__ loss) {
     __shared__ double lds[kThreads / kWave];
     const int p = blockIdx.x;
-    const int lo = min(max(seq[2 * p], 0), B), mid = min(max(seq[2 * p + 1], lo), B), hi = min(max(seq[2 * p + 2], mid), B);
+    int lo, mid, hi;
+    pair_range(seq, p, B, lo, mid, hi);
     double s0 = 0, s1 = 0;
     for (int b = lo + (int)threadIdx.x; b < hi; b += kThreads) {
         if (!live(labels, w, b, C)) continue;
@@ -290,19 +313,16 @@ __global__ __launch_bounds__(kThreads) void pair_kernel(int C, int B, int pairs,
     }
     s0 = beta * (block_sum(s0, lds) - (ref ? ref[2 * p] : 0.f));
     s1 = beta * (block_sum(s1, lds) - (ref ? ref[2 * p + 1] : 0.f));
-    const double D = s0 - s1, e = exp(-fabs(D)), up = D >= 0 ? 1 / (1 + e) : e / (1 + e);  // sig(D)
-    const double down = D >= 0 ? e / (1 + e) : 1 / (1 + e);
+    const pair_terms t(s0, s1, smoothing, beta, pairs);
     if (threadIdx.x == 0) {
         if (rewards) {
             rewards[2 * p] = (float)s0;
             rewards[2 * p + 1] = (float)s1;
         }
-        // -log sig(D) = log(1 + e) + max(-D, 0)
-        loss[p] = log1p(e) + (1 - (double)smoothing) * fmax(-D, 0.0) + smoothing * fmax(D, 0.0);
+        loss[p] = t.loss;
     }
-    const double dS = (smoothing * up - (1 - (double)smoothing) * down) * beta / pairs;
     for (int b = lo + (int)threadIdx.x; b < hi; b += kThreads)
-        if (live(labels, w, b, C)) coef[b] = (float)((b < mid ? dS : -dS) * (w ? w[b] : 1.f));
+        if (live(labels, w, b, C)) coef[b] = (float)((b < mid ? t.slope : -t.slope) * (w ? w[b] : 1.f));
 }
 
 // The loss from the partial sums, by one workgroup: out[0..3] = loss, policy part, kl, clipped share,
@@ -428,6 +448,145 @@ __global__ __launch_bounds__(kThreads) void gradient_kernel(int C, int B, const 
     }
 }
 
+// A small problem in one workgroup, which is all that such a call costs: 2^tx_shift threads over
+// the columns, the others over the classes, the tokens' values in LDS.
+constexpr int kSmallThreads = 1024;
+constexpr int kSmallTokens = 1024;       // most columns
+constexpr int kSmallElements = 1 << 15;  // most logits
+
+template <typename T, int KIND>
+__global__ __launch_bounds__(kSmallThreads) void small_loss_kernel(token_loss_args a, policy_args P, int tx_shift) {
+    constexpr int waves = kSmallThreads / kWave;
+    __shared__ float part_m[kSmallThreads], part_s[kSmallThreads];  // (2^tx_shift columns of as many waves as have them)
+    __shared__ float tm[kSmallTokens], tinv[kSmallTokens], tcoef[kSmallTokens], tlp[kSmallTokens];
+    __shared__ double lds[waves];
+    const int C = a.C, B = a.B, TX = 1 << tx_shift, TY = kSmallThreads >> tx_shift;
+    const int tx = threadIdx.x & (TX - 1), ty = threadIdx.x >> tx_shift;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const T *z = static_cast<const T *>(a.logits) + tx;  // B <= TX
+    const bool on = tx < B && live(a.labels, a.weights, tx, C);
+    auto sum = [&](double x) {
+#pragma unroll
+        for (int d = kWave / 2; d >= 1; d >>= 1) x += __shfl_xor(x, d, kWave);
+        __syncthreads();
+        if (lane == 0) lds[wave] = x;
+        __syncthreads();
+        double t = 0;
+        for (int i = 0; i < waves; ++i) t += lds[i];
+        return t;
+    };
+    float m = -INFINITY, s = 0.f;
+    if (on)
+        for (int c = ty; c < C; c += 4 * TY) {
+            float y[4], top = m;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int r = c + u * TY;
+                const float v = to_f32(z[(int64_t)min(r, C - 1) * a.ld]);
+                y[u] = r < C ? v : -INFINITY;
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) top = fmaxf(top, y[u]);
+            const float base = top == -INFINITY ? 0.f : top;
+            s *= exp_neg(m - base);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) s += exp_neg(y[u] - base);
+            m = top;
+        }
+    auto join = [&](float m2, float s2) {
+        const float top = fmaxf(m, m2), base = top == -INFINITY ? 0.f : top;
+        s = s * exp_neg(m - base) + s2 * exp_neg(m2 - base);
+        m = top;
+    };
+    for (int d = TX; d < kWave; d <<= 1) {
+        const float m2 = __shfl_xor(m, d, kWave), s2 = __shfl_xor(s, d, kWave);
+        join(m2, s2);
+    }
+    part_m[threadIdx.x] = m;
+    part_s[threadIdx.x] = s;
+    __syncthreads();
+    policy_sums ps;
+    if (ty == 0) {
+        // (a wave's rows are joined already where it has several)
+        for (int t = TX > kWave ? TX : kWave; t < kSmallThreads; t += TX > kWave ? TX : kWave)
+            join(part_m[t + tx], part_s[t + tx]);
+        const float lp = on ? (to_f32(z[(int64_t)a.labels[tx] * a.ld]) - m) - logf(s) : 0.f;
+        if (tx < B) {
+            if (a.logp) a.logp[tx] = lp;
+            if constexpr (KIND != kLogp) {
+                tm[tx] = m;
+                tinv[tx] = on ? 1.f / s : 0.f;
+                tlp[tx] = lp;
+                tcoef[tx] = KIND == kPolicy && on ? policy_token(P, a.weights, tx, lp, ps) : 0.f;
+            }
+        }
+    }
+    if constexpr (KIND == kLogp) return;
+    float scale = 1.f;
+    if constexpr (KIND == kPolicy) {
+        const double sw = sum(ps.weight), inv = sw != 0 ? 1 / sw : 0.0;
+        const double pg = sum(ps.pg) * inv, kl = sum(ps.kl) * inv, off = sum(ps.off) * inv;
+        if (threadIdx.x == 0) {
+            a.out[0] = (float)(pg + P.kl_coef * kl);
+            a.out[1] = (float)pg;
+            a.out[2] = (float)kl;
+            a.out[3] = (float)off;
+        }
+        scale = (float)inv;
+    } else {
+        __syncthreads();
+        double loss = 0;
+        for (int p = wave; p < a.pairs; p += waves) {
+            int lo, mid, hi;
+            pair_range(a.seq_ptr, p, B, lo, mid, hi);
+            double s0 = 0, s1 = 0;
+            for (int b = lo + lane; b < hi; b += kWave) {
+                const double x = (double)tlp[b] * (a.weights ? a.weights[b] : 1.f);
+                if (!live(a.labels, a.weights, b, C)) continue;
+                if (b < mid) s0 += x; else s1 += x;
+            }
+#pragma unroll
+            for (int d = kWave / 2; d >= 1; d >>= 1) {
+                s0 += __shfl_xor(s0, d, kWave);
+                s1 += __shfl_xor(s1, d, kWave);
+            }
+            s0 = a.beta * (s0 - (a.ref_logp ? a.ref_logp[2 * p] : 0.f));
+            s1 = a.beta * (s1 - (a.ref_logp ? a.ref_logp[2 * p + 1] : 0.f));
+            const pair_terms t(s0, s1, a.smoothing, a.beta, a.pairs);
+            if (lane == 0) {
+                if (a.rewards) {
+                    a.rewards[2 * p] = (float)s0;
+                    a.rewards[2 * p + 1] = (float)s1;
+                }
+                loss += t.loss;
+            }
+            for (int b = lo + lane; b < hi; b += kWave)
+                if (live(a.labels, a.weights, b, C))
+                    tcoef[b] = (float)((b < mid ? t.slope : -t.slope) * (a.weights ? a.weights[b] : 1.f));
+        }
+        loss = sum(loss);
+        if (threadIdx.x == 0) a.out[0] = a.pairs > 0 ? (float)(loss / a.pairs) : 0.f;
+    }
+    if (a.dlogits == nullptr || tx >= B) return;
+    __syncthreads();
+    const float coef = tcoef[tx] * scale, f = coef != 0.f ? -coef * tinv[tx] : 0.f;
+    const float own = coef != 0.f ? -coef * expm1f(tlp[tx]) : 0.f;
+    const int label = a.labels[tx];
+    T *dz = static_cast<T *>(a.dlogits) + tx;
+    m = tm[tx];
+    for (int c = ty; c < C; c += 4 * TY) {
+        float y[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) y[u] = to_f32(z[(int64_t)min(c + u * TY, C - 1) * a.ld]);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int r = c + u * TY;
+            if (r >= C) continue;
+            dz[(int64_t)r * a.ldd] = (T)(r == label ? own : (coef != 0.f ? f * exp_neg(y[u] - m) : 0.f));
+        }
+    }
+}
+
 template <typename T>
 constexpr int kVec = 16 / sizeof(T);
 
@@ -481,6 +640,12 @@ carved carve(int C, int B, int pairs, void *ws) {
 
 template <typename T, int V, int KIND>
 hipError_t run(const token_loss_args &a, const policy_args &P, void *ws, hipStream_t s) {
+    if (a.B <= kSmallTokens && (int64_t)a.C * a.B <= kSmallElements) {
+        int shift = 0;
+        while ((1 << shift) < a.B) ++shift;
+        small_loss_kernel<T, KIND><<<1, kSmallThreads, 0, s>>>(a, P, shift);
+        return hipGetLastError();
+    }
     const grid_shape g = shape_of(a.C, a.B, V);
     carved w = carve(a.C, a.B, a.pairs, ws);
     token_out t = w.t;
