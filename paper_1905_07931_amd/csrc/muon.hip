@@ -158,28 +158,33 @@ struct parts_of {
     }
 };
 
-// e with 2^e |U|_F in [1/2, 1), returned negated; scal[0] = s, scal[1] = s^2 with
-// s = 1 / (2^e (|U|_F + eps))
+// 2^-e |U|_F in [1/2, 1) and s = 1 / (2^-e (|U|_F + eps))
+struct norm_scale {
+    int e = 0;
+    float s;
+    __device__ __forceinline__ norm_scale(double norm, float eps) {
+        if (norm < INFINITY) {
+            (void)frexp(norm, &e);
+            const double d = ldexp(norm + (double)eps, -e);
+            s = d > 0 ? (float)(1 / d) : 0.f;
+        } else {
+            s = NAN;  // an infinity or a NaN in U, or a norm past double: nothing to give
+        }
+    }
+};
+
+// e of U's norm from its partial sums; scal[0] = s, scal[1] = s^2
 template <int waves>
 __device__ __forceinline__ int scale_of(const double *part, int n_part, float eps, float *scal, bool write,
                                         double *lds) {
     double sum = 0;
     for (int i = threadIdx.x; i < n_part; i += waves * kWave) sum += part[i];
-    const double norm = sqrt(block_sum<waves>(sum, lds));
-    int e = 0;
-    double s;
-    if (norm < INFINITY) {
-        (void)frexp(norm, &e);
-        const double d = ldexp(norm + (double)eps, -e);
-        s = d > 0 ? 1 / d : 0;
-    } else {
-        s = NAN;  // an infinity or a NaN in U, or a norm past double: nothing to give
-    }
+    const norm_scale ns(sqrt(block_sum<waves>(sum, lds)), eps);
     if (write && threadIdx.x == 0) {
-        scal[0] = (float)s;
-        scal[1] = (float)(s * s);
+        scal[0] = ns.s;
+        scal[1] = ns.s * ns.s;
     }
-    return e;
+    return ns.e;
 }
 
 // V elements of U (0 past its ends): every load in flight before the first is used
@@ -557,6 +562,161 @@ __global__ __launch_bounds__(2 * g *kWave) void small_step_kernel(const float *_
         if constexpr (!LAST) gram_slice<g, waves, per>(LX, wave, lane, acc, low);
     }
     if constexpr (!LAST) store_gram<g, waves, per>(partial, wave, lane, acc, low);
+}
+
+// ---------------------------------------------------------------------------
+// matrices that one workgroup's LDS holds: the whole call but for the prox in one launch
+// ---------------------------------------------------------------------------
+//
+// g x c waves, a 32 x 32 block of X each.  LDS: A, X by columns, and in turn A X by columns and X by
+// rows (whose reads and writes barriers keep apart).
+template <typename T, int g, int c>
+__global__ __launch_bounds__(g * c * kWave) void tiny_kernel(update_src u, int tall, int m, int n, int n_steps, float eps,
+                                                             T *O, int64_t ldo, float scale) {
+    constexpr int waves = g * c, steps = 2 * g, wide = 2 * c;  // steps of the rows, of the columns
+    __shared__ __attribute__((aligned(16))) char LA[g * steps * 2 * kBlock];
+    __shared__ __attribute__((aligned(16))) char LX[c * steps * 2 * kBlock];
+    __shared__ __attribute__((aligned(16))) char LY[c * steps * 2 * kBlock];
+    __shared__ double lds[waves];
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+    const int l = lane & 31, h = lane >> 5, gi = wave / c, gj = wave - gi * c;
+    // U along its rows; element v of a thread is (i, j) of X
+    auto at = [&](int v, int &i, int &j) {
+        const int f = threadIdx.x + waves * kWave * v;
+        i = tall ? f % (32 * g) : f / (32 * c);
+        j = tall ? f / (32 * g) : f % (32 * c);
+    };
+    float dev;
+    {
+        float x[16];
+        const T *G = static_cast<const T *>(u.G);
+        float gv[16], mv[16] = {};
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            int i, j;
+            at(v, i, j);
+            const int r = min(tall ? j : i, u.N - 1), k = min(tall ? i : j, u.K - 1);
+            gv[v] = to_f32(G[(int64_t)r * u.ldg + k]);
+        }
+        if (u.M)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                int i, j;
+                at(v, i, j);
+                const int r = min(tall ? j : i, u.N - 1), k = min(tall ? i : j, u.K - 1);
+                mv[v] = u.M[(int64_t)r * u.ldm + k];
+            }
+        double sum = 0;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            int i, j;
+            at(v, i, j);
+            const bool on = i < m && j < n;
+            const float m_new = fmaf(u.mu, mv[v], gv[v]);
+            if (on && u.M_out) u.M_out[(int64_t)(tall ? j : i) * u.ldo + (tall ? i : j)] = m_new;
+            x[v] = on ? update_at(u, gv[v], m_new) : 0.f;
+            sum = fma((double)x[v], (double)x[v], sum);
+        }
+        const norm_scale ns(sqrt(block_sum<waves>(sum, lds)), eps);
+        dev = ns.s;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            int i, j;
+            at(v, i, j);
+            const float y = ldexpf(x[v], kScaleX - ns.e);
+            const _Float16 hi = (_Float16)y, lo = (_Float16)(y - (float)hi);
+            char *a = LX + element_at(j, i, steps), *b = LY + element_at(i, j, wide);
+            *reinterpret_cast<_Float16 *>(a) = hi;
+            *reinterpret_cast<_Float16 *>(a + kBlock) = lo;
+            *reinterpret_cast<_Float16 *>(b) = hi;
+            *reinterpret_cast<_Float16 *>(b + kBlock) = lo;
+        }
+    }
+    const int mine = (gj * steps + 2 * gi) * (2 * kBlock) + l * 16 + 8 * h;  // this block in the columns of X and A X
+    for (int k = 0; k < n_steps; ++k) {
+        __syncthreads();
+        for (int t = wave; t < tiles_of(g); t += waves) {  // A
+            int ti, tj;
+            tile_of(t, ti, tj);
+            floatx16 acc = {}, low = {};
+#pragma unroll 4
+            for (int st = 0; st < wide; ++st)
+                product_step(LY + (ti * wide + st) * (2 * kBlock) + lane * 16, LY + (tj * wide + st) * (2 * kBlock) + lane * 16,
+                             acc, low);
+            acc = (acc + low) * (dev * dev * 0x1p-14f);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const float v[4] = {acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]};
+                const parts_of<4> p(v);
+                char *d = LA + (tj * steps + 2 * ti + (q >> 1)) * (2 * kBlock) + (q & 1) * 512 + l * 16 + 8 * h;
+                *reinterpret_cast<halfx4 *>(d) = p.hi;
+                *reinterpret_cast<halfx4 *>(d + kBlock) = p.lo;
+                if (ti == tj) continue;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    d = LA + element_at(ti * 32 + 8 * q + 4 * h + e, tj * 32 + l, steps);
+                    *reinterpret_cast<_Float16 *>(d) = p.hi[e];
+                    *reinterpret_cast<_Float16 *>(d + kBlock) = p.lo[e];
+                }
+            }
+        }
+        __syncthreads();
+        floatx16 y = {}, z = {}, s = {};
+#pragma unroll
+        for (int st = 0; st < steps; ++st)
+            product_step(LA + (gi * steps + st) * (2 * kBlock) + lane * 16, LX + (gj * steps + st) * (2 * kBlock) + lane * 16, y, s);
+        y = (y + s) * 0x1p-14f;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {  // (X by rows is read: a barrier ago)
+            const float v[4] = {y[4 * q], y[4 * q + 1], y[4 * q + 2], y[4 * q + 3]};
+            const parts_of<4> p(v);
+            char *d = LY + mine + (q >> 1) * (2 * kBlock) + (q & 1) * 512;
+            *reinterpret_cast<halfx4 *>(d) = p.hi;
+            *reinterpret_cast<halfx4 *>(d + kBlock) = p.lo;
+        }
+        __syncthreads();
+        s = floatx16{};
+#pragma unroll
+        for (int st = 0; st < steps; ++st)
+            product_step(LA + (gi * steps + st) * (2 * kBlock) + lane * 16, LY + (gj * steps + st) * (2 * kBlock) + lane * 16, z, s);
+        z = (z + s) * 0x1p-14f;
+        const bool last = k + 1 == n_steps;
+        const float f = last ? dev * scale : dev;
+        float v[16];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const char *p = LX + mine + (q >> 1) * (2 * kBlock) + (q & 1) * 512;
+            const halfx4 hi = *reinterpret_cast<const halfx4 *>(p), lo = *reinterpret_cast<const halfx4 *>(p + kBlock);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                v[4 * q + e] = f * fmaf(kC, z[4 * q + e], fmaf(kB, y[4 * q + e], kA * ((float)hi[e] + (float)lo[e])));
+        }
+        const int j = gj * 32 + l;
+        if (last) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int i = gi * 32 + 8 * (r >> 2) + 4 * h + (r & 3);
+                if (i < m && j < n) O[tall ? j * ldo + i : i * ldo + j] = (T)v[r];
+            }
+            return;
+        }
+        dev = 1.f;
+        __syncthreads();  // A X is read, and X by columns
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const float w[4] = {v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+            const parts_of<4> p(w);
+            char *d = LX + mine + (q >> 1) * (2 * kBlock) + (q & 1) * 512;
+            *reinterpret_cast<halfx4 *>(d) = p.hi;
+            *reinterpret_cast<halfx4 *>(d + kBlock) = p.lo;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                d = LY + element_at(gi * 32 + 8 * q + 4 * h + e, j, wide);
+                *reinterpret_cast<_Float16 *>(d) = p.hi[e];
+                *reinterpret_cast<_Float16 *>(d + kBlock) = p.lo[e];
+            }
+        }
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -1056,9 +1216,23 @@ hipError_t run_small(const muon_args &a, const update_src &u, void *ws, hipStrea
     return e;
 }
 
+template <typename T, int g, int c>
+hipError_t run_tiny(const muon_args &a, const update_src &u, hipStream_t s) {
+    tiny_kernel<T, g, c><<<1, g * c * kWave, 0, s>>>(u, a.N > a.K, std::min(a.N, a.K), std::max(a.N, a.K), a.steps, a.eps,
+                                                     static_cast<T *>(a.O), a.ldo, a.scale * exp2i(-kScaleX));
+    return hipGetLastError();
+}
+
 template <typename T>
 hipError_t run_small(const muon_args &a, const update_src &u, void *ws, hipStream_t s) {
-    const int m = std::min(a.N, a.K);
+    const int m = std::min(a.N, a.K), n = std::max(a.N, a.K);
+    // In one launch where a workgroup's waves need no more than that time of a chain of launches
+    // (us, launches and one): 32 x 128 29.9 and 17.7, 32 x 256 31.0 and 24.3, 64 x 128 36.8 and 24.6, 96 x 128 45.5 and
+    // 36.4; not 32 x 512 34.6 and 44.0, 64 x 256 37.7 and 41.3 (16 waves).
+    if (m <= 32 && n <= 128) return run_tiny<T, 1, 4>(a, u, s);
+    if (m <= 32 && n <= 256) return run_tiny<T, 1, 8>(a, u, s);
+    if (m <= 64 && n <= 128) return run_tiny<T, 2, 4>(a, u, s);
+    if (m <= 96 && n <= 128) return run_tiny<T, 3, 4>(a, u, s);
     if (m <= 32) return run_small<T, 1>(a, u, ws, s);
     if (m <= 64) return run_small<T, 2>(a, u, ws, s);
     if (m <= 96) return run_small<T, 3>(a, u, ws, s);
