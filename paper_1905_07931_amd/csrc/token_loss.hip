@@ -44,8 +44,8 @@ __device__ __forceinline__ void load_vec(const T *p, T (&x)[V]) {
 
 typedef unsigned word4 __attribute__((ext_vector_type(4), aligned(2)));
 
-// Past the caches: dz is not read again here, and z then stays in the last-level cache for
-// the gradient pass (32768 x 8192 bf16 370 -> 315 us, 32768 x 4099 230 -> 181)
+// Past the caches, where dz would only displace what is read (the whole call: 32768 x 8192 bf16 370 ->
+// 315 us, 32768 x 4099 230 -> 181)
 template <typename T, int V>
 __device__ __forceinline__ void store_vec(T *p, const T (&x)[V]) {
     if constexpr (sizeof(T) * V == 16) {
@@ -392,13 +392,14 @@ __global__ __launch_bounds__(kThreads) void gradient_kernel(int C, int B, const 
         __builtin_memset(&ones[v], on ? 0xff : 0, sizeof(T));
     }
     __builtin_memcpy(keep, ones, sizeof(T) * V);
-    // the classes that the sums read last come first: they may still be in the last-level cache
-    const int c0 = (g.splits - 1 - (int)blockIdx.y) * g.rows, c1 = min(C, c0 + g.rows);
+    const int c0 = blockIdx.y * g.rows, c1 = min(C, c0 + g.rows);
     const bool whole = k.at == k.col0;
     const int64_t step = (int64_t)TY * ld, stepd = (int64_t)TY * ldd;
-    const T *p = z + (int64_t)(c0 + ty) * ld + k.at;
-    T *d = dz + (int64_t)(c0 + ty) * ldd + k.at;
-    for (int c = c0 + ty; c < c1; c += U * TY, p += U * step, d += U * stepd) {
+    // from the range's end, whose logits the sums read last (the whole call: 326 -> 316 us)
+    for (int c = c0 + ty + max(0, c1 - c0 - ty - 1) / (U * TY) * (U * TY); c >= c0; c -= U * TY) {
+        if (c >= c1) continue;
+        const T *p = z + (int64_t)c * ld + k.at;
+        T *d = dz + (int64_t)c * ldd + k.at;
         T x[U][V];
         const int n = min(U, (c1 - c + TY - 1) / TY);
         if (work) {
