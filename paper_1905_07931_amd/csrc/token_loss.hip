@@ -104,6 +104,9 @@ __device__ __forceinline__ bool live(const int *labels, const float *w, int b, i
     return a >= 0 && a < C && (w == nullptr || w[b] != 0.f);
 }
 
+// Partial (maximum, sum of exponentials) of the columns over a range of classes.  Memory-bound: 112 us for 537 MB at
+// 32768 x 8192 bf16 (4.8 TB/s); the vector units, at 10 instructions and an exponential (a quarter of their
+// rate) a logit, are half busy, which is why the rescaling comes once in eight rows.
 template <typename T, int V>
 __global__ __launch_bounds__(kThreads) void column_sums_kernel(int C, int B, const T *__restrict__ z, int64_t ld,
                                                                const int *__restrict__ labels,
@@ -361,6 +364,7 @@ __global__ __launch_bounds__(kThreads) void finish_kernel(int n, const double *_
     finish<KIND>(n, sums, kl_coef, lds, true, out);
 }
 
+// Memory-bound: 205 us for 1074 MB at 32768 x 8192 bf16 (5.2 TB/s, a large copy 4.9).
 // dz, over the layout of column_sums_kernel; z and dz may be the same matrix (every
 // element is read by the thread that writes it; a thread's loads of its
 // neighbour's columns are not used).  A token's own class comes last, from lp.
@@ -449,7 +453,8 @@ __global__ __launch_bounds__(kThreads) void gradient_kernel(int C, int B, const 
     }
 }
 
-// A small problem in one workgroup, which is all that such a call costs: 2^tx_shift threads over
+// A small problem in one workgroup: its launches are all that such a call costs (us, three or four of them and one:
+// policy loss 10 x 128 19.4 and 13.1, 32768 x 1 20.8 and 16.7, 32 x 1000 19.6 and 15.4). 2^tx_shift threads over
 // the columns, the others over the classes, the tokens' values in LDS.
 constexpr int kSmallThreads = 1024;
 constexpr int kSmallTokens = 1024;       // most columns
@@ -591,6 +596,8 @@ __global__ __launch_bounds__(kSmallThreads) void small_loss_kernel(token_loss_ar
 template <typename T>
 constexpr int kVec = 16 / sizeof(T);
 
+// (more leave a last partial round: with 2048 the whole policy loss at 32768 x 8192 bf16 took 405 us for 370, with
+// 768 369, 32768 x 4099 259, 232 and 253)
 constexpr int kWorkgroups = 1024;
 
 // ranges of a round of loads at least
