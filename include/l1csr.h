@@ -612,12 +612,14 @@ int l1csr_softmax_xent(int32_t C, int32_t B, const float *logits, int64_t ld,
  * |U|_F is summed in double.  precision L1CSR_F32: operands as two fp16 parts
  * (22 bits), three exact products, fp32 sums; about 1e-6 of |O|_F off the exact
  * result after five steps, as fp32 products are.  L1CSR_F16: one part, about
- * 1.5e-3 off.  The accuracy is that of the whole matrix (relative to |O|_F), not
- * of single small entries, and it needs a norm that is not lost against eps
- * (|U|_F >= 1e-4 eps).  A zero U gives zeros; a NaN or an infinity anywhere in
- * U gives NaN everywhere, as the formula does.  N * K < 2^31 and N, K <= 2^22
- * (L1CSR_EUNSUPPORTED).  Results are reproducible.  ws as
- * l1csr_workspace_bytes(L1CSR_OP_MUON or L1CSR_OP_MUON_F16, N, K, 0, 0).
+ * 1.5e-3 off (both are computed with two parts where min(N, K) <= 128).  The
+ * accuracy is that of the whole matrix (relative to |O|_F), not of single small
+ * entries, and it is that of a norm of eps at least: X is kept to 2^-38, so where
+ * |U|_F is far below eps, and the update as far below 1, its error is not.
+ * A zero U gives zeros; a NaN or an infinity anywhere in U gives NaN everywhere,
+ * as the formula does.  N * K < 2^31 and N, K <= 2^22 (L1CSR_EUNSUPPORTED;
+ * l1csr_workspace_bytes gives 0).  Results are reproducible.
+ * ws as l1csr_workspace_bytes(L1CSR_OP_MUON or L1CSR_OP_MUON_F16, N, K, 0, 0).
  */
 #define L1CSR_MUON_MAX_STEPS 32
 int muon_update(int32_t N, int32_t K, int dtype, const void *G, int64_t ldg, const float *M, int64_t ldm,
@@ -634,7 +636,9 @@ int muon_update(int32_t N, int32_t K, int dtype, const void *G, int64_t ldg, con
  * exclude a class.  Sums over tokens are in double; everything is reproducible.
  * dlogits [C][ldd], of the type of the logits, receives d loss / d logits (every
  * column of it; NULL: the loss alone); it may be the logits themselves (with the
- * same leading dimension), but may not overlap them otherwise (L1CSR_EINVAL).
+ * same leading dimension), but may not overlap them otherwise, and no other output may
+ * overlap an input or an output (L1CSR_EINVAL).  C, B <= 2^30 and pairs < 2^24
+ * (L1CSR_EUNSUPPORTED; l1csr_workspace_bytes gives 0).
  * ws as l1csr_workspace_bytes(L1CSR_OP_TOKEN_LOSS, C, pairs, 0, B), pairs = 0 but
  * for the preference loss.
  *

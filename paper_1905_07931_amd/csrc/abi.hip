@@ -97,9 +97,10 @@ size_t typed_bytes(int64_t rows, int64_t cols, int64_t ld, int dtype) {
     return rows > 0 && cols > 0 ? (size_t)(((rows - 1) * ld + cols) * dtype_bytes(dtype)) : 0;
 }
 
-// What the calls over logits check alike
-int token_check(const token_loss_args &a, size_t ws_bytes, const void *ws) {
+// What the calls over logits check alike; n_out: floats of a.out
+int token_check(const token_loss_args &a, int n_out, size_t ws_bytes, const void *ws) {
     if (a.C <= 0 || a.B < 0 || a.pairs < 0 || bad_dtype(a.dtype)) return L1CSR_EINVAL;
+    if (!token_loss_fits(a.C, a.B, a.pairs)) return L1CSR_EUNSUPPORTED;
     if (bad_dense(a.logits, a.C, a.B, a.ld)) return L1CSR_EINVAL;
     if (a.B > 0 && a.labels == nullptr) return L1CSR_EINVAL;
     if (a.dlogits != nullptr) {
@@ -109,6 +110,18 @@ int token_check(const token_loss_args &a, size_t ws_bytes, const void *ws) {
                                                   typed_bytes(a.C, a.B, a.ld, a.dtype)))
             return L1CSR_EINVAL;
     }
+    // no output may lie in an input (its values are read after the first outputs are stored) or in another output
+    const size_t tokens = sizeof(float) * (size_t)a.B, seqs = sizeof(float) * 2 * (size_t)a.pairs;
+    const struct { const void *p; size_t n; } mem[] = {
+        {a.logp, tokens}, {a.rewards, seqs}, {a.out, sizeof(float) * (size_t)n_out},
+        {a.dlogits, typed_bytes(a.C, a.B, a.ldd, a.dtype)}, {a.labels, tokens}, {a.weights, tokens},
+        {a.old_logp, tokens}, {a.adv, tokens}, {a.ref_logp, a.seq_ptr ? seqs : tokens},
+        {a.seq_ptr, a.seq_ptr ? seqs + sizeof(int32_t) : 0}, {a.logits, typed_bytes(a.C, a.B, a.ld, a.dtype)}};
+    constexpr int outs = 4, all = sizeof(mem) / sizeof(mem[0]);
+    for (int i = 0; i < outs; ++i)
+        for (int j = i + 1; j < all; ++j)
+            if (!(i == 3 && j == all - 1) && bytes_overlap(mem[i].p, mem[i].n, mem[j].p, mem[j].n))
+                return L1CSR_EINVAL;
     const size_t need = token_loss_workspace_bytes(a.C, a.B, a.pairs);
     if (need > 0 && (ws == nullptr || ws_bytes < need)) return L1CSR_EINVAL;
     return L1CSR_OK;
@@ -873,7 +886,7 @@ int l1csr_token_logp(int32_t C, int32_t B, int dtype, const void *logits, int64_
     token_loss_args a{};
     a.C = C; a.B = B; a.dtype = dtype;
     a.logits = logits; a.ld = ld; a.labels = labels; a.logp = logp;
-    const int rc = token_check(a, ws_bytes, ws);
+    const int rc = token_check(a, 0, ws_bytes, ws);
     if (rc != L1CSR_OK) return rc;
     if (B > 0 && logp == nullptr) return L1CSR_EINVAL;
     return hip_status(launch_token_logp(a, ws, stream));
@@ -892,7 +905,7 @@ int l1csr_policy_loss(int32_t C, int32_t B, int dtype, const void *logits, int64
     a.out = stats;
     if (!finite_f(clip_low) || !finite_f(clip_high) || !finite_f(kl_coef)) return L1CSR_EINVAL;
     if (clip_low < 0.f || clip_low > 1.f || clip_high < 0.f || kl_coef < 0.f || stats == nullptr) return L1CSR_EINVAL;
-    const int rc = token_check(a, ws_bytes, ws);
+    const int rc = token_check(a, 4, ws_bytes, ws);
     if (rc != L1CSR_OK) return rc;
     if (B > 0 && (old_logp == nullptr || advantages == nullptr)) return L1CSR_EINVAL;
     return hip_status(launch_policy_loss(a, ws, stream));
@@ -911,7 +924,7 @@ int l1csr_preference_loss(int32_t C, int32_t B, int dtype, const void *logits, i
     a.rewards = rewards; a.out = loss;
     if (!finite_f(beta) || !(beta >= 0.f) || !(label_smoothing >= 0.f && label_smoothing <= 0.5f)) return L1CSR_EINVAL;
     if (loss == nullptr || (pairs > 0 && seq_ptr == nullptr) || pairs > INT32_MAX / 2 - 1) return L1CSR_EINVAL;
-    const int rc = token_check(a, ws_bytes, ws);
+    const int rc = token_check(a, 1, ws_bytes, ws);
     if (rc != L1CSR_OK) return rc;
     return hip_status(launch_preference_loss(a, ws, stream));
 }
@@ -920,6 +933,7 @@ int muon_update(int32_t N, int32_t K, int dtype, const void *G, int64_t ldg, con
                 float *M_out, int64_t ldmo, float mu, int nesterov, int steps, float eps, float scale, int precision,
                 void *O, int64_t ldo, void *ws, size_t ws_bytes, hipStream_t stream) {
     if (N < 0 || K < 0 || bad_dtype(dtype)) return L1CSR_EINVAL;
+    if (!muon_fits(N, K)) return L1CSR_EUNSUPPORTED;
     if (precision != L1CSR_F32 && precision != L1CSR_F16) return L1CSR_EINVAL;
     if (steps < 1 || steps > L1CSR_MUON_MAX_STEPS) return L1CSR_EINVAL;
     if (!finite_f(eps) || eps < 0.f || !finite_f(scale)) return L1CSR_EINVAL;
@@ -936,8 +950,6 @@ int muon_update(int32_t N, int32_t K, int dtype, const void *G, int64_t ldg, con
     const int parts = precision == L1CSR_F32 ? 2 : 1;
     const size_t need = muon_workspace_bytes(N, K, parts);
     if (need > 0 && (ws == nullptr || ws_bytes < need)) return L1CSR_EINVAL;
-    // 32-bit chunk numbers and offsets inside a packed group; grid rows
-    if ((int64_t)N * K > INT32_MAX || N > (1 << 22) || K > (1 << 22)) return L1CSR_EUNSUPPORTED;
     muon_args a{};
     a.N = N; a.K = K; a.dtype = dtype;
     a.G = G; a.ldg = ldg;

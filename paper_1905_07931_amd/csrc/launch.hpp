@@ -282,6 +282,7 @@ struct token_loss_args {
     float *rewards;                // [2 pairs], nullable
     float *out;                    // policy: 4 values, preference: 1
 };
+bool token_loss_fits(int C, int B, int pairs);  // else it has no workspace either
 size_t token_loss_workspace_bytes(int C, int B, int pairs);
 hipError_t launch_token_logp(const token_loss_args &a, void *ws, hipStream_t s);
 hipError_t launch_policy_loss(const token_loss_args &a, void *ws, hipStream_t s);
@@ -303,6 +304,7 @@ struct muon_args {
     void *O;             // [N][ldo]; may be G
     int64_t ldo;
 };
+bool muon_fits(int N, int K);  // else it has no workspace either
 size_t muon_workspace_bytes(int N, int K, int parts);
 hipError_t launch_muon(const muon_args &a, void *ws, hipStream_t s);
 

@@ -1339,8 +1339,11 @@ hipError_t run_type(const muon_args &a, void *ws, hipStream_t s) {
 
 }  // namespace
 
+// 32-bit chunk numbers, and offsets inside a packed group; grid rows
+bool muon_fits(int N, int K) { return (int64_t)N * K <= INT32_MAX && N <= (1 << 22) && K <= (1 << 22); }
+
 size_t muon_workspace_bytes(int N, int K, int parts) {
-    return N > 0 && K > 0 ? carve(N, K, parts, nullptr).bytes : 0;
+    return N > 0 && K > 0 && muon_fits(N, K) ? carve(N, K, parts, nullptr).bytes : 0;
 }
 
 hipError_t launch_muon(const muon_args &a, void *ws, hipStream_t s) {

@@ -364,10 +364,10 @@ __global__ __launch_bounds__(kThreads) void finish_kernel(int n, const double *_
     finish<KIND>(n, sums, kl_coef, lds, true, out);
 }
 
-// Memory-bound: 205 us for 1074 MB at 32768 x 8192 bf16 (5.2 TB/s, a large copy 4.9).
 // dz, over the layout of column_sums_kernel; z and dz may be the same matrix (every
 // element is read by the thread that writes it; a thread's loads of its
 // neighbour's columns are not used).  A token's own class comes last, from lp.
+// Memory-bound: 205 us for 1074 MB at 32768 x 8192 bf16 (5.2 TB/s, a large copy 4.9).
 template <typename T, int V, int KIND>
 __global__ __launch_bounds__(kThreads) void gradient_kernel(int C, int B, const T *z, int64_t ld,
                                                             const int *__restrict__ labels, grid_shape g, token_out t,
@@ -706,8 +706,11 @@ hipError_t run_type(const token_loss_args &a, const policy_args &P, void *ws, hi
 
 }  // namespace
 
+// 32-bit class and column numbers with room for a round of a workgroup's loads; the threads of a grid
+bool token_loss_fits(int C, int B, int pairs) { return C <= (1 << 30) && B <= (1 << 30) && pairs < (1 << 24); }
+
 size_t token_loss_workspace_bytes(int C, int B, int pairs) {
-    return C > 0 && B >= 0 && pairs >= 0 && (B > 0 || pairs > 0) ? carve(C, B, pairs, nullptr).bytes : 0;
+    return C > 0 && B >= 0 && pairs >= 0 && (B > 0 || pairs > 0) && token_loss_fits(C, B, pairs) ? carve(C, B, pairs, nullptr).bytes : 0;
 }
 
 hipError_t launch_token_logp(const token_loss_args &a, void *ws, hipStream_t s) {

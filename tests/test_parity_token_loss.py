@@ -316,6 +316,38 @@ def test_streams_and_graphs():
                 assert all(torch.equal(u, v) for u, v in zip(a, b))
 
 
+@pytest.mark.parametrize("B", [7, 300])
+def test_offsets_past_32_bits(B):
+    """Rows so far apart that offsets pass 2^32 elements: the bits of the same columns side by side."""
+    torch = _torch()
+    C, ld = 70001, 65537
+    wide = torch.empty((C, ld), dtype=torch.bfloat16, device="cuda")
+    z = wide[:, 11:11 + B]
+    z.normal_(generator=torch.Generator(device="cuda").manual_seed(1))
+    labels = torch.randint(0, C, (B,), device="cuda").to(torch.int32)
+    labels[0] = C - 1
+    old, adv = torch.full((B,), -11.0, device="cuda"), torch.linspace(-1, 1, B, device="cuda")
+    near = z.contiguous()
+    want = L1.policy_loss(near, labels, old, adv, dlogits=near)
+    got = L1.policy_loss(z, labels, old, adv, dlogits=z)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_outputs_that_are_inputs_are_refused():
+    torch = _torch()
+    z = torch.randn((9, 40), device="cuda")
+    labels = torch.zeros(40, dtype=torch.int32, device="cuda")
+    old, adv, ref = (torch.randn(40, device="cuda") for _ in range(3))
+    ptr = torch.tensor([0, 20, 40], dtype=torch.int32, device="cuda")
+    for kw in (dict(logp=old), dict(logp=adv), dict(logp=ref), dict(stats=old[:4]), dict(logp=z[0]),
+               dict(logp=labels.view(torch.float32))):
+        with pytest.raises(L1.L1CSRError):
+            L1.policy_loss(z, labels, old, adv, ref_logp=ref, **kw)
+    with pytest.raises(L1.L1CSRError):
+        r = torch.zeros(2, device="cuda")
+        L1.preference_loss(z, labels, ptr, ref_logp=r, rewards=r)
+
+
 def test_refusals():
     torch = _torch()
     z, labels, _, _ = logits(20, 16, "float32", seed=2)

@@ -92,6 +92,42 @@ def test_loss_arguments_are_rejected_before_launch(lib):
     assert logp(B=0, logp=None, labels=None, ws=None, ws_bytes=0, z=None) == OK
 
 
+@pytest.mark.skipif(not NO_GPU, reason="validation calls use placeholder pointers; run without a GPU")
+def test_outputs_of_the_losses_apart_from_their_inputs(lib):
+    at = lambda i, off=0: C.c_void_p((1 << 44) + (i << 38) + off)  # noqa: E731
+    z, labels, old, adv, ref, w, dz, logp, stats, ptr = (at(i) for i in range(10))
+    good = dict(z=z, labels=labels, old=old, adv=adv, ref=ref, w=w, dz=dz, logp=logp, stats=stats)
+    # (refused for their size only after every other check: what is left of the call is sound)
+    assert policy(lib, **good, ws_bytes=0) == EINVAL and policy(lib, **good, Cn=(1 << 30) + 1) == EUNSUPPORTED
+    for name, p in list(good.items()):
+        for out in ("logp", "stats", "dz"):
+            if out == name or (name, out) == ("z", "dz"):
+                continue
+            assert policy(lib, **{**good, out: p}) == EINVAL, (name, out)
+    assert policy(lib, **{**good, "logp": at(2, 28)}) == EINVAL
+    both = dict(z=z, labels=labels, ptr=ptr, ref=ref, w=w, dz=dz, rewards=logp, loss=stats)
+    for name, p in list(both.items()):
+        for out in ("rewards", "loss", "dz"):
+            if out == name or (name, out) == ("z", "dz"):
+                continue
+            assert preference(lib, **{**both, out: p}) == EINVAL, (name, out)
+    for p in (z, labels):
+        assert lib.l1csr_token_logp(8, 8, 0, z, 8, labels, p, at(11), BIG, None) == EINVAL
+
+
+@pytest.mark.skipif(not NO_GPU, reason="validation calls use placeholder pointers; run without a GPU")
+def test_sizes_past_the_kernels_numbers_are_refused(lib):
+    many = (1 << 30) + 1
+    assert policy(lib, Cn=many) == EUNSUPPORTED and policy(lib, B=many, ld=many, ldd=many) == EUNSUPPORTED
+    assert preference(lib, Cn=many) == EUNSUPPORTED and preference(lib, pairs=1 << 24) == EUNSUPPORTED
+    assert lib.l1csr_token_logp(many, 1, 2, P, 1, Q, R, W, BIG, None) == EUNSUPPORTED
+    ws = lib.l1csr_workspace_bytes  # nothing to allocate for a call that is refused
+    assert ws(OP_TOKEN_LOSS, many, 0, 0, 1) == 0 and ws(OP_TOKEN_LOSS, 8, 1 << 24, 0, 8) == 0
+    assert ws(OP_MUON, 65536, 32768, 0, 0) == 0 and ws(OP_MUON_F16, (1 << 22) + 1, 1, 0, 0) == 0
+    assert muon(lib, N=65536, K=32768, M=None, M_out=None, ldg=32768, ldo=32768, O=C.c_void_p(1 << 44), ws=None,
+                ws_bytes=0) == EUNSUPPORTED
+
+
 def test_binding_refuses_host_tensors_and_wrong_shapes():
     torch = pytest.importorskip("torch")
     import paper_1905_07931_amd as L1
