@@ -1254,7 +1254,8 @@ def policy_loss(logits, labels, old_logp, advantages, ref_logp=None, weights=Non
     k = exp(ref_logp - lp) - (ref_logp - lp) - 1 (0 without ref_logp), the loss is the weighted mean over the tokens of
     -min(r adv, clip(r, 1 - clip_low, 1 + clip_high) adv) + kl_coef k.  A token counts if its label lies in [0, C) and its
     weight (weights float32 [B], default 1) is not 0; the logits of the others are not used and their columns of
-    dlogits are 0.  dlogits (the type and shape of logits) may be logits itself; grad=False leaves it out.
+    dlogits are 0.  dlogits (the type and shape of logits) may be logits itself; grad=False leaves it out.  No other
+    output may share memory with an input (logp with old_logp, say).
     Returns (stats, dlogits, logp): stats[4] = loss, mean policy term, mean k, share of clipped tokens."""
     Cn, B, code, ld, dlogits, ldd, index = _token_args(logits, labels, weights, dlogits, grad, stream)
     f32 = _torch_module.float32
@@ -1354,7 +1355,7 @@ def orthogonalize(G, out=None, steps=5, eps=1e-7, scale=1.0, precision=None, str
 
     G [N][K] float32, bfloat16 or float16; out, of the same shape and type, may be G itself.  precision: F32 (fp32
     accuracy) or F16 (operands rounded to fp16, about 1.5e-3 of the norm off, less than a bfloat16 result's own
-    rounding); by default F16 for a bfloat16 G and F32 for the others.  Returns out."""
+    rounding; as F32 where min(N, K) <= 128); by default F16 for a bfloat16 G and F32 for the others.  Returns out."""
     if precision is None:
         precision = F16 if _dtype_code(G, "G") == 1 else F32
     if out is None:
@@ -1363,9 +1364,11 @@ def orthogonalize(G, out=None, steps=5, eps=1e-7, scale=1.0, precision=None, str
     return _muon_update(G, out, None, None, MuonState(None, 0.0, False, steps, eps), scale, precision, stream)
 
 
-def _muon_args(W, G, st):
-    """What the Prox-Muon calls check of the layer and its gradient; returns (N, K, scale)."""
+def _muon_args(W, G, st, eta, lam):
+    """What the Prox-Muon calls check before the momentum is stored; returns (N, K, scale)."""
     N, K, _ = _mat(G, "G")
+    if not (0 < C.c_float(eta).value < math.inf and 0 <= C.c_float(lam).value < math.inf):
+        raise ValueError("eta must be positive, lam not negative, and both finite")
     if N != W.n_rows or K != W.n_cols:
         raise ValueError("G must be [n_rows][n_cols]")
     if st.m is None:
@@ -1379,13 +1382,42 @@ def _muon_args(W, G, st):
     return N, K, scale
 
 
+def _span(t):
+    """Bytes [first, past the last) that a tensor's elements lie in."""
+    if t.numel() == 0:
+        return 0, 0
+    p = t.data_ptr()
+    return p, p + t.element_size() * (1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride())))
+
+
+def _muon_out(W, out, capacity, index, dense):
+    """What prox_muon_recompress checks of its output CSR before the momentum is stored: large enough, and apart from
+    W's arrays and the `dense` tensors."""
+    torch = _torch_module
+    if out.n_rows != W.n_rows or out.n_cols != W.n_cols or out.row_ptr.numel() < W.n_rows + 1:
+        raise ValueError("out must have the shape of W")
+    if capacity is not None and capacity > min(out.col_idx.numel(), out.vals.numel()):
+        raise ValueError("capacity exceeds out's arrays")
+    outs = []
+    for t, dtype, name in ((out.row_ptr, torch.int32, "out.row_ptr"), (out.col_idx, torch.int32, "out.col_idx"),
+                           (out.vals, torch.float32, "out.vals")):
+        _vec(_same_device(index, t, name), dtype, name)
+        outs.append(_span(t))
+    ins = [_span(t) for t in (W.row_ptr, W.col_idx, W.vals, *dense)]
+    for i, (a0, a1) in enumerate(outs):
+        if any(a0 < b1 and b0 < a1 for b0, b1 in outs[i + 1:] + ins):
+            raise ValueError("out shares memory with W, the update, the momentum or itself")
+
+
 def prox_muon_step(W: CSR, G, st: MuonState, eta, lam, Z=None, m_out=None, row_counts=None, precision=F32,
                    stream=None):
     """One Prox-Muon step of the l1 phase over all N*K weights: m' = mu m + G, O = scale * NS(G + mu m') (muon_update;
     without nesterov NS(m')), Z = S_{eta*lam}(W - eta O).  Z may be G itself; st.m is updated in place, or m_out receives
     m' and st.m is kept.  Returns Z."""
-    N, K, scale = _muon_args(W, G, st)
+    N, K, scale = _muon_args(W, G, st, eta, lam)
     W.validate_shapes()
+    if row_counts is not None:
+        _vec_of(row_counts, _torch_module.int32, N, G.get_device(), "row_counts", "row (n_rows)")
     if Z is None:
         Z = _new((N, K), _torch().float32, G.device, stream)
     _muon_update(G, Z, st.m, st.m if m_out is None else m_out, st, scale, precision, stream)
@@ -1396,10 +1428,12 @@ def prox_muon_recompress(W: CSR, G, st: MuonState, eta, lam, O=None, capacity=No
                          precision=F32, stream=None):
     """W' = CSR of the Prox-Muon step (the bits of prox_muon_step and csr_recompress), the recompression fused with the
     threshold (prox_l1_recompress).  O (float32 [N][K], may be G itself) receives the update; st.m is updated in
-    place, but not by a call that fails for its capacity."""
+    place, but not by a call that fails, for its capacity or its arguments."""
     torch = _torch()
-    N, K, scale = _muon_args(W, G, st)
+    N, K, scale = _muon_args(W, G, st, eta, lam)
     W.validate_shapes()
+    if out is not None:
+        _muon_out(W, out, capacity, G.get_device(), (st.m, G if O is None else O))
     cap = capacity if capacity is not None else (N * K if out is None else min(out.col_idx.numel(), out.vals.numel()))
     short = cap < N * K  # the count may not fit: the momentum is stored behind the recompression
     m_new = _new((N, K), torch.float32, G.device, stream) if short else st.m

@@ -335,6 +335,84 @@ def test_streams_and_graphs():
             assert all(torch.equal(a, b) for a, b in zip(o, eager))
 
 
+@pytest.mark.parametrize("N,K", [(3001, 50), (3001, 200)])
+def test_offsets_past_32_bits(N, K):
+    """Rows so far apart that offsets pass 2^32 elements: the bits of the same matrix without the gaps."""
+    torch = _torch()
+    ld = 1500001
+    wide = torch.empty((N, ld), dtype=torch.bfloat16, device="cuda")
+    G = wide[:, 3:3 + K]
+    G.copy_(gradient(N, K, 1))
+    want = L1.orthogonalize(G.contiguous())
+    assert torch.equal(L1.orthogonalize(G, out=G), want)
+
+
+@pytest.mark.parametrize("schedule", ["serial", "two_stream"])
+def test_captured_step(schedule):
+    """l1_step with a MuonState in a graph, replayed with eager steps between: each replay gives the eager result."""
+    torch = _torch()
+    N, K, Bt = 300, 784, 64
+    W, L = _layer(N, K, 0.1, 4)
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    X, dY = (torch.randn((r, Bt), device="cuda", generator=gen) for r in (K, N))
+
+    def buffers():
+        out = L1.CSR(N, K, *(torch.empty(n, dtype=t, device="cuda") for n, t in
+                             ((N + 1, torch.int32), (N * K, torch.int32), (N * K, torch.float32))))
+        return dict(Y=torch.empty((N, Bt), device="cuda"), dX=torch.empty((K, Bt), device="cuda"),
+                    dW=torch.empty((N, K), device="cuda"), csc=L1.CSC.empty(K, W.nnz, "cuda"), out=out)
+
+    a, b = buffers(), buffers()
+    sa, sb = L1.MuonState.zeros((N, K), "cuda"), L1.MuonState.zeros((N, K), "cuda")
+    run = lambda st, o: L1.l1_step(W, X, dY, 0.02, 0.05, schedule=schedule, adaptive=st, **o)  # noqa: E731
+    run(sb, b)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        run(sa, a)
+    for rep in range(3):
+        X.normal_(generator=gen)
+        dY.normal_(generator=gen)
+        sa.m.normal_(generator=gen)
+        sb.m.copy_(sa.m)
+        run(sb, b)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        n = int(b["out"].row_ptr[-1])
+        for x, y in zip([sa.m, a["Y"], a["dX"], a["dW"], a["out"].row_ptr, a["out"].col_idx[:n], a["out"].vals[:n]],
+                        [sb.m, b["Y"], b["dX"], b["dW"], b["out"].row_ptr, b["out"].col_idx[:n], b["out"].vals[:n]]):
+            assert torch.equal(x, y), rep
+
+
+def test_refused_steps_leave_the_momentum():
+    torch = _torch()
+    W, _ = _layer(20, 30, 0.5, 1)
+    G, m0 = gradient(20, 30, 1), gradient(20, 30, 2)
+    st = L1.MuonState(m0.clone())
+    new = lambda rows=21, n=600: L1.CSR(20, 30, *(torch.empty(k, dtype=t, device="cuda") for k, t in  # noqa: E731
+                                                  ((rows, torch.int32), (n, torch.int32), (n, torch.float32))))
+    for eta, lam in ((0.0, 0.1), (-0.1, 0.1), (0.1, -0.1), (float("nan"), 0.1), (0.1, float("inf")), (1e39, 0.1), (1e-60, 0.1)):
+        for f in (L1.prox_muon_step, L1.prox_muon_recompress):
+            with pytest.raises(ValueError):
+                f(W, G, st, eta, lam)
+    with pytest.raises(ValueError):
+        L1.prox_muon_step(W, G, st, 0.1, 0.1, row_counts=torch.empty(19, dtype=torch.int32, device="cuda"))
+    inside = new()
+    inside.vals = st.m.view(-1)
+    twice = new()
+    twice.vals = twice.col_idx.view(torch.float32)
+    for kw in (dict(out=new(rows=20)), dict(out=new(), capacity=601), dict(out=W), dict(out=inside), dict(out=twice)):
+        with pytest.raises(ValueError):
+            L1.prox_muon_recompress(W, G, st, 0.1, 0.1, **kw)
+    with pytest.raises(L1.L1CSRError):
+        L1.prox_muon_recompress(W, G, st, 0.1, 0.1, capacity=-1)
+    assert torch.equal(st.m, m0)
+    out = L1.prox_muon_recompress(W, G, st, 0.1, 0.1, out=new())
+    want = L1.prox_muon_recompress(W, G, L1.MuonState(m0.clone()), 0.1, 0.1)
+    assert all(bits_equal(x, y) for x, y in zip(out.to_host(), want.to_host()))
+
+
 def test_refusals():
     torch = _torch()
     G = gradient(20, 30, 1)
