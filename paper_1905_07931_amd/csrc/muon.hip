@@ -28,6 +28,7 @@
 // 300 x 784 against 8e-4).
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 #include <utility>
 
 #include "common.hpp"
@@ -873,11 +874,13 @@ __device__ __forceinline__ void finish_block(const product_args &P, int gi, int 
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 }
 
-// One tile, or one range of its reduction.  Stages of packed blocks are copied straight into LDS, two
-// ahead of the one in use; fragments are read in the lane's order.  With two parts a wave reads 8
-// fragments for 12 matrix instructions and the pipe is 68 % busy at the 1.77 GHz that the power limit leaves
-// (4096 x 4096 x 4096: 337-368 us, 1.12-1.22 PFLOP/s of fp16); with one part 4 for 4, the LDS's full
-// rate: 52 % busy, 141-147 us (0.95 PFLOP/s).
+// One tile, or one range of its reduction.  Stages of packed blocks are copied straight into LDS, up to
+// three ahead of the one in use; fragments are read in the lane's order, the next step's while this one's
+// are multiplied (five steps of 4096 x 4096, read behind the barrier and ahead: two parts 3875 and 3690 us, one
+// part 1632 and 1553).  With two parts a wave reads 8 fragments for 12 matrix instructions and the pipe is
+// 74 % busy at the 1.64 GHz that the power limit leaves (4096 x 4096 x 4096: 348 us, 1.18 PFLOP/s of
+// fp16); with one part 6 for 8, 56 % busy at 1.93 GHz, 139 us (0.99 PFLOP/s), where all workgroups
+// start and end together and the result's 10 bytes an element are waited for.
 template <int NP, typename S, typename O>
 __global__ __launch_bounds__(S::threads, 2) void product_kernel(product_args P) {
     constexpr int PIECES = (S::GA + S::GB) * NP * S::KS;  // 1 KB blocks of a stage
@@ -941,56 +944,102 @@ __global__ __launch_bounds__(S::threads, 2) void product_kernel(product_args P) 
                 dma16(src[j], (unsigned)st * stride[j] + lane * 16, dst + j * S::waves * kBlock);
             }
         };
-        auto compute = [&](const char *cur, int c) {
+        // fragments of a stage's step kk of this wave, and their products
+        struct fragments {
+            halfx8 a[NP][TM], b[NP][TN];
+        } frag[2];
+        auto read = [&](const char *cur, int kk, fragments &f) {
+            const int o = (kk * S::WK + wk) * NP * kBlock + lane * 16;
 #pragma unroll
-            for (int kk = 0; kk < KS; kk += S::WK) {
-                if (KS > 2 && (st0 + c) * KS + kk + wk >= steps) break;
-                const int o = (kk + wk) * NP * kBlock + lane * 16;
-                halfx8 af[NP][TM], bf[NP][TN];
+            for (int q = 0; q < NP; ++q) {
 #pragma unroll
-                for (int q = 0; q < NP; ++q) {
+                for (int a = 0; a < TM; ++a)
+                    f.a[q][a] = *reinterpret_cast<const halfx8 *>(cur + (wgm + a) * (NP * KS * kBlock) + o + q * kBlock);
 #pragma unroll
-                    for (int a = 0; a < TM; ++a)
-                        af[q][a] = *reinterpret_cast<const halfx8 *>(cur + (wgm + a) * (NP * KS * kBlock) + o + q * kBlock);
-#pragma unroll
-                    for (int b = 0; b < TN; ++b)
-                        bf[q][b] =
-                            *reinterpret_cast<const halfx8 *>(cur + (GA + wgn + b) * (NP * KS * kBlock) + o + q * kBlock);
-                }
-                auto term = [&](floatx16(&d)[TM][TN], int qa, int qb) {
-#pragma unroll
-                    for (int a = 0; a < TM; ++a)
-#pragma unroll
-                        for (int b = 0; b < TN; ++b)
-                            d[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(af[qa][a], bf[qb][b], d[a][b], 0, 0, 0);
-                };
-                term(acc, 0, 0);
-                if constexpr (TWO) {
-                    term(small, 1, 0);
-                    term(small, 0, 1);
-                }
+                for (int b = 0; b < TN; ++b)
+                    f.b[q][b] = *reinterpret_cast<const halfx8 *>(cur + (GA + wgn + b) * (NP * KS * kBlock) + o + q * kBlock);
             }
         };
-        // stage c: its blocks have landed everywhere (the loads of stage c + 1 may
-        // still be out), and the buffer that the loads of stage c + 2 fill was
-        // last read in stage c - 1, whose reads every wave has finished here
-        auto stage = [&](int c, const char *cur, unsigned nxt2) {
-            if (c + 1 < stages)
-                wait_vm<LPW>();
-            else
-                wait_vm<0>();
-            asm volatile("" ::: "memory");
+        auto multiply = [&](const fragments &f) {
+            auto term = [&](floatx16(&d)[TM][TN], int qa, int qb) {
+#pragma unroll
+                for (int a = 0; a < TM; ++a)
+#pragma unroll
+                    for (int b = 0; b < TN; ++b)
+                        d[a][b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f.a[qa][a], f.b[qb][b], d[a][b], 0, 0, 0);
+            };
+            term(acc, 0, 0);
+            if constexpr (TWO) {
+                term(small, 1, 0);
+                term(small, 0, 1);
+            }
+        };
+        auto together = [&] {  // (wait_vm waits for the reads from LDS too)
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
-            if (c + 2 < stages) load(nxt2, c + 2);
-            compute(cur, c);
+        };
+        constexpr int H = KS / S::WK;  // steps of a stage that a wave takes
+        // Stage c, its first fragments in frag[first]: the next ones are read while these are multiplied.  Before
+        // those of stage c + 1: its blocks have landed everywhere (the loads of stage c + 2 may still be
+        // out), and every wave has its last fragments of stage c, whose buffer then takes stage c + 3.
+        // `inner`: stage c + 3 is known to exist (a loop without conditions, whose waits the compiler can count).
+        auto stage = [&](auto inner, int c, const char *cur, const char *next, unsigned here, int first) {
+#pragma unroll
+            for (int kk = 0; kk < H; ++kk) {
+                const fragments &now = frag[(first + kk) & 1];
+                fragments &then = frag[(first + kk + 1) & 1];
+                if (kk + 1 < H) {
+                    read(cur, kk + 1, then);
+                } else if constexpr (inner.value) {
+                    wait_vm<LPW>();
+                    together();
+                    load(here, c + 3);
+                    read(next, 0, then);
+                } else {
+                    if (c + 2 < stages)
+                        wait_vm<LPW>();
+                    else
+                        wait_vm<0>();
+                    if (c + 1 < stages) {
+                        together();
+                        if (c + 3 < stages) load(here, c + 3);
+                        read(next, 0, then);
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);  // (or the reads sink to where their values are used)
+                // (steps are even in number: only the last of more than two a stage can end inside one)
+                if (inner.value || KS <= 2 || (st0 + c) * KS + kk * S::WK + wk < steps) multiply(now);
+                __builtin_amdgcn_sched_barrier(0);
+            }
         };
         load(l0, 0);
         if (stages > 1) load(l1, 1);
-        for (int c = 0; c < stages; c += 3) {
-            stage(c, S0, l2);
-            if (c + 1 < stages) stage(c + 1, S1, l0);
-            if (c + 2 < stages) stage(c + 2, S2, l1);
+        if (stages > 2) load(l2, 2);
+        if (stages > 2)
+            wait_vm<2 * LPW>();
+        else if (stages > 1)
+            wait_vm<LPW>();
+        else
+            wait_vm<0>();
+        together();
+        read(S0, 0, frag[0]);
+        constexpr int odd = H & 1;  // the set that the next stage begins with is the other one
+        int c = 0;
+        for (const std::true_type inner; c + 8 < stages; c += 6) {
+            stage(inner, c, S0, S1, l0, 0);
+            stage(inner, c + 1, S1, S2, l1, odd);
+            stage(inner, c + 2, S2, S0, l2, 0);
+            stage(inner, c + 3, S0, S1, l0, odd);
+            stage(inner, c + 4, S1, S2, l1, 0);
+            stage(inner, c + 5, S2, S0, l2, odd);
+        }
+        for (const std::false_type inner; c < stages; c += 6) {
+            stage(inner, c, S0, S1, l0, 0);
+            if (c + 1 < stages) stage(inner, c + 1, S1, S2, l1, odd);
+            if (c + 2 < stages) stage(inner, c + 2, S2, S0, l2, 0);
+            if (c + 3 < stages) stage(inner, c + 3, S0, S1, l0, odd);
+            if (c + 4 < stages) stage(inner, c + 4, S1, S2, l1, 0);
+            if (c + 5 < stages) stage(inner, c + 5, S2, S0, l2, odd);
         }
         if constexpr (TWO)
 #pragma unroll
@@ -1039,8 +1088,10 @@ __global__ __launch_bounds__(S::threads, 2) void product_kernel(product_args P) 
         // two positions in each of two buffers that every wave has read its last
         // fragments from (behind the barrier in front of the shared sums, if there are any)
         if constexpr (S::WK == 1) __syncthreads();
-        static_assert(S::WM * S::WN <= 4 && 2 * kTurned * 4 <= SB, "room for the turned blocks");
-        buf = reinterpret_cast<float *>(S::WK > 1 ? (wp < 2 ? S1 : S2) : (wp < 2 ? S0 : S1)) + (wp & 1) * kTurned;
+        constexpr int each = S::WM * S::WN / 2;
+        static_assert(each * kTurned * 4 <= SB, "room for the turned blocks");
+        const int second = wp / each;
+        buf = reinterpret_cast<float *>(S::WK > 1 ? (second ? S2 : S1) : (second ? S1 : S0)) + (wp - second * each) * kTurned;
     }
 #pragma unroll
     for (int a = 0; a < TM; ++a)
@@ -1081,11 +1132,11 @@ __global__ __launch_bounds__(256) void join_kernel(product_args P) {
 }
 
 // Large products: 128 x 128 tiles.  Products of fewer tiles: 128 x 64, or 64 x 64 with two waves a
-// position and four steps between two barriers.
+// position and four steps between two barriers.  One part, where they fill the CUs: 256 x 256, of eight waves.
 template <int NP>
 using large_tile = tile_shape<2, 2, 2, 2, 1, NP == 2 ? 1 : 2>;
-template <int NP>
-using medium_tile = tile_shape<2, 1, 2, 2, 1, NP == 2 ? 2 : 4>;
+using medium_tile = tile_shape<2, 1, 2, 2, 1, 2>;
+using huge_tile = tile_shape<2, 4, 4, 2, 1, 2>;
 using small_tile = tile_shape<1, 1, 2, 2, 2, 4>;
 
 template <typename S>
@@ -1126,17 +1177,24 @@ hipError_t launch_tiles(product_args P, int most, int least, hipStream_t s) {
     return hipGetLastError();
 }
 
-// By the number of large tiles.  us for five steps, symmetric and other products both with small,
-// medium and large tiles, two parts: 700 x 700 166, 237, 352; 1001 x 1777 268, 347, 539; 1500 x 1500 515, 456, 616;
-// 2048 x 2048 968, 752, 823; 2500 x 2500 (symmetric ones medium, 210 large tiles, the others
-// large, 400) 1159, all large 1204; 3500 x 3500 3920, 3075, 2858.  One part: 1001 x 1777 173, 229, 314; 1500 x 1500
-// 250, 261, 334; 2048 x 2048 440, 387, 444; 4096 x 4096 2255, 2071, 1839.  Cut tiles: large 4096 x 4096 4254 -> 3781
-// (528 symmetric tiles: 16 past the second round), 3500 x 3500 2858 -> 2710.
+// By the number of large tiles.  us for five steps, every product with small, medium and large tiles, two parts:
+// 700 x 700 159, 217, 324; 1001 x 1777 242, 328, 353; 1500 x 1500 485, 438, 457; 2048 x 2048 895, 725, 754; 2500 x 2500 1472,
+// 1177, 1124 (and 1150 as chosen: the symmetric ones, 210 large tiles, medium); 3500 x 3500 3410, 2765, 2586.  One
+// part: 1001 x 1777 172, 225, 260; 1500 x 1500 247, 256, 305 (as chosen 238); 2048 x 2048 461, 369, 405 (as chosen 380);
+// 4096 x 4096 2240, 1840, 1600, with huge tiles for the product with X 1556; 4096 x 16384 large 5255, huge 4900, 8192 x
+// 8192 11900, 10890; not where they leave a tenth of the CUs idle (576 tiles: 4096 x 9216, where both take 3160).  With
+// two parts, or four waves of 128 x 128, they were slower.  Cut tiles: 4096 x 4096 4070 -> 3645 (528 symmetric
+// tiles: 16 past the second round), 3500 x 3500 2720 -> 2580, 2048 x 2048 (272 medium) 742 -> 718; one part's medium tiles
+// only where more is saved (2048 x 2048 366 -> 412).
 template <int NP, typename O>
 hipError_t launch_product(product_args P, hipStream_t s) {
+    if constexpr (NP == 1) {
+        count_tiles<huge_tile>(P);
+        if (!P.symmetric && P.tiles * 10 >= ceil_div(P.tiles, kCus) * kCus * 9) return launch_tiles<NP, huge_tile, O>(P, 1, 0, s);
+    }
     count_tiles<large_tile<NP>>(P);
     if (P.tiles >= kCus) return launch_tiles<NP, large_tile<NP>, O>(P, 4, 40, s);
-    if (P.tiles >= kCus / 4) return launch_tiles<NP, medium_tile<NP>, O>(P, 4, 100, s);
+    if (P.tiles >= kCus / (NP == 2 ? 4 : 2)) return launch_tiles<NP, medium_tile, O>(P, 4, NP == 2 ? 40 : 100, s);
     return launch_tiles<NP, small_tile, O>(P, 32, 24, s);
 }
 
@@ -1188,9 +1246,9 @@ int norm_blocks(const muon_args &a) {
 
 // Steps between two products with X: the m x m products that stand for them pay where X is
 // wider than square and they are not bound by their launches.  us, one step and three, two parts:
-// 512 x 512 137 and 157, 300 x 784 128 and 133, 200 x 2000 128 and 127, 400 x 2000 174 and 164, 512 x 4096 219 and 188,
-// 200 x 9216 193 and 152; 600 x 2000 219 and 194, 1001 x 1777 271 and 261, 2048 x 2048 867 and 987, 2048 x 4096 1230 and
-// 1146, 4096 x 9216 7181 and 5366.
+// 512 x 512 141 and 161, 300 x 784 128 and 134, 200 x 2000 136 and 129, 400 x 2000 175 and 164, 512 x 4096 219 and 192,
+// 200 x 9216 196 and 155; 600 x 2000 199 and 182, 1001 x 1777 247 and 235, 2048 x 2048 717 and 780, 2048 x 4096 1068 and
+// 931, 4096 x 9216 6750 and 4960.
 int most_steps(int m, int n) {
     return 2 * (int64_t)n >= 3 * (int64_t)m && (m > 512 || n >= 5 * (int64_t)m) ? kMaxGroup : 1;
 }
