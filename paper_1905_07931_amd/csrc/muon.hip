@@ -806,30 +806,34 @@ constexpr int kTurned = 32 * 33;  // floats of a turned block
 // The epilogue of a 32 x 32 block.  Lane l, register 4 q + e holds row 8 q + 4 (l / 32) + e,
 // column l % 32: four consecutive indices of a packed row j (8 bytes a part), so
 // the matrix packed by rows j is stored from the registers, the one by rows i through LDS.
+struct operand_e {  // E of a block, as stored
+    halfx4 hi[4], lo[4];
+    __device__ __forceinline__ operand_e(const product_args &P, int gi, int gj, int lane) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            hi[q] = lo[q] = halfx4{};
+            if (P.E.data == nullptr) continue;
+            const char *p = P.E.data + ((int64_t)gj * P.E.steps + 2 * gi + (q >> 1)) * (P.E.parts * kBlock) +
+                            ((lane & 31) + 32 * (q & 1)) * 16 + 8 * (lane >> 5);
+            hi[q] = *reinterpret_cast<const halfx4 *>(p);
+            if (P.E.parts == 2) lo[q] = *reinterpret_cast<const halfx4 *>(p + kBlock);
+        }
+    }
+};
+
 template <typename O>
 __device__ __forceinline__ void finish_block(const product_args &P, int gi, int gj, int lane, const floatx16 &acc,
-                                             float *buf) {
-    if (gi >= P.A.groups || gj >= P.B.groups || (P.symmetric && gi > gj)) return;
+                                             const operand_e &E, float *buf) {
     const float dev = P.dev ? *P.dev : 1.f;
     const int l = lane & 31, h = lane >> 5;
     const int i0 = gi * kGroup, j = gj * kGroup + l;
     float v[16];
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-        float e4[4] = {0.f, 0.f, 0.f, 0.f};
-        if (P.E.data) {
-            const char *p = P.E.data + ((int64_t)gj * P.E.steps + 2 * gi + (q >> 1)) * (P.E.parts * kBlock) +
-                            (l + 32 * (q & 1)) * 16 + 8 * h;
-            const halfx4 hi = *reinterpret_cast<const halfx4 *>(p);
-            halfx4 lo = {};
-            if (P.E.parts == 2) lo = *reinterpret_cast<const halfx4 *>(p + kBlock);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) e4[e] = (float)hi[e] + (float)lo[e];
-        }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int i = i0 + 8 * q + 4 * h + e;
-            float x = dev * fmaf(P.al, acc[4 * q + e], P.be * e4[e]);
+            float x = dev * fmaf(P.al, acc[4 * q + e], P.be * ((float)E.hi[q][e] + (float)E.lo[q][e]));
             if (i == j && i < P.rows) x += P.ga;
             v[4 * q + e] = x;
         }
@@ -872,6 +876,14 @@ __device__ __forceinline__ void finish_block(const product_args &P, int gi, int 
         if (o.parts == 2) *reinterpret_cast<halfx8 *>(d + s * (o.parts * kBlock) + kBlock) = p.lo;
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+}
+
+// (not past the operands, nor below a symmetric result's diagonal)
+template <typename O>
+__device__ __forceinline__ void finish_block(const product_args &P, int gi, int gj, int lane, const floatx16 &acc,
+                                             float *buf) {
+    if (gi >= P.A.groups || gj >= P.B.groups || (P.symmetric && gi > gj)) return;
+    finish_block<O>(P, gi, gj, lane, acc, operand_e(P, gi, gj, lane), buf);
 }
 
 // One tile, or one range of its reduction.  Stages of packed blocks are copied straight into LDS, up to
@@ -1099,6 +1111,70 @@ __global__ __launch_bounds__(S::threads, 2) void product_kernel(product_args P) 
         for (int b = 0; b < TN; ++b) finish_block<O>(P, tm * GA + wgm + a, tn * GB + wgn + b, lane, acc[a][b], buf);
 }
 
+// A product of few blocks: a workgroup a 32 x 32 block, its 16 waves sharing the reduction, fragments straight from
+// memory (a step of them is a wave's 1 KB a part), U steps in flight.  Bound by latency: the launch, the operands
+// (which other XCDs' workgroups stored), the sums of the waves and the epilogue, 5-6 us at 300 x 784.
+constexpr int kBlockWaves = 16, kMostBlocks = 512, kMostBlockSteps = 256;
+
+template <int NP, typename O>
+__global__ __launch_bounds__(kBlockWaves *kWave) void block_kernel(product_args P) {
+    constexpr int waves = kBlockWaves, U = 4;
+    __shared__ float sums[waves][16 * kWave];
+    __shared__ float turned[kTurned];
+    const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63, steps = P.A.steps;
+    int gi, gj;
+    if (P.symmetric) {  // blocks gi <= gj by columns
+        gj = (int)((sqrtf(8.f * blockIdx.x + 1.f) - 1.f) * 0.5f);
+        while (gj * (gj + 1) / 2 > (int)blockIdx.x) --gj;
+        while ((gj + 1) * (gj + 2) / 2 <= (int)blockIdx.x) ++gj;
+        gi = blockIdx.x - gj * (gj + 1) / 2;
+    } else {
+        gj = blockIdx.x / P.A.groups;
+        gi = blockIdx.x - gj * P.A.groups;
+    }
+    gi = uniform(gi);
+    gj = uniform(gj);
+    const char *pa = P.A.data + (int64_t)gi * steps * (P.A.parts * kBlock) + lane * 16;
+    const char *pb = P.B.data + (int64_t)gj * steps * (P.B.parts * kBlock) + lane * 16;
+    floatx16 acc = {}, small = {};
+    for (int s0 = wave; s0 < steps; s0 += waves * U) {
+        halfx8 a[U][NP], b[U][NP];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int st = min(s0 + u * waves, steps - 1);  // (past the end the last again, not used)
+#pragma unroll
+            for (int q = 0; q < NP; ++q) {
+                a[u][q] = *reinterpret_cast<const halfx8 *>(pa + (int64_t)st * (P.A.parts * kBlock) + q * kBlock);
+                b[u][q] = *reinterpret_cast<const halfx8 *>(pb + (int64_t)st * (P.B.parts * kBlock) + q * kBlock);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (s0 + u * waves >= steps) break;
+            acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[u][0], b[u][0], acc, 0, 0, 0);
+            if constexpr (NP == 2) {
+                small = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[u][1], b[u][0], small, 0, 0, 0);
+                small = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[u][0], b[u][1], small, 0, 0, 0);
+            }
+        }
+    }
+    if constexpr (NP == 2) acc += small;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) sums[wave][r * kWave + lane] = acc[r];
+    const operand_e E(P, gi, gj, lane);  // (for the first wave: ahead of the wait)
+    __syncthreads();
+    static_assert(waves == 16, "a wave a register");
+    float t = 0.f;
+#pragma unroll
+    for (int w = 0; w < waves; ++w) t += sums[w][wave * kWave + lane];
+    sums[0][wave * kWave + lane] = t;  // (read by this wave alone)
+    __syncthreads();
+    if (wave > 0) return;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[r] = sums[0][r * kWave + lane];
+    finish_block<O>(P, gi, gj, lane, acc, E, turned);
+}
+
 // The blocks of the tiles that were cut: a wave adds the ranges of a 32 x 32 block and finishes it.
 template <typename S, typename O>
 __global__ __launch_bounds__(256) void join_kernel(product_args P) {
@@ -1177,7 +1253,11 @@ hipError_t launch_tiles(product_args P, int most, int least, hipStream_t s) {
     return hipGetLastError();
 }
 
-// By the number of large tiles.  us for five steps, every product with small, medium and large tiles, two parts:
+// Few blocks take a workgroup each: us for five steps with small tiles and with blocks, two parts 300 x 784 125 and 102,
+// 512 x 512 137 and 109, 700 x 700 (484 blocks and 253) 155 and 126; up to 800 blocks 850 x 850 162 -> 188; one part
+// 300 x 784 102 and 83, 700 x 700 119 and 107.  A long reduction wants more workgroups, ranges of small tiles:
+// 200 x 9216 (28 blocks of 576 steps) 137 and 160, but 300 x 4096 bf16 (256 steps) 136 and 126.
+// The others by the number of large tiles.  us for five steps, every product with small, medium and large tiles, two parts:
 // 700 x 700 159, 217, 324; 1001 x 1777 242, 328, 353; 1500 x 1500 485, 438, 457; 2048 x 2048 895, 725, 754; 2500 x 2500 1472,
 // 1177, 1124 (and 1150 as chosen: the symmetric ones, 210 large tiles, medium); 3500 x 3500 3410, 2765, 2586.  One
 // part: 1001 x 1777 172, 225, 260; 1500 x 1500 247, 256, 305 (as chosen 238); 2048 x 2048 461, 369, 405 (as chosen 380);
@@ -1191,6 +1271,11 @@ hipError_t launch_product(product_args P, hipStream_t s) {
     if constexpr (NP == 1) {
         count_tiles<huge_tile>(P);
         if (!P.symmetric && P.tiles * 10 >= ceil_div(P.tiles, kCus) * kCus * 9) return launch_tiles<NP, huge_tile, O>(P, 1, 0, s);
+    }
+    const int64_t blocks = P.symmetric ? (int64_t)P.A.groups * (P.A.groups + 1) / 2 : (int64_t)P.A.groups * P.B.groups;
+    if (blocks <= kMostBlocks && P.A.steps <= kMostBlockSteps) {
+        block_kernel<NP, O><<<(unsigned)blocks, kBlockWaves * kWave, 0, s>>>(P);
+        return hipGetLastError();
     }
     count_tiles<large_tile<NP>>(P);
     if (P.tiles >= kCus) return launch_tiles<NP, large_tile<NP>, O>(P, 4, 40, s);
@@ -1246,11 +1331,11 @@ int norm_blocks(const muon_args &a) {
 
 // Steps between two products with X: the m x m products that stand for them pay where X is
 // wider than square and they are not bound by their launches.  us, one step and three, two parts:
-// 512 x 512 141 and 161, 300 x 784 128 and 134, 200 x 2000 136 and 129, 400 x 2000 175 and 164, 512 x 4096 219 and 192,
-// 200 x 9216 196 and 155; 600 x 2000 199 and 182, 1001 x 1777 247 and 235, 2048 x 2048 717 and 780, 2048 x 4096 1068 and
-// 931, 4096 x 9216 6750 and 4960.
+// 512 x 512 110 and 117, 300 x 784 101 and 108, 500 x 1500 131 and 129, 300 x 1200 118 and 111, 150 x 1000 93 and 95,
+// 200 x 2000 128 and 112, 400 x 2000 152 and 129, 512 x 4096 196 and 157, 200 x 9216 188 and 137; 600 x 2000 161 and 148,
+// 1001 x 1777 237 and 233, 2048 x 2048 699 and 779, 2048 x 4096 1053 and 929, 4096 x 9216 6877 and 5095.
 int most_steps(int m, int n) {
-    return 2 * (int64_t)n >= 3 * (int64_t)m && (m > 512 || n >= 5 * (int64_t)m) ? kMaxGroup : 1;
+    return 2 * (int64_t)n >= 3 * (int64_t)m && (m > 512 || n >= 3 * (int64_t)m) ? kMaxGroup : 1;
 }
 
 template <typename T, int g>

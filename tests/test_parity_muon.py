@@ -89,6 +89,15 @@ def test_orthogonalize_large(N, K):
     assert rel(L1.orthogonalize(G, precision=L1.F16), want) <= 4.9e-3
 
 
+@pytest.mark.parametrize("precision", [L1.F32, L1.F16])
+@pytest.mark.parametrize("N,K", [(4001, 4090), (4090, 3900), (161, 4100), (161, 4090), (340, 331), (500, 4000), (705, 690), (737, 700),
+                                 (2050, 2047)])
+def test_orthogonalize_on_either_side_of_the_tile_rules(N, K, precision):
+    G = gradient(N, K, 4)
+    want = steps_of(G)
+    assert rel(L1.orthogonalize(G, precision=precision), want) <= (4.9e-3 if precision == L1.F16 else bound(G, want))
+
+
 @pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
 @pytest.mark.parametrize("N,K", [(1, 1), (1, 5), (33, 65), (100, 300), (129, 200), (784, 300), (600, 2000), (1001, 1777), (1500, 1500),
                                  (2100, 2100)])
