@@ -619,7 +619,7 @@ int l1csr_softmax_xent(int32_t C, int32_t B, const float *logits, int64_t ld,
  * A zero U gives zeros; a NaN or an infinity anywhere in U gives NaN everywhere,
  * as the formula does.  N * K < 2^31 and N, K <= 2^22 (L1CSR_EUNSUPPORTED;
  * l1csr_workspace_bytes gives 0).  Results are reproducible.
- * ws as l1csr_workspace_bytes(L1CSR_OP_MUON or L1CSR_OP_MUON_F16, N, K, 0, 0).
+ * ws, 16-byte aligned, as l1csr_workspace_bytes(L1CSR_OP_MUON or L1CSR_OP_MUON_F16, N, K, 0, 0).
  */
 #define L1CSR_MUON_MAX_STEPS 32
 int muon_update(int32_t N, int32_t K, int dtype, const void *G, int64_t ldg, const float *M, int64_t ldm,
@@ -639,8 +639,8 @@ int muon_update(int32_t N, int32_t K, int dtype, const void *G, int64_t ldg, con
  * same leading dimension), but may not overlap them otherwise, and no other output may
  * overlap an input or an output (L1CSR_EINVAL).  C, B <= 2^30 and pairs < 2^24
  * (L1CSR_EUNSUPPORTED; l1csr_workspace_bytes gives 0).
- * ws as l1csr_workspace_bytes(L1CSR_OP_TOKEN_LOSS, C, pairs, 0, B), pairs = 0 but
- * for the preference loss.
+ * ws, 16-byte aligned, as l1csr_workspace_bytes(L1CSR_OP_TOKEN_LOSS, C, pairs, 0, B),
+ * pairs = 0 but for the preference loss.
  *
  * l1csr_token_logp: logp[b] = lp_b (weights do not apply).
  *

@@ -123,7 +123,7 @@ int token_check(const token_loss_args &a, int n_out, size_t ws_bytes, const void
             if (!(i == 3 && j == all - 1) && bytes_overlap(mem[i].p, mem[i].n, mem[j].p, mem[j].n))
                 return L1CSR_EINVAL;
     const size_t need = token_loss_workspace_bytes(a.C, a.B, a.pairs);
-    if (need > 0 && (ws == nullptr || ws_bytes < need)) return L1CSR_EINVAL;
+    if (need > 0 && (ws == nullptr || ws_bytes < need || !aligned16(ws))) return L1CSR_EINVAL;
     return L1CSR_OK;
 }
 
@@ -949,7 +949,7 @@ int muon_update(int32_t N, int32_t K, int dtype, const void *G, int64_t ldg, con
         return L1CSR_EINVAL;
     const int parts = precision == L1CSR_F32 ? 2 : 1;
     const size_t need = muon_workspace_bytes(N, K, parts);
-    if (need > 0 && (ws == nullptr || ws_bytes < need)) return L1CSR_EINVAL;
+    if (need > 0 && (ws == nullptr || ws_bytes < need || !aligned16(ws))) return L1CSR_EINVAL;
     muon_args a{};
     a.N = N; a.K = K; a.dtype = dtype;
     a.G = G; a.ldg = ldg;

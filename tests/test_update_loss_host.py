@@ -128,6 +128,16 @@ def test_sizes_past_the_kernels_numbers_are_refused(lib):
                 ws_bytes=0) == EUNSUPPORTED
 
 
+@pytest.mark.skipif(not NO_GPU, reason="validation calls use placeholder pointers; run without a GPU")
+def test_misaligned_workspaces_are_refused(lib):
+    odd = C.c_void_p((1 << 36) + 8)
+    far = dict(dz=C.c_void_p(1 << 40))
+    assert muon(lib, ws=odd) == EINVAL
+    assert policy(lib, stats=C.c_void_p(1 << 41), ws=odd, **far) == EINVAL
+    assert preference(lib, loss=C.c_void_p(1 << 41), ws=odd, **far) == EINVAL
+    assert lib.l1csr_token_logp(8, 8, 0, P, 8, Q, R, odd, BIG, None) == EINVAL
+
+
 def test_binding_refuses_host_tensors_and_wrong_shapes():
     torch = pytest.importorskip("torch")
     import paper_1905_07931_amd as L1
