@@ -1003,11 +1003,13 @@ __global__ __launch_bounds__(S::threads, 2) void product_kernel(product_args P) 
                 if (kk + 1 < H) {
                     read(cur, kk + 1, then);
                 } else if constexpr (inner.value) {
+                    asm volatile("" ::: "memory");  // no read moves behind the wait
                     wait_vm<LPW>();
                     together();
                     load(here, c + 3);
                     read(next, 0, then);
                 } else {
+                    asm volatile("" ::: "memory");
                     if (c + 2 < stages)
                         wait_vm<LPW>();
                     else
