@@ -394,6 +394,19 @@ def test_captured_step(schedule):
             assert torch.equal(x, y), rep
 
 
+@pytest.mark.parametrize("N,K", [(0, 5), (5, 0), (0, 0)])
+def test_empty_layers(N, K):
+    torch = _torch()
+    G = torch.empty((N, K), device="cuda")
+    assert L1.orthogonalize(G).shape == (N, K)
+    W = L1.CSR(N, K, torch.zeros(N + 1, dtype=torch.int32, device="cuda"), torch.empty(0, dtype=torch.int32, device="cuda"),
+               torch.empty(0, device="cuda"), 0)
+    st = L1.MuonState.zeros((N, K), "cuda")
+    assert L1.prox_muon_step(W, G, st, 0.1, 0.1).shape == (N, K)
+    out = L1.prox_muon_recompress(W, G, st, 0.1, 0.1)
+    assert out.host_nnz() == 0 and not out.row_ptr.any()
+
+
 def test_refused_steps_leave_the_momentum():
     torch = _torch()
     W, _ = _layer(20, 30, 0.5, 1)
