@@ -159,15 +159,15 @@ struct parts_of {
     }
 };
 
-// 2^-e |U|_F in [1/2, 1) and s = 1 / (2^-e (|U|_F + eps))
+// 2^-e |U|_F in [1/2, 1) and s = 1 / (2^-e (|U|_F + eps)), at most 2.  U = 0: s = 0, not 1 / eps, whose square, taken
+// in float, would be infinite below eps = 5.4e-20 and NaN times the zero Gram matrix.
 struct norm_scale {
     int e = 0;
     float s;
     __device__ __forceinline__ norm_scale(double norm, float eps) {
         if (norm < INFINITY) {
             (void)frexp(norm, &e);
-            const double d = ldexp(norm + (double)eps, -e);
-            s = d > 0 ? (float)(1 / d) : 0.f;
+            s = norm > 0 ? (float)(1 / ldexp(norm + (double)eps, -e)) : 0.f;
         } else {
             s = NAN;  // an infinity or a NaN in U, or a norm past double: nothing to give
         }

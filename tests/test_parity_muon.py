@@ -465,3 +465,30 @@ def test_refusals():
         L1.prox_muon_step(W, G, L1.MuonState.zeros((20, 30), "cuda", mu=1.0), 0.1, 0.1)
     with pytest.raises(L1.L1CSRError):  # the momentum is the gradient
         L1.prox_muon_step(W, G, L1.MuonState(G), 0.1, 0.1)
+
+
+# every form of the products: one workgroup, a step a launch (few ranges, ranges summed ahead), blocks, groups of steps, tiles
+FORMS = [(20, 30), (96, 128), (40, 300), (100, 300), (100, 5000), (300, 784), (700, 300), (600, 2000), (1100, 1100)]
+
+
+@pytest.mark.parametrize("precision", [L1.F32, L1.F16])
+@pytest.mark.parametrize("N,K", FORMS)
+def test_zero_update_whatever_eps_is(N, K, precision):
+    # U = 0 gives X = 0 / (0 + eps): zeros, also where 1 / eps^2 or 1 / eps is past the largest float
+    torch = _torch()
+    Z = torch.zeros((N, K), device="cuda")
+    for eps in (0.0, 2.0 ** -149, 1e-40, 1e-20, 1e-7, 1.0, 3e38):
+        assert not bool(L1.orthogonalize(Z, eps=eps, precision=precision).any()), eps
+
+
+@pytest.mark.parametrize("N,K", [(20, 30), (100, 300), (300, 400)])
+def test_zero_update_leaves_the_prox_step_alone(N, K):
+    # neither a gradient nor momentum: Z = S(W)
+    torch = _torch()
+    W, _ = _layer(N, K, 0.3, 2)
+    G = torch.zeros((N, K), device="cuda")
+    st = L1.MuonState.zeros((N, K), "cuda", eps=1e-20)
+    want = L1.prox_l1_step(L1.PROX_DENSE, W, G, 0.02, 0.1)
+    assert torch.equal(L1.prox_muon_step(W, G, st, 0.02, 0.1), want) and not bool(st.m.any())
+    out = L1.prox_muon_recompress(W, G, st, 0.02, 0.1)
+    assert all(bits_equal(x, y) for x, y in zip(out.to_host(), L1.csr_recompress(want).to_host()))
