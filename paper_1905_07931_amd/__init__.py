@@ -366,12 +366,6 @@ def _vec_of(t, dtype, n, index, name, what):
     return _same_device(index, t, name)
 
 
-def _own_workspace(nbytes, device, stream):
-    """_workspace for the calls below it: under capture the buffer is the call's own (from the graph's pool), so two
-    graphs captured on one stream may be replayed side by side."""
-    return _workspace(nbytes, device, stream, keep=not _torch().cuda.is_current_stream_capturing())
-
-
 def _new(shape, dtype, device, stream):
     """An output of a call, allocated in the order of the stream that the call runs on."""
     torch = _torch()
@@ -396,12 +390,17 @@ def _empty_bytes(nbytes, device, stream):
 def _workspace(nbytes, device, stream=None, least=None, keep=True):
     """Scratch for one call, cached per (device, stream the call runs on): calls
     on one stream run in order and may share it, calls on two streams never do.
-    Beyond _WS_KEEP bytes, or without `keep`, the buffer is the call's own and
-    goes back to the caching allocator behind it.  A call that can do with
+    Beyond _WS_KEEP bytes, without `keep` or while the current stream is being
+    captured, the buffer is the call's own and goes back to the caching allocator
+    behind it (to the graph's memory pool under capture: a graph shares its scratch
+    neither with eager calls nor with another graph that is replayed beside it, and
+    keeps it when a later call needs a larger buffer).  A call that can do with
     `least` bytes (its route without the packed operands) gets those where
     memory for `nbytes` is short.  Returns (buffer or None, its bytes)."""
     if nbytes == 0:
         return None, 0
+    if keep and _torch().cuda.is_current_stream_capturing():
+        keep = False
     index = device.index
     key = (index, _raw_stream(index) if stream is None else stream.cuda_stream)
     buf = _ws_cache.get(key) if keep else None
@@ -1240,7 +1239,7 @@ def token_logp(logits, labels, logp=None, stream=None):
     a label outside [0, C) gives 0.  Returns logp (float32 [B])."""
     Cn, B, code, ld, _, _, index = _token_args(logits, labels, None, None, False, stream)
     logp = _result(logp, B, logits, index, "logp", "token (B)", stream)
-    ws, wsb = _own_workspace(workspace_bytes(OP_TOKEN_LOSS, Cn, 0, 0, B), logits.device, stream)
+    ws, wsb = _workspace(workspace_bytes(OP_TOKEN_LOSS, Cn, 0, 0, B), logits.device, stream)
     _check(lib().l1csr_token_logp(Cn, B, code, logits.data_ptr(), ld, labels.data_ptr(), logp.data_ptr(), _p(ws), wsb,
                                   _stream(stream)), "l1csr_token_logp")
     return logp
@@ -1265,7 +1264,7 @@ def policy_loss(logits, labels, old_logp, advantages, ref_logp=None, weights=Non
         _vec_of(ref_logp, f32, B, index, "ref_logp", "token (B)")
     logp = _result(logp, B, logits, index, "logp", "token (B)", stream)
     stats = _result(stats, 4, logits, index, "stats", "statistic (4)", stream)
-    ws, wsb = _own_workspace(workspace_bytes(OP_TOKEN_LOSS, Cn, 0, 0, B), logits.device, stream)
+    ws, wsb = _workspace(workspace_bytes(OP_TOKEN_LOSS, Cn, 0, 0, B), logits.device, stream)
     _check(lib().l1csr_policy_loss(Cn, B, code, logits.data_ptr(), ld, labels.data_ptr(), old_logp.data_ptr(),
                                    advantages.data_ptr(), _p(ref_logp), _p(weights), clip_low, clip_high, kl_coef,
                                    _p(dlogits), ldd, logp.data_ptr(), stats.data_ptr(), _p(ws), wsb, _stream(stream)),
@@ -1293,7 +1292,7 @@ def preference_loss(logits, labels, seq_ptr, ref_logp=None, weights=None, beta=0
         _vec_of(ref_logp, torch.float32, 2 * pairs, index, "ref_logp", "sequence (2 * pairs)")
     rewards = _result(rewards, 2 * pairs, logits, index, "rewards", "sequence (2 * pairs)", stream)
     loss = _result(loss, 1, logits, index, "loss", "call (1)", stream)
-    ws, wsb = _own_workspace(workspace_bytes(OP_TOKEN_LOSS, Cn, pairs, 0, B), logits.device, stream)
+    ws, wsb = _workspace(workspace_bytes(OP_TOKEN_LOSS, Cn, pairs, 0, B), logits.device, stream)
     _check(lib().l1csr_preference_loss(Cn, B, code, logits.data_ptr(), ld, labels.data_ptr(), pairs, seq_ptr.data_ptr(),
                                        _p(ref_logp), _p(weights), beta, label_smoothing, _p(dlogits), ldd,
                                        rewards.data_ptr(), loss.data_ptr(), _p(ws), wsb, _stream(stream)),
@@ -1343,7 +1342,7 @@ def _muon_update(G, O, m, m_out, st, scale, precision, stream):
                 raise ValueError("m_out must be [n_rows][n_cols]")
     if precision != F32 and precision != F16:
         raise ValueError("precision must be F32 or F16")
-    ws, wsb = _own_workspace(workspace_bytes(OP_MUON if precision == F32 else OP_MUON_F16, N, K, 0, 0), G.device, stream)
+    ws, wsb = _workspace(workspace_bytes(OP_MUON if precision == F32 else OP_MUON_F16, N, K, 0, 0), G.device, stream)
     _check(lib().muon_update(N, K, code, G.data_ptr(), ldg, _p(m), ldm, _p(m_out), ldmo, st.mu, 1 if st.nesterov else 0,
                              st.steps, st.eps, scale, precision, O.data_ptr(), ldo, _p(ws), wsb, _stream(stream)),
            "muon_update")

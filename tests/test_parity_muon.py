@@ -492,3 +492,89 @@ def test_zero_update_leaves_the_prox_step_alone(N, K):
     assert torch.equal(L1.prox_muon_step(W, G, st, 0.02, 0.1), want) and not bool(st.m.any())
     out = L1.prox_muon_recompress(W, G, st, 0.02, 0.1)
     assert all(bits_equal(x, y) for x, y in zip(out.to_host(), L1.csr_recompress(want).to_host()))
+
+
+def _full_csr(N, K):
+    torch = _torch()
+    return L1.CSR(N, K, *(torch.empty(n, dtype=t, device="cuda") for n, t in
+                          ((N + 1, torch.int32), (N * K, torch.int32), (N * K, torch.float32))))
+
+
+def test_recompressing_graphs_side_by_side():
+    # two graphs captured on one stream and replayed on two: neither's scratch of the recompression is the other's
+    torch = _torch()
+    N, K = 300, 784
+    W, _ = _layer(N, K, 0.2, 1)
+    graphs, ins, outs = [], [], []
+    for k in range(2):
+        G, m, out = gradient(N, K, k), torch.zeros((N, K), device="cuda"), _full_csr(N, K)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            L1.prox_muon_recompress(W, G, L1.MuonState(m), 0.05, 0.3, out=out)
+        graphs.append(g)
+        ins.append((G, m))
+        outs.append(out)
+    # eager calls that need more scratch replace what the stream keeps
+    W2, _ = _layer(900, 2000, 0.2, 2)
+    big = L1.MuonState.zeros((900, 2000), "cuda")
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for rep in range(3):
+        want = []
+        for i, (G, m) in enumerate(ins):
+            G.copy_(torch.randn_like(G) * (1 + i + rep))
+            m.copy_(torch.randn_like(m))
+            st = L1.MuonState(m.clone())
+            want.append((L1.prox_muon_recompress(W, G, st, 0.05, 0.3, out=_full_csr(N, K)), st.m))
+        L1.prox_muon_recompress(W2, gradient(900, 2000, rep), big, 0.05, 0.3)
+        others = [torch.full((1 << 20,), 7, dtype=torch.uint8, device="cuda") for _ in range(8)]
+        torch.cuda.synchronize()
+        for s, g in zip(streams, graphs):
+            with torch.cuda.stream(s):
+                g.replay()
+        torch.cuda.synchronize()
+        for (ref, m), out, (_, m_got) in zip(want, outs, ins):
+            n = int(ref.row_ptr[-1])
+            assert torch.equal(out.row_ptr, ref.row_ptr) and torch.equal(out.col_idx[:n], ref.col_idx[:n])
+            assert torch.equal(out.vals[:n], ref.vals[:n]) and torch.equal(m_got, m)
+        assert all(bool((o == 7).all()) for o in others)
+
+
+@pytest.mark.parametrize("schedule", ["serial", "two_stream"])
+def test_captured_steps_side_by_side(schedule):
+    torch = _torch()
+    N, K, Bt = 300, 784, 64
+    W, _ = _layer(N, K, 0.1, 4)
+    gen = torch.Generator(device="cuda").manual_seed(6)
+
+    def buffers():
+        return dict(Y=torch.empty((N, Bt), device="cuda"), dX=torch.empty((K, Bt), device="cuda"),
+                    dW=torch.empty((N, K), device="cuda"), csc=L1.CSC.empty(K, W.nnz, "cuda"), out=_full_csr(N, K))
+
+    def results(st, o):
+        n = int(o["out"].row_ptr[-1])
+        return [st.m, o["Y"], o["dX"], o["dW"], o["out"].row_ptr, o["out"].col_idx[:n], o["out"].vals[:n]]
+
+    cases = []
+    for k in range(2):
+        X, dY = (torch.randn((r, Bt), device="cuda", generator=gen) for r in (K, N))
+        st, o = L1.MuonState.zeros((N, K), "cuda"), buffers()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            L1.l1_step(W, X, dY, 0.02, 0.05, schedule=schedule, adaptive=st, **o)
+        cases.append((g, X, dY, st, o))
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for rep in range(3):
+        want = []
+        for g, X, dY, st, o in cases:
+            for x in (X, dY, st.m):
+                x.normal_(generator=gen)
+            ref, ro = L1.MuonState(st.m.clone()), buffers()
+            L1.l1_step(W, X, dY, 0.02, 0.05, schedule=schedule, adaptive=ref, **ro)
+            want.append(results(ref, ro))
+        torch.cuda.synchronize()
+        for s, c in zip(streams, cases):
+            with torch.cuda.stream(s):
+                c[0].replay()
+        torch.cuda.synchronize()
+        for c, w in zip(cases, want):
+            assert all(torch.equal(a, b) for a, b in zip(results(c[3], c[4]), w)), rep

@@ -161,3 +161,23 @@ def test_binding_refuses_host_tensors_and_wrong_shapes():
     for name in ("token_logp", "policy_loss", "preference_loss", "orthogonalize", "MuonState", "prox_muon_step",
                  "prox_muon_recompress", "F16"):
         assert name in L1.__all__ and hasattr(L1, name)
+
+
+def test_workspaces_under_capture_are_not_the_streams(monkeypatch):
+    """Scratch that a captured call uses stays out of the stream's cache, and the cache's buffer out of the graph."""
+    torch = pytest.importorskip("torch")
+    import paper_1905_07931_amd as L1
+    capturing = [False]
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: capturing[0])
+    monkeypatch.setattr(L1, "_raw_stream", lambda index: 0)
+    monkeypatch.setattr(L1, "_empty_bytes", lambda n, device, stream: torch.empty(n, dtype=torch.uint8))
+    monkeypatch.setattr(L1, "_ws_cache", {})
+    dev = torch.device("cuda", 0)
+    eager, n = L1._workspace(1000, dev)
+    assert n == 1000 and L1._workspace(500, dev)[0] is eager
+    capturing[0] = True
+    first, second = L1._workspace(500, dev)[0], L1._workspace(2000, dev)[0]
+    assert first is not eager and first.numel() == 500 and second.numel() == 2000
+    assert list(L1._ws_cache.values()) == [eager]
+    capturing[0] = False
+    assert L1._workspace(1000, dev)[0] is eager
