@@ -1383,10 +1383,33 @@ def _muon_args(W, G, st, eta, lam):
 
 def _span(t):
     """Bytes [first, past the last) that a tensor's elements lie in."""
-    if t.numel() == 0:
+    if not isinstance(t, _torch().Tensor):
+        raise TypeError(f"a torch.Tensor is needed (got {type(t).__name__})")
+    n = t.numel()
+    if n == 0:
         return 0, 0
     p = t.data_ptr()
+    if t.is_contiguous():
+        return p, p + t.element_size() * n
     return p, p + t.element_size() * (1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride())))
+
+
+def _apart(written, others, what):
+    """Refuses tensors that a call writes (spans) and that share memory with others of the call."""
+    for a0, a1 in written:
+        for b0, b1 in others:
+            if a0 < b1 and b0 < a1:
+                raise ValueError(what)
+
+
+def _muon_writes(W, O, st, m_out=None, row_counts=None):
+    """What the Prox-Muon calls check before the momentum is stored: the prox reads W after the update and the momentum are
+    written, so neither lies in W's arrays; row_counts lies in none of them."""
+    layer = [_span(t) for t in (W.row_ptr, W.col_idx, W.vals)]
+    dense = [_span(t) for t in ((O, st.m) if m_out is None else (O, st.m, m_out))]
+    _apart(dense, layer, "the update or the momentum shares memory with W")
+    if row_counts is not None:
+        _apart([_span(row_counts)], layer + dense, "row_counts shares memory with W, the update or the momentum")
 
 
 def _muon_out(W, out, capacity, index, dense):
@@ -1403,9 +1426,8 @@ def _muon_out(W, out, capacity, index, dense):
         _vec(_same_device(index, t, name), dtype, name)
         outs.append(_span(t))
     ins = [_span(t) for t in (W.row_ptr, W.col_idx, W.vals, *dense)]
-    for i, (a0, a1) in enumerate(outs):
-        if any(a0 < b1 and b0 < a1 for b0, b1 in outs[i + 1:] + ins):
-            raise ValueError("out shares memory with W, the update, the momentum or itself")
+    for i, a in enumerate(outs):
+        _apart([a], outs[i + 1:] + ins, "out shares memory with W, the update, the momentum or itself")
 
 
 def prox_muon_step(W: CSR, G, st: MuonState, eta, lam, Z=None, m_out=None, row_counts=None, precision=F32,
@@ -1419,6 +1441,7 @@ def prox_muon_step(W: CSR, G, st: MuonState, eta, lam, Z=None, m_out=None, row_c
         _vec_of(row_counts, _torch_module.int32, N, G.get_device(), "row_counts", "row (n_rows)")
     if Z is None:
         Z = _new((N, K), _torch().float32, G.device, stream)
+    _muon_writes(W, Z, st, m_out, row_counts)
     _muon_update(G, Z, st.m, st.m if m_out is None else m_out, st, scale, precision, stream)
     return prox_l1_step(PROX_DENSE, W, Z, eta, lam, Z=Z, row_counts=row_counts, stream=stream)
 
@@ -1431,6 +1454,7 @@ def prox_muon_recompress(W: CSR, G, st: MuonState, eta, lam, O=None, capacity=No
     torch = _torch()
     N, K, scale = _muon_args(W, G, st, eta, lam)
     W.validate_shapes()
+    _muon_writes(W, G if O is None else O, st)
     if out is not None:
         _muon_out(W, out, capacity, G.get_device(), (st.m, G if O is None else O))
     cap = capacity if capacity is not None else (N * K if out is None else min(out.col_idx.numel(), out.vals.numel()))

@@ -578,3 +578,27 @@ def test_captured_steps_side_by_side(schedule):
         torch.cuda.synchronize()
         for c, w in zip(cases, want):
             assert all(torch.equal(a, b) for a, b in zip(results(c[3], c[4]), w)), rep
+
+
+def test_steps_that_would_write_into_the_layer_are_refused():
+    torch = _torch()
+    N, K = 20, 30
+    W, _ = _layer(N, K, 1.0, 1)
+    assert W.nnz == N * K
+    keep = [x.clone() for x in (W.row_ptr, W.col_idx, W.vals)]
+    G, m0 = gradient(N, K, 1), gradient(N, K, 2)
+    over = W.vals[:N * K].view(N, K)
+    at = lambda x, n: x.view(torch.int32).view(-1)[:n]  # noqa: E731
+    st = L1.MuonState(m0.clone())
+    Z = torch.empty((N, K), device="cuda")
+    for kw in (dict(Z=over), dict(m_out=over), dict(Z=W.col_idx[:N * K].view(torch.float32).view(N, K)),
+               dict(row_counts=W.row_ptr[:N]), dict(row_counts=W.col_idx[:N]), dict(Z=Z, row_counts=at(Z, N)),
+               dict(row_counts=at(st.m, N))):
+        with pytest.raises(ValueError):
+            L1.prox_muon_step(W, G, st, 0.1, 0.1, **kw)
+    with pytest.raises(ValueError):
+        L1.prox_muon_recompress(W, G, st, 0.1, 0.1, O=over)
+    for f in (L1.prox_muon_step, L1.prox_muon_recompress):
+        with pytest.raises(ValueError):
+            f(W, G, L1.MuonState(over), 0.1, 0.1)
+    assert torch.equal(st.m, m0) and all(torch.equal(a, b) for a, b in zip(keep, (W.row_ptr, W.col_idx, W.vals)))

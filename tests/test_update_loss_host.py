@@ -181,3 +181,29 @@ def test_workspaces_under_capture_are_not_the_streams(monkeypatch):
     assert list(L1._ws_cache.values()) == [eager]
     capturing[0] = False
     assert L1._workspace(1000, dev)[0] is eager
+
+
+def test_prox_muon_refuses_to_write_into_what_it_reads():
+    """The check of the Prox-Muon calls' written tensors against the layer's arrays, on host tensors."""
+    torch = pytest.importorskip("torch")
+    import paper_1905_07931_amd as L1
+    N, K = 4, 6
+    full = lambda: L1.CSR(N, K, torch.arange(0, N * K + 1, K, dtype=torch.int32),  # noqa: E731
+                          torch.arange(K, dtype=torch.int32).repeat(N), torch.ones(N * K), N * K)
+    W, st = full(), L1.MuonState(torch.zeros(N, K))
+    Z, new, counts = torch.zeros(N, K), torch.zeros(N, K), torch.zeros(N, dtype=torch.int32)
+    wide = torch.zeros(N, 2 * K)
+    L1._muon_writes(W, Z, st)
+    L1._muon_writes(W, Z, st, new, counts)
+    L1._muon_writes(W, wide[:, :K], L1.MuonState(wide[:, K:]), new, counts)  # columns of one buffer
+    over = W.vals.view(N, K)
+    cols = W.col_idx.view(torch.float32).view(N, K)
+    bad = [(over, st, None, None), (cols, st, None, None), (Z, L1.MuonState(over), None, None), (Z, st, over, None),
+           (Z, L1.MuonState(over), new, None), (Z, st, None, W.row_ptr[:N]), (Z, st, None, W.col_idx[3:3 + N]),
+           (Z, st, None, Z.view(torch.int32).view(-1)[:N]), (Z, st, None, st.m.view(torch.int32).view(-1)[-N:]),
+           (Z, st, new, st.m.view(torch.int32).view(-1)[:N]), (Z, st, new, new.view(torch.int32).view(-1)[:N])]
+    for O, state, m_out, row_counts in bad:
+        with pytest.raises(ValueError):
+            L1._muon_writes(W, O, state, m_out, row_counts)
+    with pytest.raises(TypeError):
+        L1._muon_writes(W, Z.numpy(), st)
