@@ -894,8 +894,13 @@ def prox_l1_recompress(W: CSR, G, eta, lam, capacity=None, out: CSR | None = Non
                   torch.empty(max(cap, 1), dtype=torch.float32, device=dev), None)
     cap = min(out.col_idx.numel(), out.vals.numel()) if capacity is None else int(capacity)
     ws, wsb = _workspace(workspace_bytes(OP_PROX_RECOMPRESS, N, K, nnz, 0), dev, stream)
+    return _prox_l1_recompress(W, nnz, G, ldg, eta, lam, cap, out, ws, wsb, stream)
+
+
+def _prox_l1_recompress(W, nnz, G, ldg, eta, lam, cap, out, ws, wsb, stream):
+    """The call itself, on checked arguments and memory that is there."""
     need = C.c_int64(-1)
-    _check(lib().prox_l1_recompress(N, K, nnz, _p(W.row_ptr), _p(W.col_idx), _p(W.vals), _p(G), ldg,
+    _check(lib().prox_l1_recompress(W.n_rows, W.n_cols, nnz, _p(W.row_ptr), _p(W.col_idx), _p(W.vals), _p(G), ldg,
                                     float(eta), float(lam), _p(out.row_ptr), _p(out.col_idx),
                                     _p(out.vals), cap, _nnz_dev(out), C.byref(need), _p(ws), wsb,
                                     _stream(stream)), "prox_l1_recompress")
@@ -1317,8 +1322,8 @@ class MuonState:
         return MuonState(torch.zeros(shape, dtype=torch.float32, device=device), **kw)
 
 
-def _muon_update(G, O, m, m_out, st, scale, precision, stream):
-    """muon_update of G [N][K] into O; m None: no momentum."""
+def _muon_update(G, O, m, m_out, st, scale, precision, stream, room=0):
+    """muon_update of G [N][K] into O; m None: no momentum.  Returns the workspace and its size, at least `room` bytes."""
     N, K, ldg, code = _typed_mat(G, "G")
     index = _device_of(G)
     if O is G:
@@ -1342,11 +1347,12 @@ def _muon_update(G, O, m, m_out, st, scale, precision, stream):
                 raise ValueError("m_out must be [n_rows][n_cols]")
     if precision != F32 and precision != F16:
         raise ValueError("precision must be F32 or F16")
-    ws, wsb = _workspace(workspace_bytes(OP_MUON if precision == F32 else OP_MUON_F16, N, K, 0, 0), G.device, stream)
+    need = workspace_bytes(OP_MUON if precision == F32 else OP_MUON_F16, N, K, 0, 0)
+    ws, wsb = _workspace(max(need, room), G.device, stream)
     _check(lib().muon_update(N, K, code, G.data_ptr(), ldg, _p(m), ldm, _p(m_out), ldmo, st.mu, 1 if st.nesterov else 0,
                              st.steps, st.eps, scale, precision, O.data_ptr(), ldo, _p(ws), wsb, _stream(stream)),
            "muon_update")
-    return O
+    return ws, wsb
 
 
 def orthogonalize(G, out=None, steps=5, eps=1e-7, scale=1.0, precision=None, stream=None):
@@ -1360,7 +1366,8 @@ def orthogonalize(G, out=None, steps=5, eps=1e-7, scale=1.0, precision=None, str
     if out is None:
         N, K, _, _ = _typed_mat(G, "G")
         out = _new((N, K), G.dtype, G.device, stream)
-    return _muon_update(G, out, None, None, MuonState(None, 0.0, False, steps, eps), scale, precision, stream)
+    _muon_update(G, out, None, None, MuonState(None, 0.0, False, steps, eps), scale, precision, stream)
+    return out
 
 
 def _muon_args(W, G, st, eta, lam):
@@ -1450,20 +1457,26 @@ def prox_muon_recompress(W: CSR, G, st: MuonState, eta, lam, O=None, capacity=No
                          precision=F32, stream=None):
     """W' = CSR of the Prox-Muon step (the bits of prox_muon_step and csr_recompress), the recompression fused with the
     threshold (prox_l1_recompress).  O (float32 [N][K], may be G itself) receives the update; st.m is updated in
-    place, but not by a call that fails, for its capacity or its arguments."""
+    place, but not by a call that fails, for its capacity, its arguments or want of memory."""
     torch = _torch()
     N, K, scale = _muon_args(W, G, st, eta, lam)
-    W.validate_shapes()
+    nnz = W.validate_shapes()
     _muon_writes(W, G if O is None else O, st)
     if out is not None:
         _muon_out(W, out, capacity, G.get_device(), (st.m, G if O is None else O))
-    cap = capacity if capacity is not None else (N * K if out is None else min(out.col_idx.numel(), out.vals.numel()))
-    short = cap < N * K  # the count may not fit: the momentum is stored behind the recompression
-    m_new = _new((N, K), torch.float32, G.device, stream) if short else st.m
+    # everything that the call needs is allocated before the update is launched, in the order of the call's stream
     if O is None:
         O = _new((N, K), torch.float32, G.device, stream)
-    _muon_update(G, O, st.m, m_new, st, scale, precision, stream)
-    out = prox_l1_recompress(W, O, eta, lam, capacity=capacity, out=out, stream=stream)
+    if out is None:
+        cap = N * K if capacity is None else int(capacity)
+        out = CSR(N, K, *(_new((n,), dtype, G.device, stream) for n, dtype in
+                          ((N + 1, torch.int32), (max(cap, 1), torch.int32), (max(cap, 1), torch.float32))))
+    cap = min(out.col_idx.numel(), out.vals.numel()) if capacity is None else int(capacity)
+    short = cap < N * K  # the count may not fit: the momentum is stored behind the recompression
+    m_new = _new((N, K), torch.float32, G.device, stream) if short else st.m
+    ws, wsb = _muon_update(G, O, st.m, m_new, st, scale, precision, stream,
+                           room=workspace_bytes(OP_PROX_RECOMPRESS, N, K, nnz, 0))
+    _prox_l1_recompress(W, nnz, O, _mat(O, "O")[2], eta, lam, cap, out, ws, wsb, stream)
     if short:
         with torch.cuda.stream(torch.cuda.current_stream(G.device) if stream is None else stream):
             st.m.copy_(m_new)

@@ -602,3 +602,61 @@ def test_steps_that_would_write_into_the_layer_are_refused():
         with pytest.raises(ValueError):
             f(W, G, L1.MuonState(over), 0.1, 0.1)
     assert torch.equal(st.m, m0) and all(torch.equal(a, b) for a, b in zip(keep, (W.row_ptr, W.col_idx, W.vals)))
+
+
+@pytest.mark.parametrize("call", ["step", "recompress", "recompress_short"])
+def test_calls_without_memory_leave_the_momentum(call, monkeypatch):
+    # whichever of a call's allocations fails, the momentum is not stored
+    torch = _torch()
+    N, K = 300, 200
+    W, _ = _layer(N, K, 0.3, 5)
+    G, m0 = gradient(N, K, 1), gradient(N, K, 2)
+    st = L1.MuonState(m0.clone())
+    run = {"step": lambda: L1.prox_muon_step(W, G, st, 0.05, 0.1),
+           "recompress": lambda: L1.prox_muon_recompress(W, G, st, 0.05, 0.1),
+           "recompress_short": lambda: L1.prox_muon_recompress(W, G, st, 0.05, 0.1, capacity=N * K - 1)}[call]
+    empty, left = torch.empty, [0]
+
+    def limited(*a, **kw):
+        if left[0] == 0:
+            raise torch.OutOfMemoryError("no memory left")
+        left[0] -= 1
+        return empty(*a, **kw)
+
+    for n in range(20):
+        L1._ws_cache.clear()
+        left[0] = n
+        monkeypatch.setattr(torch, "empty", limited)
+        try:
+            done = run()
+        except torch.OutOfMemoryError:
+            done = None
+        monkeypatch.setattr(torch, "empty", empty)
+        torch.cuda.synchronize()
+        if done is not None:
+            break
+        assert torch.equal(st.m, m0), n
+    assert done is not None and n >= 2 and not torch.equal(st.m, m0)
+
+
+def test_memory_belongs_to_the_calls_stream(monkeypatch):
+    # what a call allocates for its work on a stream is allocated in that stream's order
+    torch = _torch()
+    W, _ = _layer(300, 200, 0.3, 5)
+    G, st = gradient(300, 200, 1), L1.MuonState.zeros((300, 200), "cuda")
+    torch.cuda.synchronize()
+    side, seen, empty = torch.cuda.Stream(), [], torch.empty
+
+    def watched(*a, **kw):
+        seen.append(torch.cuda.current_stream().cuda_stream)
+        return empty(*a, **kw)
+
+    monkeypatch.setattr(torch, "empty", watched)
+    L1._ws_cache.clear()
+    L1.prox_muon_recompress(W, G, st, 0.05, 0.1, stream=side)
+    L1.prox_muon_recompress(W, G, st, 0.05, 0.1, capacity=300 * 200 - 1, stream=side)
+    L1.prox_muon_step(W, G, st, 0.05, 0.1, stream=side)
+    L1.orthogonalize(G, stream=side)
+    monkeypatch.setattr(torch, "empty", empty)
+    side.synchronize()
+    assert len(seen) >= 8 and set(seen) == {side.cuda_stream}
