@@ -607,7 +607,8 @@ int l1csr_softmax_xent(int32_t C, int32_t B, const float *logits, int64_t ld,
  * G [N][ldg] and O [N][ldo] are of `dtype` (l1csr_dtype), M [N][ldm] and M_out
  * [N][ldmo] float.  M_out receives M' (NULL: not stored; may be M itself with
  * the same leading dimension); O may be G itself with the same leading
- * dimension; the arrays may not overlap otherwise (L1CSR_EINVAL).  0 <= mu < 1
+ * dimension; the arrays may not overlap otherwise (L1CSR_EINVAL; columns of one
+ * buffer, whose rows have the same number of bytes, do not).  0 <= mu < 1
  * (ignored without M), 1 <= steps <= L1CSR_MUON_MAX_STEPS, eps >= 0, scale finite.
  * |U|_F is summed in double.  precision L1CSR_F32: operands as two fp16 parts
  * (22 bits), three exact products, fp32 sums; about 1e-6 of |O|_F off the exact
@@ -636,9 +637,10 @@ int muon_update(int32_t N, int32_t K, int dtype, const void *G, int64_t ldg, con
  * exclude a class.  Sums over tokens are in double; everything is reproducible.
  * dlogits [C][ldd], of the type of the logits, receives d loss / d logits (every
  * column of it; NULL: the loss alone); it may be the logits themselves (with the
- * same leading dimension), but may not overlap them otherwise, and no other output may
- * overlap an input or an output (L1CSR_EINVAL).  C, B <= 2^30 and pairs < 2^24
- * (L1CSR_EUNSUPPORTED; l1csr_workspace_bytes gives 0).
+ * same leading dimension) or other columns of the same buffer, but may not overlap
+ * them otherwise, and no other output may overlap an input or an output
+ * (L1CSR_EINVAL).  C, B <= 2^30 and pairs < 2^24 (L1CSR_EUNSUPPORTED;
+ * l1csr_workspace_bytes gives 0).
  * ws, 16-byte aligned, as l1csr_workspace_bytes(L1CSR_OP_TOKEN_LOSS, C, pairs, 0, B),
  * pairs = 0 but for the preference loss.
  *

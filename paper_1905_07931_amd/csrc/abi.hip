@@ -97,6 +97,25 @@ size_t typed_bytes(int64_t rows, int64_t cols, int64_t ld, int dtype) {
     return rows > 0 && cols > 0 ? (size_t)(((rows - 1) * ld + cols) * dtype_bytes(dtype)) : 0;
 }
 
+// Two matrices of `rows` rows share memory: by their extents, but not if they lie side by side in rows of
+// the same number of bytes (columns of one buffer).
+struct matrix_span {
+    const void *p;
+    size_t row, pitch;  // bytes used of a row, bytes from row to row
+};
+matrix_span span_of(const void *p, int64_t cols, int64_t ld, int dtype) {
+    return {p, (size_t)(cols * dtype_bytes(dtype)), (size_t)(ld * dtype_bytes(dtype))};
+}
+bool share_memory(const matrix_span &a, const matrix_span &b, int64_t rows) {
+    if (a.row == 0 || b.row == 0 || rows <= 0) return false;
+    const size_t last = (size_t)(rows - 1);
+    if (!bytes_overlap(a.p, last * a.pitch + a.row, b.p, last * b.pitch + b.row)) return false;
+    if (a.pitch != b.pitch) return true;
+    const uintptr_t pa = reinterpret_cast<uintptr_t>(a.p), pb = reinterpret_cast<uintptr_t>(b.p);
+    const size_t d = pa <= pb ? (pb - pa) % a.pitch : (a.pitch - (pa - pb) % a.pitch) % a.pitch;  // b behind a in a row
+    return d < a.row || a.pitch - d < b.row;
+}
+
 // What the calls over logits check alike; n_out: floats of a.out
 int token_check(const token_loss_args &a, int n_out, size_t ws_bytes, const void *ws) {
     if (a.C <= 0 || a.B < 0 || a.pairs < 0 || bad_dtype(a.dtype)) return L1CSR_EINVAL;
@@ -106,8 +125,8 @@ int token_check(const token_loss_args &a, int n_out, size_t ws_bytes, const void
     if (a.dlogits != nullptr) {
         if (a.ldd < a.B) return L1CSR_EINVAL;
         if (a.dlogits == a.logits ? a.ldd != a.ld
-                                  : bytes_overlap(a.dlogits, typed_bytes(a.C, a.B, a.ldd, a.dtype), a.logits,
-                                                  typed_bytes(a.C, a.B, a.ld, a.dtype)))
+                                  : share_memory(span_of(a.dlogits, a.B, a.ldd, a.dtype),
+                                                 span_of(a.logits, a.B, a.ld, a.dtype), a.C))
             return L1CSR_EINVAL;
     }
     // no output may lie in an input (its values are read after the first outputs are stored) or in another output
@@ -940,12 +959,11 @@ int muon_update(int32_t N, int32_t K, int dtype, const void *G, int64_t ldg, con
     if (bad_dense(G, N, K, ldg) || bad_dense(O, N, K, ldo)) return L1CSR_EINVAL;
     if (M != nullptr && (ldm < K || !(mu >= 0.f && mu < 1.f))) return L1CSR_EINVAL;
     if (M_out != nullptr && (M == nullptr || ldmo < K)) return L1CSR_EINVAL;
-    const size_t g = typed_bytes(N, K, ldg, dtype), o = typed_bytes(N, K, ldo, dtype);
-    const size_t m = M ? dense_bytes(N, K, ldm) : 0, mo = M_out ? dense_bytes(N, K, ldmo) : 0;
-    if (G == O ? ldg != ldo : bytes_overlap(G, g, O, o)) return L1CSR_EINVAL;
-    if (M != nullptr && M == M_out ? ldm != ldmo : bytes_overlap(M, m, M_out, mo)) return L1CSR_EINVAL;
-    if (bytes_overlap(M, m, G, g) || bytes_overlap(M, m, O, o) || bytes_overlap(M_out, mo, G, g) ||
-        bytes_overlap(M_out, mo, O, o))
+    const matrix_span g = span_of(G, K, ldg, dtype), o = span_of(O, K, ldo, dtype),
+                      m = span_of(M, K, ldm, L1CSR_DTYPE_F32), mo = span_of(M_out, K, ldmo, L1CSR_DTYPE_F32);
+    if (G == O ? ldg != ldo : share_memory(g, o, N)) return L1CSR_EINVAL;
+    if (M != nullptr && M == M_out ? ldm != ldmo : share_memory(m, mo, N)) return L1CSR_EINVAL;
+    if (share_memory(m, g, N) || share_memory(m, o, N) || share_memory(mo, g, N) || share_memory(mo, o, N))
         return L1CSR_EINVAL;
     const int parts = precision == L1CSR_F32 ? 2 : 1;
     const size_t need = muon_workspace_bytes(N, K, parts);

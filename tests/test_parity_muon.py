@@ -660,3 +660,26 @@ def test_memory_belongs_to_the_calls_stream(monkeypatch):
     monkeypatch.setattr(torch, "empty", empty)
     side.synchronize()
     assert len(seen) >= 8 and set(seen) == {side.cuda_stream}
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("N,K", [(33, 65), (130, 301), (301, 130)])
+def test_columns_of_one_buffer(N, K, dtype):
+    # the parts of a fused gradient, their update beside them: the bits of matrices apart, the other columns untouched
+    torch = _torch()
+    buf = torch.full((N, 4 * K + 3), 7.0, device="cuda", dtype=getattr(torch, dtype))
+    G, O = buf[:, K:2 * K], buf[:, 2 * K:3 * K]
+    G.copy_(gradient(N, K, 5) * 1e3)
+    want = L1.orthogonalize(G.contiguous())
+    assert torch.equal(L1.orthogonalize(G, out=O), want) and torch.equal(O, want)
+    assert bool((buf[:, :K] == 7).all()) and bool((buf[:, 3 * K:] == 7).all())
+    if dtype != "float32":
+        return
+    W, _ = _layer(N, K, 0.3, 1)
+    state = torch.full((N, 3 * K), 5.0, device="cuda")
+    m, new, Z = (state[:, i * K:(i + 1) * K] for i in range(3))
+    m.copy_(gradient(N, K, 6))
+    ref, ref_new = L1.MuonState(m.contiguous()), torch.empty((N, K), device="cuda")
+    want = L1.prox_muon_step(W, G, ref, 0.05, 0.1, m_out=ref_new)
+    assert torch.equal(L1.prox_muon_step(W, G, L1.MuonState(m), 0.05, 0.1, Z=Z, m_out=new), want)
+    assert torch.equal(new, ref_new) and torch.equal(m, ref.m)

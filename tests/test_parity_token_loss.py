@@ -381,3 +381,21 @@ def test_refusals():
         L1.preference_loss(z, labels, torch.zeros(3, dtype=torch.int32, device=z.device), label_smoothing=0.7)
     with pytest.raises(ValueError):
         L1.token_logp(z, labels.cpu())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("C,B", [(9, 13), (700, 77), (4000, 3)])
+def test_gradient_beside_the_logits(C, B, dtype):
+    # logits and gradient as columns of one buffer: the bits of matrices apart, the other columns untouched
+    torch = _torch()
+    z, labels, _, _ = logits(C, B, dtype, seed=6)
+    buf = torch.full((C, 3 * B + 1), 7.0, dtype=z.dtype, device=z.device)
+    own, dz = buf[:, :B], buf[:, B:2 * B]
+    own.copy_(z)
+    old, adv = vec(np.full(B, -4.0)), vec(np.linspace(-1, 1, B))
+    ptr = torch.tensor([0, B // 2, B], dtype=torch.int32, device=z.device)
+    for f in (lambda x, d: L1.policy_loss(x, labels, old, adv, dlogits=d), lambda x, d: L1.preference_loss(x, labels, ptr, dlogits=d)):
+        want = f(z, None)
+        got = f(own, dz)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        assert torch.equal(own, z) and bool((buf[:, 2 * B:] == 7).all())

@@ -207,3 +207,27 @@ def test_prox_muon_refuses_to_write_into_what_it_reads():
             L1._muon_writes(W, O, state, m_out, row_counts)
     with pytest.raises(TypeError):
         L1._muon_writes(W, Z.numpy(), st)
+
+
+@pytest.mark.skipif(not NO_GPU, reason="validation calls use placeholder pointers; run without a GPU")
+def test_columns_of_one_buffer_are_no_overlap(lib):
+    """Matrices that lie side by side in the rows of one buffer share no element; shifted ones do."""
+    at = lambda n: C.c_void_p((1 << 30) + n)  # noqa: E731
+    far = C.c_void_p(1 << 44)
+    for dtype, e in ((0, 4), (1, 2), (2, 2)):
+        wide = dict(dtype=dtype, G=at(0), ldg=24, ldo=24, M=None, M_out=None)
+        for o, apart in ((8, True), (16, True), (7, False), (17, False), (1, False), (24 + 8, True), (24 + 4, False),
+                         (24 * 7, False), (24 * 8, True)):
+            # (not refused: the launch itself fails where there is no GPU)
+            assert (muon(lib, O=at(o * e), **wide) != EINVAL) == apart, (dtype, o)
+            assert (muon(lib, **{**wide, "G": at(o * e), "O": at(0)}) != EINVAL) == apart, (dtype, o)
+            z = dict(dtype=dtype, z=at(0), ld=24, dz=at(o * e), ldd=24, labels=far, old=far, adv=far, stats=C.c_void_p(1 << 45))
+            assert (policy(lib, **z) != EINVAL) == apart, (dtype, o)
+    side = dict(G=far, ldg=8, O=C.c_void_p(1 << 45), ldo=8, M=at(0), ldm=24)
+    assert muon(lib, M_out=at(32), ldmo=24, **side) != EINVAL and muon(lib, M_out=at(28), ldmo=24, **side) == EINVAL
+    # a 16-bit gradient of 16 columns' bytes beside the momentum: the same bytes a row
+    mixed = dict(dtype=1, O=far, ldo=8, M=at(0), M_out=at(0), ldm=12, ldmo=12, ldg=24)
+    assert muon(lib, G=at(32), **mixed) != EINVAL and muon(lib, G=at(30), **mixed) == EINVAL
+    assert muon(lib, G=at(34), **mixed) == EINVAL
+    # rows of other lengths: refused where the extents meet
+    assert muon(lib, G=at(0), ldg=24, O=at(32), ldo=25, M=None, M_out=None) == EINVAL
