@@ -683,3 +683,16 @@ def test_columns_of_one_buffer(N, K, dtype):
     want = L1.prox_muon_step(W, G, ref, 0.05, 0.1, m_out=ref_new)
     assert torch.equal(L1.prox_muon_step(W, G, L1.MuonState(m), 0.05, 0.1, Z=Z, m_out=new), want)
     assert torch.equal(new, ref_new) and torch.equal(m, ref.m)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("N,K", [(100, 300), (300, 784), (1500, 1500)])
+def test_fewer_bits_only_where_asked_for(N, K, dtype):
+    torch = _torch()
+    G = (gradient(N, K, 8) * 1e3).to(getattr(torch, dtype))
+    full = L1.orthogonalize(G, precision=L1.F32)
+    assert torch.equal(L1.orthogonalize(G), full) and torch.equal(L1.orthogonalize(G, precision=None), full)
+    # the result's rounding is all that a 16-bit matrix loses: half a step an element
+    want = steps_of(G)
+    assert rel(full, want) <= bound(G, want) + HALF_STEP[dtype]
+    assert (min(N, K) <= 128) == torch.equal(L1.orthogonalize(G, precision=L1.F16), full)
