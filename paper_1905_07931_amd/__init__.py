@@ -1308,13 +1308,15 @@ def preference_loss(logits, labels, seq_ptr, ref_logp=None, weights=None, beta=0
 @dataclass
 class MuonState:
     """Hyper-parameters and momentum of Prox-Muon.  m is a float32 device tensor [N][K] (a leading dimension >= K is
-    allowed) that starts at zero; scale multiplies the orthogonalised update (None: sqrt(max(1, N / K)))."""
+    allowed) that starts at zero; scale multiplies the orthogonalised update (None: sqrt(max(1, N / K))); precision (F32 or
+    F16, as in orthogonalize) is that of the update's products where a call does not name its own."""
     m: object
     mu: float = 0.95
     nesterov: bool = True
     steps: int = 5
     eps: float = 1e-7
     scale: float | None = None
+    precision: int = F32
 
     @staticmethod
     def zeros(shape, device, **kw):
@@ -1345,6 +1347,8 @@ def _muon_update(G, O, m, m_out, st, scale, precision, stream, room=0):
             rows, cols, ldmo = _mat(_same_device(index, m_out, "m_out"), "m_out")
             if rows != N or cols != K:
                 raise ValueError("m_out must be [n_rows][n_cols]")
+    if precision is None:
+        precision = st.precision
     if precision != F32 and precision != F16:
         raise ValueError("precision must be F32 or F16")
     need = workspace_bytes(OP_MUON if precision == F32 else OP_MUON_F16, N, K, 0, 0)
@@ -1362,8 +1366,6 @@ def orthogonalize(G, out=None, steps=5, eps=1e-7, scale=1.0, precision=F32, stre
     accuracy, whatever the type) or, where the caller asks for it, F16: operands rounded to fp16, about 1.5e-3 of the
     norm off, in 2/5 of the time for large matrices (as F32 where min(N, K) <= 128).  A bfloat16 result's own rounding is
     1.7e-3.  Returns out."""
-    if precision is None:
-        precision = F32
     if out is None:
         N, K, _, _ = _typed_mat(G, "G")
         out = _new((N, K), G.dtype, G.device, stream)
@@ -1438,7 +1440,7 @@ def _muon_out(W, out, capacity, index, dense):
         _apart([a], outs[i + 1:] + ins, "out shares memory with W, the update, the momentum or itself")
 
 
-def prox_muon_step(W: CSR, G, st: MuonState, eta, lam, Z=None, m_out=None, row_counts=None, precision=F32,
+def prox_muon_step(W: CSR, G, st: MuonState, eta, lam, Z=None, m_out=None, row_counts=None, precision=None,
                    stream=None):
     """One Prox-Muon step of the l1 phase over all N*K weights: m' = mu m + G, O = scale * NS(G + mu m') (muon_update;
     without nesterov NS(m')), Z = S_{eta*lam}(W - eta O).  Z may be G itself; st.m is updated in place, or m_out receives
@@ -1455,7 +1457,7 @@ def prox_muon_step(W: CSR, G, st: MuonState, eta, lam, Z=None, m_out=None, row_c
 
 
 def prox_muon_recompress(W: CSR, G, st: MuonState, eta, lam, O=None, capacity=None, out: CSR | None = None,
-                         precision=F32, stream=None):
+                         precision=None, stream=None):
     """W' = CSR of the Prox-Muon step (the bits of prox_muon_step and csr_recompress), the recompression fused with the
     threshold (prox_l1_recompress).  O (float32 [N][K], may be G itself) receives the update; st.m is updated in
     place, but not by a call that fails, for its capacity, its arguments or want of memory."""

@@ -133,7 +133,7 @@ def l1_step(W: CSR, X, dY, eta: float, lam: float, *, Y, dX, dW, csc: CSC, out: 
     adaptive: Prox-RMSProp / Prox-ADAM state with dense [N][K] m, v; the step
     then ends with prox_adaptive_recompress (state updated in place, t
     advanced) instead of dense_wgrad_prox + csr_recompress_counted; a MuonState ends it with
-    prox_muon_recompress (st.m updated in place).  bitmap: buffers for
+    prox_muon_recompress (st.m updated in place, the update in st.precision).  bitmap: buffers for
     W's bitmap index (Bitmap.empty(N, K), shared by the CSC build and the weight
     update); allocated per call if None.  All
     outputs are ready on the

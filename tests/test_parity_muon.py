@@ -696,3 +696,31 @@ def test_fewer_bits_only_where_asked_for(N, K, dtype):
     want = steps_of(G)
     assert rel(full, want) <= bound(G, want) + HALF_STEP[dtype]
     assert (min(N, K) <= 128) == torch.equal(L1.orthogonalize(G, precision=L1.F16), full)
+
+
+def test_step_takes_the_states_precision():
+    torch = _torch()
+    N, K, Bt = 300, 784, 64
+    W, _ = _layer(N, K, 0.1, 4)
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    X, dY = (torch.randn((r, Bt), device="cuda", generator=gen) for r in (K, N))
+    G = L1.dense_wgrad(dY, X)
+    updates = {}
+    for precision in (L1.F32, L1.F16):
+        st, dW = L1.MuonState.zeros((N, K), "cuda", precision=precision), torch.empty((N, K), device="cuda")
+        out = _full_csr(N, K)
+        L1.l1_step(W, X, dY, 0.02, 0.05, Y=torch.empty((N, Bt), device="cuda"), dX=torch.empty((K, Bt), device="cuda"), dW=dW,
+                   csc=L1.CSC.empty(K, W.nnz, "cuda"), out=out, adaptive=st)
+        ref, O = L1.MuonState.zeros((N, K), "cuda"), torch.empty((N, K), device="cuda")
+        want = L1.prox_muon_recompress(W, G, ref, 0.02, 0.05, O=O, precision=precision)
+        assert torch.equal(dW, O) and all(bits_equal(a, b) for a, b in zip(out.to_host(), want.to_host()))
+        # a call's own choice goes before the state's
+        other = L1.MuonState.zeros((N, K), "cuda", precision=L1.F16)
+        assert torch.equal(L1.prox_muon_step(W, G, other, 0.02, 0.05, precision=precision),
+                           L1.prox_muon_step(W, G, L1.MuonState.zeros((N, K), "cuda"), 0.02, 0.05, precision=precision))
+        updates[precision] = dW
+    exact = steps_of(1.95 * G.double())  # mu 0.95 from zero momentum: U = 1.95 G
+    assert rel(updates[L1.F32], exact) <= bound(1.95 * G, exact) and rel(updates[L1.F16], exact) <= 4.9e-3
+    assert not torch.equal(updates[L1.F32], updates[L1.F16])
+    with pytest.raises(ValueError):
+        L1.prox_muon_step(W, G, L1.MuonState.zeros((N, K), "cuda", precision=L1.BF16X3), 0.02, 0.05)
