@@ -667,6 +667,12 @@ int muon_update(int32_t N, int32_t K, int dtype, const void *G, int64_t ldg, con
  *   with ls = label_smoothing in [0, 1/2], beta >= 0; ref_logp [2 pairs] or NULL (zeros).
  *   rewards [2 pairs] (nullable) receives the rewards, *loss (device) the loss, 0 for
  *   no pairs.  Columns of dlogits that belong to no sequence are 0.
+ *
+ * The _scaled calls take a finite factor of the gradient: dlogits receives grad_scale d loss /
+ * d logits (1 in the calls without), the factor ahead of dlogits' one rounding; nothing
+ * else is scaled.  A mean over many tokens and classes has entries under the smallest
+ * fp16 value, 2^-24, which are lost without it; entries past the type's largest are
+ * infinite.  It also weighs the parts of a batch that is taken in several calls.
  */
 int l1csr_token_logp(int32_t C, int32_t B, int dtype, const void *logits, int64_t ld, const int32_t *labels,
                      float *logp, void *ws, size_t ws_bytes, hipStream_t stream);
@@ -678,6 +684,15 @@ int l1csr_preference_loss(int32_t C, int32_t B, int dtype, const void *logits, i
                           int32_t pairs, const int32_t *seq_ptr, const float *ref_logp, const float *weights,
                           float beta, float label_smoothing, void *dlogits, int64_t ldd, float *rewards, float *loss,
                           void *ws, size_t ws_bytes, hipStream_t stream);
+int l1csr_policy_loss_scaled(int32_t C, int32_t B, int dtype, const void *logits, int64_t ld, const int32_t *labels,
+                             const float *old_logp, const float *advantages, const float *ref_logp,
+                             const float *weights, float clip_low, float clip_high, float kl_coef, float grad_scale,
+                             void *dlogits, int64_t ldd, float *logp, float *stats, void *ws, size_t ws_bytes,
+                             hipStream_t stream);
+int l1csr_preference_loss_scaled(int32_t C, int32_t B, int dtype, const void *logits, int64_t ld, const int32_t *labels,
+                                 int32_t pairs, const int32_t *seq_ptr, const float *ref_logp, const float *weights,
+                                 float beta, float label_smoothing, float grad_scale, void *dlogits, int64_t ldd,
+                                 float *rewards, float *loss, void *ws, size_t ws_bytes, hipStream_t stream);
 
 #ifdef __cplusplus
 }

@@ -121,9 +121,13 @@ def lib():
                                         vp, sz, vp]
         L.l1csr_preference_loss.argtypes = [i32, i32, C.c_int, vp, i64, vp, i32, vp, vp, vp, f32, f32, vp, i64, vp, vp,
                                             vp, sz, vp]
+        for name, at in (("l1csr_policy_loss", 13), ("l1csr_preference_loss", 12)):  # (grad_scale in front of dlogits)
+            plain = getattr(L, name).argtypes
+            getattr(L, name + "_scaled").argtypes = [*plain[:at], f32, *plain[at:]]
         L.muon_update.argtypes = [i32, i32, C.c_int, vp, i64, vp, i64, vp, i64, f32, C.c_int, C.c_int, f32, f32, C.c_int,
                                   vp, i64, vp, sz, vp]
-        for name in ("l1csr_token_logp", "l1csr_policy_loss", "l1csr_preference_loss", "muon_update", "csr_spmm_fwd", "csr_spmm_plan", "csr_spmm_planned", "csc_build", "csc_update_vals", "csr_spmm_bwd_t", "dense_wgrad",
+        for name in ("l1csr_token_logp", "l1csr_policy_loss", "l1csr_preference_loss", "l1csr_policy_loss_scaled",
+                     "l1csr_preference_loss_scaled", "muon_update", "csr_spmm_fwd", "csr_spmm_plan", "csr_spmm_planned", "csc_build", "csc_update_vals", "csr_spmm_bwd_t", "dense_wgrad",
                      "sddmm_masked_wgrad", "prox_l1_step", "csr_recompress", "prox_l1_recompress",
                      "prox_l1_recompress_noalloc", "dense_wgrad_prox", "csr_recompress_counted", "csr_bitmap_build",
                      "csr_compact", "csr_validate", "l1csr_relu_fwd", "l1csr_relu_bwd", "l1csr_softmax_xent",
@@ -1251,15 +1255,17 @@ def token_logp(logits, labels, logp=None, stream=None):
 
 
 def policy_loss(logits, labels, old_logp, advantages, ref_logp=None, weights=None, clip_low=0.2, clip_high=0.2,
-                kl_coef=0.0, dlogits=None, logp=None, stats=None, grad=True, stream=None):
+                kl_coef=0.0, dlogits=None, logp=None, stats=None, grad=True, stream=None, *, grad_scale=1.0):
     """Clipped policy loss with a penalty on the distance from a reference, and its gradient.
 
     With lp the token_logp of logits [C][B], r = exp(lp - old_logp) and the KL estimate
     k = exp(ref_logp - lp) - (ref_logp - lp) - 1 (0 without ref_logp), the loss is the weighted mean over the tokens of
     -min(r adv, clip(r, 1 - clip_low, 1 + clip_high) adv) + kl_coef k.  A token counts if its label lies in [0, C) and its
     weight (weights float32 [B], default 1) is not 0; the logits of the others are not used and their columns of
-    dlogits are 0.  dlogits (the type and shape of logits) may be logits itself; grad=False leaves it out.  No other
-    output may share memory with an input (logp with old_logp, say).
+    dlogits are 0.  dlogits (the type and shape of logits) may be logits itself; grad=False leaves it out.  It receives
+    grad_scale times the gradient, scaled ahead of its rounding (an fp16 gradient of a large vocabulary needs that:
+    entries under 2^-24 are lost; nothing else is scaled).  No other output may share memory with an input (logp with
+    old_logp, say).
     Returns (stats, dlogits, logp): stats[4] = loss, mean policy term, mean k, share of clipped tokens."""
     Cn, B, code, ld, dlogits, ldd, index = _token_args(logits, labels, weights, dlogits, grad, stream)
     f32 = _torch_module.float32
@@ -1270,22 +1276,22 @@ def policy_loss(logits, labels, old_logp, advantages, ref_logp=None, weights=Non
     logp = _result(logp, B, logits, index, "logp", "token (B)", stream)
     stats = _result(stats, 4, logits, index, "stats", "statistic (4)", stream)
     ws, wsb = _workspace(workspace_bytes(OP_TOKEN_LOSS, Cn, 0, 0, B), logits.device, stream)
-    _check(lib().l1csr_policy_loss(Cn, B, code, logits.data_ptr(), ld, labels.data_ptr(), old_logp.data_ptr(),
-                                   advantages.data_ptr(), _p(ref_logp), _p(weights), clip_low, clip_high, kl_coef,
-                                   _p(dlogits), ldd, logp.data_ptr(), stats.data_ptr(), _p(ws), wsb, _stream(stream)),
-           "l1csr_policy_loss")
+    _check(lib().l1csr_policy_loss_scaled(Cn, B, code, logits.data_ptr(), ld, labels.data_ptr(), old_logp.data_ptr(),
+                                          advantages.data_ptr(), _p(ref_logp), _p(weights), clip_low, clip_high, kl_coef,
+                                          grad_scale, _p(dlogits), ldd, logp.data_ptr(), stats.data_ptr(), _p(ws), wsb,
+                                          _stream(stream)), "l1csr_policy_loss")
     return stats, dlogits, logp
 
 
 def preference_loss(logits, labels, seq_ptr, ref_logp=None, weights=None, beta=0.1, label_smoothing=0.0, dlogits=None,
-                    rewards=None, loss=None, grad=True, stream=None):
+                    rewards=None, loss=None, grad=True, stream=None, *, grad_scale=1.0):
     """Preference loss over pairs of sequences packed along the tokens, and its gradient.
 
     seq_ptr (int32 [2 pairs + 1], not decreasing, within [0, B]): sequence 2p is the preferred one of pair p, 2p + 1 the
     rejected one.  rewards[s] = beta (sum of weights * token_logp over s - ref_logp[s]) (ref_logp float32 [2 pairs],
     default 0), D = rewards[2p] - rewards[2p + 1], loss = the mean over the pairs of
-    -(1 - ls) log sigmoid(D) - ls log sigmoid(-D) with ls = label_smoothing.  Tokens that do not count and dlogits as in
-    policy_loss; columns in no sequence get 0.  Returns (loss[1], dlogits, rewards)."""
+    -(1 - ls) log sigmoid(D) - ls log sigmoid(-D) with ls = label_smoothing.  Tokens that do not count, dlogits and
+    grad_scale as in policy_loss; columns in no sequence get 0.  Returns (loss[1], dlogits, rewards)."""
     Cn, B, code, ld, dlogits, ldd, index = _token_args(logits, labels, weights, dlogits, grad, stream)
     torch = _torch_module
     _vec(seq_ptr, torch.int32, "seq_ptr")
@@ -1298,10 +1304,10 @@ def preference_loss(logits, labels, seq_ptr, ref_logp=None, weights=None, beta=0
     rewards = _result(rewards, 2 * pairs, logits, index, "rewards", "sequence (2 * pairs)", stream)
     loss = _result(loss, 1, logits, index, "loss", "call (1)", stream)
     ws, wsb = _workspace(workspace_bytes(OP_TOKEN_LOSS, Cn, pairs, 0, B), logits.device, stream)
-    _check(lib().l1csr_preference_loss(Cn, B, code, logits.data_ptr(), ld, labels.data_ptr(), pairs, seq_ptr.data_ptr(),
-                                       _p(ref_logp), _p(weights), beta, label_smoothing, _p(dlogits), ldd,
-                                       rewards.data_ptr(), loss.data_ptr(), _p(ws), wsb, _stream(stream)),
-           "l1csr_preference_loss")
+    _check(lib().l1csr_preference_loss_scaled(Cn, B, code, logits.data_ptr(), ld, labels.data_ptr(), pairs,
+                                              seq_ptr.data_ptr(), _p(ref_logp), _p(weights), beta, label_smoothing,
+                                              grad_scale, _p(dlogits), ldd, rewards.data_ptr(), loss.data_ptr(), _p(ws),
+                                              wsb, _stream(stream)), "l1csr_preference_loss")
     return loss, dlogits, rewards
 
 

@@ -915,6 +915,15 @@ int l1csr_policy_loss(int32_t C, int32_t B, int dtype, const void *logits, int64
                       const float *old_logp, const float *advantages, const float *ref_logp, const float *weights,
                       float clip_low, float clip_high, float kl_coef, void *dlogits, int64_t ldd, float *logp,
                       float *stats, void *ws, size_t ws_bytes, hipStream_t stream) {
+    return l1csr_policy_loss_scaled(C, B, dtype, logits, ld, labels, old_logp, advantages, ref_logp, weights, clip_low,
+                                    clip_high, kl_coef, 1.f, dlogits, ldd, logp, stats, ws, ws_bytes, stream);
+}
+
+int l1csr_policy_loss_scaled(int32_t C, int32_t B, int dtype, const void *logits, int64_t ld, const int32_t *labels,
+                             const float *old_logp, const float *advantages, const float *ref_logp,
+                             const float *weights, float clip_low, float clip_high, float kl_coef, float grad_scale,
+                             void *dlogits, int64_t ldd, float *logp, float *stats, void *ws, size_t ws_bytes,
+                             hipStream_t stream) {
     token_loss_args a{};
     a.C = C; a.B = B; a.dtype = dtype;
     a.logits = logits; a.ld = ld; a.labels = labels; a.weights = weights;
@@ -922,7 +931,8 @@ int l1csr_policy_loss(int32_t C, int32_t B, int dtype, const void *logits, int64
     a.old_logp = old_logp; a.adv = advantages; a.ref_logp = ref_logp;
     a.clip_low = clip_low; a.clip_high = clip_high; a.kl_coef = kl_coef;
     a.out = stats;
-    if (!finite_f(clip_low) || !finite_f(clip_high) || !finite_f(kl_coef)) return L1CSR_EINVAL;
+    a.grad_scale = grad_scale;
+    if (!finite_f(clip_low) || !finite_f(clip_high) || !finite_f(kl_coef) || !finite_f(grad_scale)) return L1CSR_EINVAL;
     if (clip_low < 0.f || clip_low > 1.f || clip_high < 0.f || kl_coef < 0.f || stats == nullptr) return L1CSR_EINVAL;
     const int rc = token_check(a, 4, ws_bytes, ws);
     if (rc != L1CSR_OK) return rc;
@@ -934,6 +944,14 @@ int l1csr_preference_loss(int32_t C, int32_t B, int dtype, const void *logits, i
                           int32_t pairs, const int32_t *seq_ptr, const float *ref_logp, const float *weights,
                           float beta, float label_smoothing, void *dlogits, int64_t ldd, float *rewards, float *loss,
                           void *ws, size_t ws_bytes, hipStream_t stream) {
+    return l1csr_preference_loss_scaled(C, B, dtype, logits, ld, labels, pairs, seq_ptr, ref_logp, weights, beta,
+                                        label_smoothing, 1.f, dlogits, ldd, rewards, loss, ws, ws_bytes, stream);
+}
+
+int l1csr_preference_loss_scaled(int32_t C, int32_t B, int dtype, const void *logits, int64_t ld, const int32_t *labels,
+                                 int32_t pairs, const int32_t *seq_ptr, const float *ref_logp, const float *weights,
+                                 float beta, float label_smoothing, float grad_scale, void *dlogits, int64_t ldd,
+                                 float *rewards, float *loss, void *ws, size_t ws_bytes, hipStream_t stream) {
     token_loss_args a{};
     a.C = C; a.B = B; a.dtype = dtype;
     a.logits = logits; a.ld = ld; a.labels = labels; a.weights = weights;
@@ -941,6 +959,8 @@ int l1csr_preference_loss(int32_t C, int32_t B, int dtype, const void *logits, i
     a.pairs = pairs; a.seq_ptr = seq_ptr; a.ref_logp = ref_logp;
     a.beta = beta; a.smoothing = label_smoothing;
     a.rewards = rewards; a.out = loss;
+    a.grad_scale = grad_scale;
+    if (!finite_f(grad_scale)) return L1CSR_EINVAL;
     if (!finite_f(beta) || !(beta >= 0.f) || !(label_smoothing >= 0.f && label_smoothing <= 0.5f)) return L1CSR_EINVAL;
     if (loss == nullptr || (pairs > 0 && seq_ptr == nullptr) || pairs > INT32_MAX / 2 - 1) return L1CSR_EINVAL;
     const int rc = token_check(a, 1, ws_bytes, ws);

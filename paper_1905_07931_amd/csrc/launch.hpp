@@ -281,6 +281,7 @@ struct token_loss_args {
     float beta, smoothing;
     float *rewards;                // [2 pairs], nullable
     float *out;                    // policy: 4 values, preference: 1
+    float grad_scale;              // dlogits = grad_scale d loss / d logits
 };
 bool token_loss_fits(int C, int B, int pairs);  // else it has no workspace either
 size_t token_loss_workspace_bytes(int C, int B, int pairs);

@@ -8,7 +8,8 @@
 //               D = reward_chosen - reward_rejected,
 //               loss = mean_p( -(1 - ls) log sig(D) - ls log sig(-D) )
 // Both gradients are dz[c][b] = coef_b (1[c = a_b] - softmax(z_.b)_c) with one
-// coefficient a token, coef_b = d loss / d lp_b.
+// coefficient a token, coef_b = d loss / d lp_b, times a factor of the caller's
+// that comes before dz's rounding (fp16 holds nothing under 2^-24).
 //
 // Three passes: partial (maximum, sum of exponentials) of every column over
 // ranges of classes; a token pass that joins them and takes the loss and the
@@ -372,11 +373,11 @@ template <typename T, int V, int KIND>
 __global__ __launch_bounds__(kThreads) void gradient_kernel(int C, int B, const T *z, int64_t ld,
                                                             const int *__restrict__ labels, grid_shape g, token_out t,
                                                             T *dz, int64_t ldd, int n_sums, float kl_coef,
-                                                            float *__restrict__ out) {
+                                                            float grad_scale, float *__restrict__ out) {
     constexpr int U = 4;
     __shared__ double lds[kThreads / kWave];
     const float scale =
-        (float)finish<KIND>(n_sums, t.sums, kl_coef, lds, blockIdx.x == 0 && blockIdx.y == 0, out);
+        (float)(grad_scale * finish<KIND>(n_sums, t.sums, kl_coef, lds, blockIdx.x == 0 && blockIdx.y == 0, out));
     const int TX = 1 << g.tx_shift, TY = kThreads >> g.tx_shift;
     const int tx = threadIdx.x & (TX - 1), ty = threadIdx.x >> g.tx_shift;
     const columns<V> k(tx, g.tx_shift, B);
@@ -528,7 +529,7 @@ __global__ __launch_bounds__(kSmallThreads) void small_loss_kernel(token_loss_ar
         }
     }
     if constexpr (KIND == kLogp) return;
-    float scale = 1.f;
+    float scale = a.grad_scale;
     if constexpr (KIND == kPolicy) {
         const double sw = sum(ps.weight), inv = sw != 0 ? 1 / sw : 0.0;
         const double pg = sum(ps.pg) * inv, kl = sum(ps.kl) * inv, off = sum(ps.off) * inv;
@@ -538,7 +539,7 @@ __global__ __launch_bounds__(kSmallThreads) void small_loss_kernel(token_loss_ar
             a.out[2] = (float)kl;
             a.out[3] = (float)off;
         }
-        scale = (float)inv;
+        scale = (float)(a.grad_scale * inv);
     } else {
         __syncthreads();
         double loss = 0;
@@ -687,7 +688,7 @@ hipError_t run(const token_loss_args &a, const policy_args &P, void *ws, hipStre
         else
             gradient_kernel<T, V, KIND><<<grid, kThreads, 0, s>>>(a.C, a.B, z, a.ld, a.labels, g, t,
                                                                   static_cast<T *>(a.dlogits), a.ldd, n, P.kl_coef,
-                                                                  a.out);
+                                                                  a.grad_scale, a.out);
         return hipGetLastError();
     }
 }

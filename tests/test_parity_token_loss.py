@@ -399,3 +399,42 @@ def test_gradient_beside_the_logits(C, B, dtype):
         got = f(own, dz)
         assert all(torch.equal(a, b) for a, b in zip(got, want))
         assert torch.equal(own, z) and bool((buf[:, 2 * B:] == 7).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("C,B", [(10, 100), (32768, 64), (50257, 5)])
+def test_scaled_gradients(C, B, dtype):
+    """grad_scale comes before the one rounding of dlogits: what fp16 cannot hold of a mean's gradient over a large vocabulary
+    (entries under 2^-24) is there in the scaled one, to the formula's tolerance."""
+    torch = _torch()
+    z, labels, z64, lab = logits(C, B, dtype, seed=8)
+    lp, p = ref_logp(z64, lab, np.ones(B, bool))
+    old, adv = (lp - 0.1).astype(np.float32), np.linspace(0.25, 1, B).astype(np.float32)
+    ones = np.ones(B)
+    _, coef = ref_policy(lp, ones.astype(bool), ones, old.astype(np.float64), adv.astype(np.float64), None, 0.2, 0.3, 0.0)
+    size = np.exp(lp - old) * adv / B
+    ptr = torch.tensor([0, B // 2, B], dtype=torch.int32, device=z.device)
+    sums = np.array([lp[:B // 2].sum(), lp[B // 2:].sum()])
+    slope = 0.1 * (1 / (1 + math.exp(-0.1 * (sums[0] - sums[1]))) - 1)
+    pair = np.where(np.arange(B) < B // 2, slope, -slope)
+    err = 0.1 / 4 * el(C, lp).sum() / el(C, 0.0)  # of the slope, in the coefficients' own unit
+    policy = lambda **kw: L1.policy_loss(z, labels, vec(old), vec(adv), clip_high=0.3, **kw)  # noqa: E731
+    prefer = lambda **kw: L1.preference_loss(z, labels, ptr, beta=0.1, **kw)  # noqa: E731
+    for f, want, scale in ((policy, coef, size), (prefer, pair, 0.1 * (1 + err) * ones)):
+        plain = f()
+        for s in (2.0 ** 12, 0.3, -4.0):
+            got = f(grad_scale=s)
+            assert torch.equal(got[0], plain[0]) and torch.equal(got[2], plain[2])  # the loss and the log-probabilities are not scaled
+            s32 = float(np.float32(s))
+            check_dz(got[1], p, lab, want * s32, scale * abs(s32), C, lp, dtype)
+        assert torch.equal(f(grad_scale=1.0)[1], plain[1]) and not bool(f(grad_scale=0.0)[1].any())
+        if dtype == "float32":
+            assert torch.equal(f(grad_scale=2.0 ** 12)[1], plain[1] * 2.0 ** 12)  # a power of two changes no bit
+        if dtype == "float16" and C == 32768:
+            lost = float((plain[1] == 0).float().mean())
+            kept = float((f(grad_scale=2.0 ** 12)[1] == 0).float().mean())
+            assert lost > 0.1 and kept < lost / 10
+    for bad in (float("nan"), float("inf")):
+        for f in (policy, prefer):
+            with pytest.raises(L1.L1CSRError):
+                f(grad_scale=bad)

@@ -231,3 +231,14 @@ def test_columns_of_one_buffer_are_no_overlap(lib):
     assert muon(lib, G=at(34), **mixed) == EINVAL
     # rows of other lengths: refused where the extents meet
     assert muon(lib, G=at(0), ldg=24, O=at(32), ldo=25, M=None, M_out=None) == EINVAL
+
+
+@pytest.mark.skipif(not NO_GPU, reason="validation calls use placeholder pointers; run without a GPU")
+def test_gradient_factors_that_are_refused(lib):
+    far = C.c_void_p(1 << 45)
+    for s, fine in ((1.0, True), (-65536.0, True), (0.0, True), (nan, False), (inf, False), (-inf, False)):
+        # (a sound call is not refused: the launch itself fails where there is no GPU)
+        rc = lib.l1csr_policy_loss_scaled(8, 8, 2, P, 8, Q, Q, Q, None, None, 0.2, 0.2, 0.1, s, R, 8, None, far, W, BIG, None)
+        assert (rc != EINVAL) == fine, s
+        rc = lib.l1csr_preference_loss_scaled(8, 8, 2, P, 8, Q, 2, Q, None, None, 0.1, 0.0, s, R, 8, None, far, W, BIG, None)
+        assert (rc != EINVAL) == fine, s
