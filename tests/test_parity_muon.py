@@ -724,3 +724,77 @@ def test_step_takes_the_states_precision():
     assert not torch.equal(updates[L1.F32], updates[L1.F16])
     with pytest.raises(ValueError):
         L1.prox_muon_step(W, G, L1.MuonState.zeros((N, K), "cuda", precision=L1.BF16X3), 0.02, 0.05)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("nesterov", [0, 1])
+@pytest.mark.parametrize("N,K", FORMS)
+def test_momentum_read_but_not_stored(N, K, nesterov, dtype):
+    # muon_update with M and without M_out: the update of the call that stores it, and M as it was
+    torch = _torch()
+    G = (gradient(N, K, 1) * 1e3).to(getattr(torch, dtype))
+    code = {"float32": 0, "bfloat16": 1}[dtype]
+    M = torch.full((N, K + 3), 9.0, device="cuda")
+    M[:, :K] = gradient(N, K, 2) * 1e3
+    before = M.clone()
+    for precision, op in ((L1.F32, L1.OP_MUON), (L1.F16, L1.OP_MUON_F16)):
+        out, new = [torch.empty_like(G) for _ in range(2)], torch.empty((N, K), device="cuda")
+        n = L1.workspace_bytes(op, N, K, 0, 0)
+        ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+        for O, store in zip(out, (None, new)):
+            assert L1.lib().muon_update(N, K, code, G.data_ptr(), K, M.data_ptr(), K + 3, None if store is None else store.data_ptr(),
+                                        K, 0.9, nesterov, 5, 1e-7, 1.0, precision, O.data_ptr(), K, ws.data_ptr(), n,
+                                        torch.cuda.current_stream().cuda_stream) == L1.OK
+        assert torch.equal(out[0], out[1]) and torch.equal(M, before)
+        m64 = 0.9 * M[:, :K].double() + G.double()
+        assert rel(new, m64) <= 2.0 ** -22
+        U = (G.double() + 0.9 * new.double()) if nesterov else new.double()
+        want = steps_of(U)
+        tol = 4.9e-3 if precision == L1.F16 else bound(U.float(), want) + 2.0 ** -22
+        assert rel(out[0], want) <= tol + HALF_STEP[dtype]
+
+
+def _quintic(x):
+    return A * x + B * x ** 3 + C * x ** 5
+
+
+@pytest.mark.parametrize("steps", [8, 9, 12, 16, 20])
+@pytest.mark.parametrize("N,K", [(15, 30), (96, 128), (300, 98), (98, 5000), (300, 784), (700, 302), (602, 2000), (1100, 1100)])
+def test_many_steps_of_equal_singular_values(N, K, steps):
+    """Orthonormal rows (columns): every singular value is s = m^(-1/2) at first and runs through the quintic, and the matrix is
+    f^k(s) Q.  An error of the matrix grows by |f'(s)| (in directions that change singular values) or f(s) / s (in those that
+    turn vectors) a step, with 18 e^2 of its square (|f''| / 2 <= 18 up to 1.2); a step adds 16 roundings of 2^-23 of its three
+    terms (operands as parts, sums, stored parts), the input and its norm 2^-22."""
+    torch = _torch()
+    m = min(N, K)
+    gen = torch.Generator().manual_seed(N + K)
+    Q = torch.linalg.qr(torch.randn((max(N, K), m), generator=gen, dtype=torch.float64))[0].cuda()
+    Q = (Q if N >= K else Q.t()).contiguous()
+    s, e = m ** -0.5, m ** -0.5 * 2.0 ** -22
+    for _ in range(steps):
+        slope = abs(A + 3 * B * s * s + 5 * C * s ** 4)
+        e = max(slope, abs(_quintic(s) / s)) * e + 18 * e * e + 16 * 2.0 ** -23 * (A * s - B * s ** 3 + C * s ** 5)
+        s = _quintic(s)
+    assert e / s <= 0.02  # (a step more or less is off by far more)
+    got = L1.orthogonalize(Q.float() * 3.0, steps=steps, eps=0.0)
+    assert rel(got, s * Q) <= e / s
+
+
+@pytest.mark.parametrize("precision", [L1.F32, L1.F16])
+@pytest.mark.parametrize("N,K", [(20, 33), (60, 128), (300, 70), (100, 5000), (200, 784), (250, 900), (600, 2000)])
+def test_most_steps(N, K, precision):
+    """L1CSR_MUON_MAX_STEPS steps of any matrix.  The quintic maps [0.681, 1.204] (its lowest value past the first maximum, at
+    1.050, and that maximum, at 0.554) into itself and lifts smaller values by 3.4 a step, so all singular values end there, a
+    step's roundings aside: 16 2^-23 (two parts) or 3 2^-11 (one part) of three terms of 10.3 at most.  The singular vectors stay,
+    so G O^T is symmetric: an error that turns vectors grows by (f(s) + f(t)) / (s + t) a step, a product that telescopes to
+    1.204 / 0.681 at most, and a step's roundings add 16 2^-23 10.3 / 0.681."""
+    torch = _torch()
+    G = torch.randn((N, K), device="cuda", generator=torch.Generator(device="cuda").manual_seed(N))
+    O = L1.orthogonalize(G, steps=L1.MUON_MAX_STEPS, precision=precision).double()
+    one = precision == L1.F16 and min(N, K) > 128
+    step = (3 * 2.0 ** -11 if one else 16 * 2.0 ** -23) * 10.3
+    sv = torch.linalg.svdvals(O.cpu())
+    assert 0.681 - step <= float(sv.min()) and float(sv.max()) <= 1.204 + step
+    if not one:
+        P = (G.double() @ O.t().contiguous()) if N <= K else (O.t().contiguous() @ G.double())
+        assert float((P - P.t()).norm() / P.norm()) <= L1.MUON_MAX_STEPS * step / 0.681 * (1.204 / 0.681)

@@ -438,3 +438,114 @@ def test_scaled_gradients(C, B, dtype):
         for f in (policy, prefer):
             with pytest.raises(L1.L1CSRError):
                 f(grad_scale=bad)
+
+
+# few tokens of a large vocabulary: a column at a time (fewer columns than a vector has values), many ranges of classes
+FEW = [(50257, 1), (50257, 3), (131072, 1), (131071, 3), (40001, 2), (131072, 7)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("C,B", FEW)
+def test_few_tokens_count_every_class_once(C, B, dtype):
+    """Equal logits: every exponential is 1 and their sum the integer C, exact in fp32 (below 2^24) in any order, so lp is
+    -log C but for the logarithm's and one subtraction's rounding, 2^-22 (1 + log C) < 3.1e-6.  A class left out or counted
+    twice moves it by 1 / C >= 7.6e-6.  Another class a token, raised by 20: its own place in the sum."""
+    torch = _torch()
+    labels = torch.full((B,), C // 2, dtype=torch.int32, device="cuda")
+    z = torch.empty((C, B), dtype=getattr(torch, dtype), device="cuda")
+    z[:] = torch.tensor([-3.0, 0.0, 5.0, 1.0, 2.0, 64.0, -64.0][:B], device="cuda")
+    tol = 2.0 ** -22 * (1 + math.log(C))
+    lp = h(L1.token_logp(z, labels)).astype(np.float64)
+    assert (np.abs(lp + math.log(C)) <= tol).all()
+    old, adv = vec(lp), vec(np.ones(B))
+    st, dz, _ = L1.policy_loss(z, labels, old, adv, grad_scale=2.0 ** 10)
+    # dz = 2^10 / B (1 / C - [c = a]): the ratio and 1 / C are within tol, dz rounds once
+    want = np.full(C, 1.0 / C)
+    want[C // 2] -= 1
+    want *= 2.0 ** 10 / B
+    err = np.abs(want) * (4 * tol + HALF_STEP[dtype]) + TINY[dtype]
+    assert (np.abs(dz.cpu().double().numpy() - want[:, None]) <= err[:, None]).all()
+    # one class far above the others: e^20 of the sum
+    for c in (0, 1, 255, 256, 2010, 2011, C // 3, C - 257, C - 256, C - 2, C - 1):
+        x = z.clone()
+        x[c] += 20
+        x64 = x.double()  # (the raised value as its type holds it)
+        raised = (x64[c] - x64[C // 2]).cpu().numpy()
+        S = np.exp(raised) + C - 1
+        got = h(L1.token_logp(x, labels)).astype(np.float64)
+        assert (np.abs(got + np.log(S)) <= el(512, np.log(S))).all(), c
+
+
+def check_dz_of_depth(got, p, labels, coef, scale, depth, lp, dtype):
+    """check_dz with the sums' error that of `depth` terms, whatever the number of classes."""
+    C, B = p.shape
+    want = ref_dz(p, labels, coef)
+    got = got.detach().cpu().double().numpy()
+    with np.errstate(divide="ignore"):
+        ep = es(depth) + (np.abs(np.log(np.maximum(p, 1e-300))) + 4) * 2.0 ** -22
+    own = np.zeros_like(p)
+    own[labels, np.arange(B)] = 1.0
+    tol = np.abs(own - p) * scale * 4 * (el(depth, lp) + 2.0 ** -22) + np.abs(coef) * (p * ep + own * el(depth, lp))
+    tol = tol + np.abs(want) * HALF_STEP[dtype] * 1.001 + TINY[dtype]
+    bad = np.abs(got - want) > tol
+    assert not bad.any(), (int(bad.sum()), np.argwhere(bad)[0], got[bad][0], want[bad][0], tol[bad][0])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("C,B", FEW)
+def test_few_tokens_of_a_large_vocabulary(C, B, dtype):
+    """Against the formula, with a sum's real depth: 8 rows at a time in a thread, at most 256 threads and 64 ranges joined."""
+    torch = _torch()
+    z, labels, z64, lab = logits(C, B, dtype, seed=C - B, pad=1)
+    every = np.ones(B, bool)
+    lp, p = ref_logp(z64, lab, every)
+    tol = el(256, lp)  # (2 * 256 + 16) 2^-24
+    assert (np.abs(h(L1.token_logp(z, labels)).astype(np.float64) - lp) <= tol).all()
+    old, adv = (lp - 0.05).astype(np.float32), np.linspace(-1, 1, B).astype(np.float32) + 0.125
+    ref = (lp + 0.3).astype(np.float32)
+    stats, coef = ref_policy(lp, every, np.ones(B), old.astype(np.float64), adv.astype(np.float64), ref.astype(np.float64), 0.2,
+                             0.3, 0.1)
+    st, dz, got = L1.policy_loss(z, labels, vec(old), vec(adv), ref_logp=vec(ref), kl_coef=0.1, clip_high=0.3, grad_scale=256.0)
+    assert (np.abs(h(got).astype(np.float64) - lp) <= tol).all()
+    assert (np.abs(h(st).astype(np.float64) - stats) <= 16 * tol.max() + 2.0 ** -22 * (1 + np.abs(stats))).all()
+    size = (np.exp(lp - old) * np.abs(adv) + 0.1 * (np.expm1(ref - lp) + 1)) / B
+    check_dz_of_depth(dz, p, lab, coef * 256, size * 256, 256, lp, dtype)
+    ptr = torch.tensor([0, (B + 1) // 2, B], dtype=torch.int32, device=z.device)
+    loss, dz, rew = L1.preference_loss(z, labels, ptr, beta=0.1, grad_scale=256.0)
+    sums = np.array([lp[:(B + 1) // 2].sum(), lp[(B + 1) // 2:].sum()])
+    D = 0.1 * (sums[0] - sums[1])
+    assert (np.abs(h(rew).astype(np.float64) - 0.1 * sums) <= 0.1 * tol.sum() + 2.0 ** -22 * np.abs(0.1 * sums)).all()
+    assert abs(float(loss) - np.logaddexp(0, -D)) <= 0.1 * tol.sum() + 2.0 ** -22 * (1 + abs(D))
+    slope = 0.1 * (1 / (1 + math.exp(-D)) - 1)
+    coef = np.where(np.arange(B) < (B + 1) // 2, slope, -slope)
+    scale = 0.1 * (1 + 0.1 / 4 * tol.sum() / el(256, 0.0)) * np.ones(B)
+    check_dz_of_depth(dz, p, lab, coef * 256, scale * 256, 256, lp, dtype)
+
+
+@pytest.mark.parametrize("C,B", [(20, 16), (4099, 16), (3000, 40)])
+def test_offsets_outside_the_tokens(C, B):
+    """Offsets beyond [0, B] or falling back, through the one-workgroup kernel and the pair pass: a pair reads lo = seq[2p]
+    clamped to [0, B], mid = seq[2p + 1] to [lo, B], hi = seq[2p + 2] to [mid, B]; nothing outside dlogits is written."""
+    torch = _torch()
+    z, labels, z64, lab = logits(C, B, "float32", seed=2)
+    lp, _ = ref_logp(z64, lab, np.ones(B, bool))
+    guard = torch.full((C + 2, B + 6), 7.0, device=z.device)
+    dz = guard[1:-1, 3:-3]
+    big = 2 ** 31 - 1
+    for bad in ([-5, 4, 2, 99, 7], [big, -big, big, 0, -1], [3, 1, -4, -9, big], [-big, big, -big, 5, 9]):
+        _, _, rew = L1.preference_loss(z, labels, torch.tensor(bad, dtype=torch.int32, device=z.device), beta=0.5, dlogits=dz)
+        want, err = [], []
+        inside = np.zeros(B, bool)
+        for q in range(2):
+            lo = min(max(bad[2 * q], 0), B)
+            mid = min(max(bad[2 * q + 1], lo), B)
+            hi = min(max(bad[2 * q + 2], mid), B)
+            want += [0.5 * lp[lo:mid].sum(), 0.5 * lp[mid:hi].sum()]
+            err += [0.5 * el(C, lp)[lo:mid].sum(), 0.5 * el(C, lp)[mid:hi].sum()]
+            inside[lo:hi] = True
+        want = np.array(want)
+        assert (np.abs(h(rew).astype(np.float64) - want) <= np.array(err) + 2.0 ** -22 * np.abs(want)).all(), bad
+        assert bool(torch.isfinite(dz).all()) and not bool(dz[:, torch.from_numpy(~inside).to(z.device)].any())
+        edge = guard.clone()
+        edge[1:-1, 3:-3] = 7.0
+        assert bool((edge == 7).all())
