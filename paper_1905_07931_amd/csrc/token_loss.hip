@@ -223,6 +223,20 @@ __device__ __forceinline__ float policy_token(const policy_args &P, const float 
     return wt * dlp;
 }
 
+// A token's coefficient times the factor of all of them (grad_scale over the sum of weights), in double where that
+// is no normal float: weights of any size enter by their shares, and a token that does not count keeps 0.
+struct coef_scale {
+    double wide;
+    float narrow;
+    bool normal;
+    __device__ __forceinline__ explicit coef_scale(double x)
+        : wide(x), narrow((float)x), normal(fabsf(narrow) >= 0x1p-126f && fabsf(narrow) < INFINITY) {}
+    __device__ __forceinline__ float operator()(float coef) const {
+        if (coef == 0.f) return 0.f;
+        return normal ? coef * narrow : (float)(coef * wide);
+    }
+};
+
 // A pair's loss, its rewards given, and d loss / d (sum of the preferred sequence), which is minus the other's
 struct pair_terms {
     double loss, slope;
@@ -376,8 +390,8 @@ __global__ __launch_bounds__(kThreads) void gradient_kernel(int C, int B, const 
                                                             float grad_scale, float *__restrict__ out) {
     constexpr int U = 4;
     __shared__ double lds[kThreads / kWave];
-    const float scale =
-        (float)(grad_scale * finish<KIND>(n_sums, t.sums, kl_coef, lds, blockIdx.x == 0 && blockIdx.y == 0, out));
+    const coef_scale scale(grad_scale *
+                           finish<KIND>(n_sums, t.sums, kl_coef, lds, blockIdx.x == 0 && blockIdx.y == 0, out));
     const int TX = 1 << g.tx_shift, TY = kThreads >> g.tx_shift;
     const int tx = threadIdx.x & (TX - 1), ty = threadIdx.x >> g.tx_shift;
     const columns<V> k(tx, g.tx_shift, B);
@@ -389,7 +403,7 @@ __global__ __launch_bounds__(kThreads) void gradient_kernel(int C, int B, const 
     bool work = false;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        const float coef = t.coef[k.at + v] * scale;
+        const float coef = scale(t.coef[k.at + v]);
         const bool on = coef != 0.f;
         m[v] = on ? t.m[k.at + v] : 0.f;
         f[v] = on ? -coef * t.inv[k.at + v] : 0.f;
@@ -449,7 +463,7 @@ __global__ __launch_bounds__(kThreads) void gradient_kernel(int C, int B, const 
     for (int v = 0; v < V; ++v) {
         const int b = k.at + v, a = labels[b];
         if (!k.mine(v) || a < c0 || a >= c1 || (a - c0) % TY != ty) continue;
-        const float coef = t.coef[b] * scale;
+        const float coef = scale(t.coef[b]);
         if (coef != 0.f) dz[(int64_t)a * ldd + b] = (T)(-coef * expm1f(t.lp[b]));
     }
 }
@@ -529,7 +543,7 @@ __global__ __launch_bounds__(kSmallThreads) void small_loss_kernel(token_loss_ar
         }
     }
     if constexpr (KIND == kLogp) return;
-    float scale = a.grad_scale;
+    double factor = a.grad_scale;
     if constexpr (KIND == kPolicy) {
         const double sw = sum(ps.weight), inv = sw != 0 ? 1 / sw : 0.0;
         const double pg = sum(ps.pg) * inv, kl = sum(ps.kl) * inv, off = sum(ps.off) * inv;
@@ -539,7 +553,7 @@ __global__ __launch_bounds__(kSmallThreads) void small_loss_kernel(token_loss_ar
             a.out[2] = (float)kl;
             a.out[3] = (float)off;
         }
-        scale = (float)(a.grad_scale * inv);
+        factor *= inv;
     } else {
         __syncthreads();
         double loss = 0;
@@ -576,7 +590,7 @@ __global__ __launch_bounds__(kSmallThreads) void small_loss_kernel(token_loss_ar
     }
     if (a.dlogits == nullptr || tx >= B) return;
     __syncthreads();
-    const float coef = tcoef[tx] * scale, f = coef != 0.f ? -coef * tinv[tx] : 0.f;
+    const float coef = coef_scale(factor)(tcoef[tx]), f = coef != 0.f ? -coef * tinv[tx] : 0.f;
     const float own = coef != 0.f ? -coef * expm1f(tlp[tx]) : 0.f;
     const int label = a.labels[tx];
     T *dz = static_cast<T *>(a.dlogits) + tx;

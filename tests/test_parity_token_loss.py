@@ -549,3 +549,30 @@ def test_offsets_outside_the_tokens(C, B):
         edge = guard.clone()
         edge[1:-1, 3:-3] = 7.0
         assert bool((edge == 7).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("C,B", [(10, 64), (1000, 64)])
+@pytest.mark.parametrize("e", [-131, -120, 122, 126])
+def test_weights_of_any_size(C, B, e, dtype):
+    """Weights enter by their shares: all of them times 2^e changes nothing, also where their sum's inverse is no normal float.
+    (At 2^-131 the weights themselves hold 18 bits or more, their products with a gradient of 2^-2 or more 16: 2^-17 off.)"""
+    torch = _torch()
+    z, labels, z64, lab = logits(C, B, dtype, seed=12)
+    lp, p = ref_logp(z64, lab, np.ones(B, bool))
+    old = vec(lp - 0.05)
+    adv = vec(np.linspace(0.5, 1, B) * np.where(np.arange(B) % 2, 1, -1))
+    w = np.linspace(1, 1.9, B).astype(np.float32)
+    w[::5] = 0
+    st, dz, _ = L1.policy_loss(z, labels, old, adv, weights=vec(w), clip_high=0.3)
+    st2, dz2, _ = L1.policy_loss(z, labels, old, adv, weights=vec(np.ldexp(w, e)), clip_high=0.3)
+    assert not bool(dz2[:, ::5].any()) and bool(dz[:, 1::5].any())
+    tol = 2.0 ** -17 if e == -131 else 2.0 ** -21  # (a few roundings of 2^-24)
+    a, b = dz.cpu().double().numpy(), dz2.cpu().double().numpy()
+    # both round to the type: half a step each, beside the weights'
+    assert (np.abs(a - b) <= np.abs(a) * (tol + 2.002 * HALF_STEP[dtype]) + 2 * TINY[dtype]).all()
+    assert (np.abs(h(st) - h(st2)) <= tol * (1 + np.abs(h(st)))).all()
+    # a factor that only the products can hold
+    st3, dz3, _ = L1.policy_loss(z, labels, old, adv, weights=vec(np.ldexp(w, e)), clip_high=0.3, grad_scale=2.0 ** 10)
+    c = dz3.cpu().double().numpy() / 2.0 ** 10
+    assert (np.abs(a - c) <= np.abs(a) * (tol + 2.002 * HALF_STEP[dtype]) + 2 * TINY[dtype]).all() and not dz3[:, ::5].any()
