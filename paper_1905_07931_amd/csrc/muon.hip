@@ -890,8 +890,8 @@ __device__ __forceinline__ void finish_block(const product_args &P, int gi, int 
 // three ahead of the one in use; fragments are read in the lane's order, the next step's while this one's
 // are multiplied (five steps of 4096 x 4096, read behind the barrier and ahead: two parts 3875 and 3690 us, one
 // part 1632 and 1553).  With two parts a wave reads 8 fragments for 12 matrix instructions and the pipe is
-// 74 % busy at the 1.64 GHz that the power limit leaves (4096 x 4096 x 4096: 348 us, 1.18 PFLOP/s of
-// fp16); with one part 6 for 8, 56 % busy at 1.93 GHz, 139 us (0.99 PFLOP/s), where all workgroups
+// 74-77 % busy at the 1.6 GHz that the power limit leaves (4096 x 4096 x 4096: 348 us, 1.18 PFLOP/s of
+// fp16); with one part 6 for 8, 56-59 % busy at 1.9 GHz, 139 us (0.99 PFLOP/s), where all workgroups
 // start and end together and the result's 10 bytes an element are waited for.
 template <int NP, typename S, typename O>
 __global__ __launch_bounds__(S::threads, 2) void product_kernel(product_args P) {
@@ -1258,7 +1258,7 @@ hipError_t launch_tiles(product_args P, int most, int least, hipStream_t s) {
 // Few blocks take a workgroup each: us for five steps with small tiles and with blocks, two parts 300 x 784 125 and 102,
 // 512 x 512 137 and 109, 700 x 700 (484 blocks and 253) 155 and 126; up to 800 blocks 850 x 850 162 -> 188; one part
 // 300 x 784 102 and 83, 700 x 700 119 and 107.  A long reduction wants more workgroups, ranges of small tiles:
-// 200 x 9216 (28 blocks of 576 steps) 137 and 160, but 300 x 4096 bf16 (256 steps) 136 and 126.
+// 200 x 9216 (28 blocks of 576 steps) 137 and 160, but one part 300 x 4096 (256 steps) 136 and 126.
 // The others by the number of large tiles.  us for five steps, every product with small, medium and large tiles, two parts:
 // 700 x 700 159, 217, 324; 1001 x 1777 242, 328, 353; 1500 x 1500 485, 438, 457; 2048 x 2048 895, 725, 754; 2500 x 2500 1472,
 // 1177, 1124 (and 1150 as chosen: the symmetric ones, 210 large tiles, medium); 3500 x 3500 3410, 2765, 2586.  One
