@@ -15,6 +15,9 @@
  *   orthogonalised     momentum and its prox step muon_update
  *   conv layers        direct sparse convolution  csr_conv_fwd, csr_conv_bwd_data, conv_im2col
  *   losses             cross-entropy, policy, preference  l1csr_softmax_xent, l1csr_policy_loss, l1csr_preference_loss
+ *   around the layers  embedding, its gradients  l1csr_embedding_fwd, l1csr_embedding_bwd, l1csr_embedding_masked_bwd
+ *                      norms, gate and residual  l1csr_residual_norm_fwd, l1csr_residual_norm_bwd
+ *   before a solver    global norm and clipping  l1csr_grad_norm, l1csr_clip_grad_norm
  *
  * Conventions shared by every call
  *   - CSR: row_ptr[n_rows+1] (row_ptr[0] = 0, non-decreasing), col_idx[nnz]
@@ -69,7 +72,7 @@ enum l1csr_precision {
     L1CSR_F16 = 3            /* muon_update: operands rounded to fp16, one exact product, fp32 sums */
 };
 
-/* element types of the calls that take more than float (muon_update, the losses over logits) */
+/* element types of the calls that take more than float (muon_update, the losses over logits, embedding, norms, clipping) */
 enum l1csr_dtype {
     L1CSR_DTYPE_F32 = 0,
     L1CSR_DTYPE_BF16 = 1,
@@ -105,7 +108,11 @@ enum l1csr_op {
     L1CSR_OP_PROX_DENSE = 13,   /* prox_adaptive_recompress, dense result kept (nnz, B unused) */
     L1CSR_OP_MUON = 14,         /* muon_update, L1CSR_F32 (nnz, B unused) */
     L1CSR_OP_MUON_F16 = 15,     /* muon_update, L1CSR_F16 */
-    L1CSR_OP_TOKEN_LOSS = 16    /* l1csr_token_logp / _policy_loss / _preference_loss: n_rows = C, n_cols = pairs, B */
+    L1CSR_OP_TOKEN_LOSS = 16,   /* l1csr_token_logp / _policy_loss / _preference_loss: n_rows = C, n_cols = pairs, B */
+    L1CSR_OP_EMBEDDING_PLAN = 17, /* the plan of l1csr_embedding_plan: n_rows = V, B (n_cols, nnz unused) */
+    L1CSR_OP_EMBEDDING_BWD = 18,  /* l1csr_embedding_bwd / _masked_bwd: n_rows = V, n_cols = D, B */
+    L1CSR_OP_RESIDUAL_NORM = 19,  /* l1csr_residual_norm_fwd / _bwd: n_rows = K, B */
+    L1CSR_OP_GRAD_NORM = 20       /* l1csr_grad_norm / l1csr_clip_grad_norm: n_rows = number of tensors */
 };
 
 /* Human-readable name of a status code (static string, never NULL). */
@@ -693,6 +700,102 @@ int l1csr_preference_loss_scaled(int32_t C, int32_t B, int dtype, const void *lo
                                  int32_t pairs, const int32_t *seq_ptr, const float *ref_logp, const float *weights,
                                  float beta, float label_smoothing, float grad_scale, void *dlogits, int64_t ldd,
                                  float *rewards, float *loss, void *ws, size_t ws_bytes, hipStream_t stream);
+
+/*
+ * Embedding: rows of a table E[V][D] (features contiguous, as a layer's weights) as columns of the activations
+ * X[D][B], for tokens[B] (device int32):
+ *     X[d][b] = scale E[tokens[b]][d];   0 where tokens[b] lies outside [0, V) (padding)
+ * Such tokens take no part in the gradients either.  D = the inputs of the first layer; a table tied to the
+ * output layer is that layer's W[C][K] (V = C, D = K).  scale is finite.
+ *
+ * l1csr_embedding_fwd: E of `dtype`, X of x_dtype: the same or fp32; one rounding.
+ * l1csr_embedding_csr_fwd: the table kept in CSR (V x D, fp32); X fp32.
+ * l1csr_embedding_plan: the tokens' order (by token, then by position), which the gradients add up in, into the
+ *   caller's buffer plan of l1csr_workspace_bytes(L1CSR_OP_EMBEDDING_PLAN, V, 0, 0, B) bytes.  The plan depends on
+ *   the tokens, V and B only; the calls that take it get the same V and B and run behind it.
+ * l1csr_embedding_bwd: the dense gradient, every row of it,
+ *     dE[v][d] = add[v][d] + scale sum_{b: tokens[b] = v} dX[d][b]
+ *   dX of `dtype`; dE and add (NULL: 0) of e_dtype, the same or fp32.  add may be dE itself (with the same leading
+ *   dimension): the gradient is added in place, and rows without tokens are neither read nor written.  Sums are
+ *   fp32, in an order that the tokens fix; rounded once.
+ * l1csr_embedding_masked_bwd: the gradient on the pattern of a table kept in CSR (debiasing, as sddmm_masked_wgrad),
+ *     gv[p] = scale sum_{b: tokens[b] = row of p} dX[col_idx[p]][b]
+ * ws, 16-byte aligned, as l1csr_workspace_bytes(L1CSR_OP_EMBEDDING_BWD, V, D, 0, B).  No output may overlap an
+ * input (add = dE aside).  V, D <= 2^30 and B <= 2^24 (L1CSR_EUNSUPPORTED).  Results are reproducible.
+ */
+int l1csr_embedding_fwd(int32_t V, int32_t D, int32_t B, int dtype, const void *E, int64_t lde, const int32_t *tokens,
+                        float scale, int x_dtype, void *X, int64_t ldx, hipStream_t stream);
+int l1csr_embedding_csr_fwd(int32_t V, int32_t D, int64_t nnz, const int32_t *row_ptr, const int32_t *col_idx,
+                            const float *vals, int32_t B, const int32_t *tokens, float scale, float *X, int64_t ldx,
+                            hipStream_t stream);
+int l1csr_embedding_plan(int32_t V, int32_t B, const int32_t *tokens, void *plan, size_t plan_bytes, hipStream_t stream);
+int l1csr_embedding_bwd(int32_t V, int32_t D, int32_t B, int dtype, const void *dX, int64_t lddx, const void *plan,
+                        size_t plan_bytes, float scale, int e_dtype, const void *add, int64_t ldadd, void *dE, int64_t ldde,
+                        void *ws, size_t ws_bytes, hipStream_t stream);
+int l1csr_embedding_masked_bwd(int32_t V, int32_t D, int64_t nnz, const int32_t *row_ptr, const int32_t *col_idx, int32_t B,
+                               const float *dX, int64_t lddx, const void *plan, size_t plan_bytes, float scale, float *gv,
+                               void *ws, size_t ws_bytes, hipStream_t stream);
+
+/*
+ * The norms before and after a block with its gate and its residual, per token (column) of activations [K][B]:
+ *     n  = y / sqrt(mean_k y^2 + eps) post_gain      (y itself without post_gain)
+ *     r' = r + alpha a(gate) n
+ *     h  = r' / sqrt(mean_k r'^2 + eps) pre_gain     (left out without pre_gain)
+ * r is the residual, y the block's output, h the next block's input.  y NULL: r' = r, the norm alone (r_out NULL).
+ * All matrices are of `dtype`; the gains float [K].  gate_kind: L1CSR_GATE_NONE (a = 1), L1CSR_GATE_ROW (gate is
+ * float [K], one for all tokens) or L1CSR_GATE_FULL (gate [K][ldg] of `dtype`); a(g) = g, or the logistic function
+ * of g with gate_sigmoid.  h comes from the unrounded r'.  Sums are in double; eps > 0, alpha finite.
+ * r_out and h may each be r or y themselves (with the same leading dimension), but not each other.
+ *
+ * l1csr_residual_norm_bwd: from r_out (r' as stored; pre_gain given), dr_out (d loss / d r' from its further uses; NULL: 0,
+ * with pre_gain only) and dh (with pre_gain only):
+ *     t  = dr_out + d(h) / d(r') dh;   dr = t   (d loss / d r as well)
+ *     dy, dgate, dpost_gain [K], dpre_gain [K]: d loss / d of what was given, summed over the tokens where it is
+ *     one for all of them
+ * dr may be NULL without pre_gain (t is dr_out).  dr may be dr_out or dh itself, dy y itself and dgate the gate
+ * itself (with the same leading dimensions).  Each value is rounded once.
+ * No output may overlap an input or an output otherwise (columns of one buffer do not).  ws, 16-byte aligned, as
+ * l1csr_workspace_bytes(L1CSR_OP_RESIDUAL_NORM, K, 0, 0, B).  K, B <= 2^24 (L1CSR_EUNSUPPORTED).  Results are
+ * reproducible.
+ */
+enum l1csr_gate {
+    L1CSR_GATE_NONE = 0,
+    L1CSR_GATE_ROW = 1,
+    L1CSR_GATE_FULL = 2
+};
+int l1csr_residual_norm_fwd(int32_t K, int32_t B, int dtype, const void *r, int64_t ldr, const void *y, int64_t ldy,
+                            int gate_kind, int gate_sigmoid, const void *gate, int64_t ldg, const float *post_gain,
+                            const float *pre_gain, float alpha, float eps, void *r_out, int64_t ldro, void *h, int64_t ldh,
+                            void *ws, size_t ws_bytes, hipStream_t stream);
+int l1csr_residual_norm_bwd(int32_t K, int32_t B, int dtype, const void *r_out, int64_t ldr, const void *dr_out, int64_t lddro,
+                            const void *dh, int64_t lddh, const void *y, int64_t ldy, int gate_kind, int gate_sigmoid,
+                            const void *gate, int64_t ldg, const float *post_gain, const float *pre_gain, float alpha,
+                            float eps, void *dr, int64_t lddr, void *dy, int64_t lddy, void *dgate, int64_t lddg,
+                            float *dpost_gain, float *dpre_gain, void *ws, size_t ws_bytes, hipStream_t stream);
+
+/*
+ * The norm of n gradients taken together, and their clipping to it, between the gradients and a solver:
+ *     norm = sqrt(sum over all tensors and entries of g^2) / grad_scale
+ *     l1csr_clip_grad_norm:  f = min(1, max_norm / (norm + eps)) / grad_scale,   out = f g
+ * grads, rows, cols, ld, dtype are HOST arrays of n values, read before the call returns: tensor i is [rows][ld] of
+ * dtype[i] (l1csr_dtype), cols of each row used (a vector or a whole buffer is one row).  out (HOST array of device
+ * pointers; NULL: in place) with ld_out (NULL: cols) and dtype_out (NULL: dtype; each the tensor's type or fp32)
+ * takes the results.  grad_scale > 0 is a factor that the gradients hold (the losses' grad_scale, a power of two
+ * best): it is taken out.  stats[2] (device) = norm, f (l1csr_grad_norm: norm, 1 / grad_scale).
+ * max_norm >= 0 (infinity: no limit), eps > 0.  Squares and their sum are in double, f multiplies in double, one
+ * rounding.  A norm that is not finite gives what the formula gives (an infinite one 0 or NaN, NaN everywhere for a
+ * NaN); with zero_nonfinite != 0 it gives f = 0 and zeros everywhere instead, so that nothing of such a step
+ * reaches the momentum or the weights.  No tensors: norm 0.
+ * A result may be its own tensor (same type and leading dimension), but nothing written may overlap anything else
+ * (L1CSR_EINVAL; a tensor given twice and columns of one buffer that cross are refused).
+ * ws, 16-byte aligned, as l1csr_workspace_bytes(L1CSR_OP_GRAD_NORM, n, 0, 0, 0).  Results are reproducible.
+ */
+int l1csr_grad_norm(int32_t n, const void *const *grads, const int64_t *rows, const int64_t *cols, const int64_t *ld,
+                    const int32_t *dtype, float grad_scale, float *stats, void *ws, size_t ws_bytes, hipStream_t stream);
+int l1csr_clip_grad_norm(int32_t n, const void *const *grads, const int64_t *rows, const int64_t *cols, const int64_t *ld,
+                         const int32_t *dtype, void *const *out, const int64_t *ld_out, const int32_t *dtype_out,
+                         float max_norm, float grad_scale, float eps, int zero_nonfinite, float *stats, void *ws,
+                         size_t ws_bytes, hipStream_t stream);
 
 #ifdef __cplusplus
 }

@@ -27,6 +27,8 @@ __all__ = [
     "csr_spmm_bwd_t_plan", "csr_spmm_bwd_t_planned",
     "token_logp", "policy_loss", "preference_loss", "F16", "MuonState", "orthogonalize", "prox_muon_step",
     "prox_muon_recompress",
+    "embedding_fwd", "EmbeddingPlan", "embedding_plan", "embedding_bwd", "embedding_masked_bwd",
+    "residual_norm_fwd", "residual_norm_bwd", "ResidualNormGrads", "grad_norm", "clip_grad_norm",
 ]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libl1csr.so")
@@ -47,6 +49,11 @@ OP_PROX_DENSE = 13
 OP_MUON = 14
 OP_MUON_F16 = 15
 OP_TOKEN_LOSS = 16
+OP_EMBEDDING_PLAN = 17
+OP_EMBEDDING_BWD = 18
+OP_RESIDUAL_NORM = 19
+OP_GRAD_NORM = 20
+GATE_NONE, GATE_ROW, GATE_FULL = 0, 1, 2
 MUON_MAX_STEPS = 32  # L1CSR_MUON_MAX_STEPS
 
 
@@ -126,7 +133,21 @@ def lib():
             getattr(L, name + "_scaled").argtypes = [*plain[:at], f32, *plain[at:]]
         L.muon_update.argtypes = [i32, i32, C.c_int, vp, i64, vp, i64, vp, i64, f32, C.c_int, C.c_int, f32, f32, C.c_int,
                                   vp, i64, vp, sz, vp]
-        for name in ("l1csr_token_logp", "l1csr_policy_loss", "l1csr_preference_loss", "l1csr_policy_loss_scaled",
+        L.l1csr_embedding_fwd.argtypes = [i32, i32, i32, C.c_int, vp, i64, vp, f32, C.c_int, vp, i64, vp]
+        L.l1csr_embedding_csr_fwd.argtypes = [i32, i32, i64, vp, vp, vp, i32, vp, f32, vp, i64, vp]
+        L.l1csr_embedding_plan.argtypes = [i32, i32, vp, vp, sz, vp]
+        L.l1csr_embedding_bwd.argtypes = [i32, i32, i32, C.c_int, vp, i64, vp, sz, f32, C.c_int, vp, i64, vp, i64, vp, sz, vp]
+        L.l1csr_embedding_masked_bwd.argtypes = [i32, i32, i64, vp, vp, i32, vp, i64, vp, sz, f32, vp, vp, sz, vp]
+        L.l1csr_residual_norm_fwd.argtypes = [i32, i32, C.c_int, vp, i64, vp, i64, C.c_int, C.c_int, vp, i64, vp, vp, f32, f32,
+                                              vp, i64, vp, i64, vp, sz, vp]
+        L.l1csr_residual_norm_bwd.argtypes = [i32, i32, C.c_int, vp, i64, vp, i64, vp, i64, vp, i64, C.c_int, C.c_int, vp, i64,
+                                              vp, vp, f32, f32, vp, i64, vp, i64, vp, i64, vp, vp, vp, sz, vp]
+        L.l1csr_grad_norm.argtypes = [i32, vp, vp, vp, vp, vp, f32, vp, vp, sz, vp]
+        L.l1csr_clip_grad_norm.argtypes = [i32, vp, vp, vp, vp, vp, vp, vp, vp, f32, f32, f32, C.c_int, vp, vp, sz, vp]
+        for name in ("l1csr_embedding_fwd", "l1csr_embedding_csr_fwd", "l1csr_embedding_plan", "l1csr_embedding_bwd",
+                     "l1csr_embedding_masked_bwd", "l1csr_residual_norm_fwd", "l1csr_residual_norm_bwd", "l1csr_grad_norm",
+                     "l1csr_clip_grad_norm",
+                     "l1csr_token_logp", "l1csr_policy_loss", "l1csr_preference_loss", "l1csr_policy_loss_scaled",
                      "l1csr_preference_loss_scaled", "muon_update", "csr_spmm_fwd", "csr_spmm_plan", "csr_spmm_planned", "csc_build", "csc_update_vals", "csr_spmm_bwd_t", "dense_wgrad",
                      "sddmm_masked_wgrad", "prox_l1_step", "csr_recompress", "prox_l1_recompress",
                      "prox_l1_recompress_noalloc", "dense_wgrad_prox", "csr_recompress_counted", "csr_bitmap_build",
@@ -1490,6 +1511,359 @@ def prox_muon_recompress(W: CSR, G, st: MuonState, eta, lam, O=None, capacity=No
         with torch.cuda.stream(torch.cuda.current_stream(G.device) if stream is None else stream):
             st.m.copy_(m_new)
     return out
+
+
+# ---------------------------------------------------------------------------
+# around the layers of a network on tokens
+# ---------------------------------------------------------------------------
+
+def _out_mat(t, shape, dtypes, index, name, what, device, stream):
+    """A call's output matrix, the caller's or a new one of the first type; returns (tensor, ld, l1csr_dtype)."""
+    if t is None:
+        t = _new(shape, dtypes[0], device, stream)
+    rows, cols, ld, code = _typed_mat(t, name)
+    if (rows, cols) != tuple(shape) or t.dtype not in dtypes:
+        raise ValueError(f"{name} must be {what}")
+    _same_device(index, t, name)
+    return t, ld, code
+
+
+def _csr_on(W, index):
+    for t_, name in ((W.row_ptr, "row_ptr"), (W.col_idx, "col_idx"), (W.vals, "vals")):
+        _same_device(index, t_, name)
+
+
+def embedding_fwd(E, tokens, X=None, scale=1.0, dtype=None, stream=None):
+    """Rows of a table as columns of the activations: X[d][b] = scale * E[tokens[b]][d], 0 where tokens[b] lies outside
+    [0, V) (padding).
+
+    E is a table [V][D] (float32, bfloat16 or float16, features contiguous, as a layer's weights) or a CSR (V x D);
+    tokens int32 [B]; X [D][B] of the table's type or float32 (dtype: which a new one has; default the table's).  Returns X."""
+    torch = _torch()
+    _dev(tokens, torch.int32, "tokens")
+    index = _device_of(tokens)
+    _vec(tokens, torch.int32, "tokens")
+    B = tokens.numel()
+    if isinstance(E, CSR):
+        nnz = E.validate_shapes()
+        _csr_on(E, index)
+        if dtype is not None and dtype is not torch.float32:
+            raise ValueError("a CSR table gives float32")
+        X, ldx, _ = _out_mat(X, (E.n_cols, B), (torch.float32,), index, "X", "[D][B] float32", tokens.device, stream)
+        _check(lib().l1csr_embedding_csr_fwd(E.n_rows, E.n_cols, nnz, _p(E.row_ptr), _p(E.col_idx), _p(E.vals), B, _p(tokens),
+                                             scale, _p(X), ldx, _stream(stream)), "l1csr_embedding_csr_fwd")
+        return X
+    V, D, lde, code = _typed_mat(E, "E")
+    _same_device(index, E, "E")
+    dtypes = (E.dtype, torch.float32)
+    if dtype is not None:
+        if dtype not in dtypes:
+            raise ValueError("dtype must be the table's or float32")
+        dtypes = (dtype,)
+    X, ldx, xcode = _out_mat(X, (D, B), dtypes, index, "X", "[D][B] of the table's type or float32", E.device, stream)
+    _check(lib().l1csr_embedding_fwd(V, D, B, code, E.data_ptr(), lde, tokens.data_ptr(), scale, xcode, X.data_ptr(), ldx,
+                                     _stream(stream)), "l1csr_embedding_fwd")
+    return X
+
+
+@dataclass
+class EmbeddingPlan:
+    """The order that an embedding's gradients add up in (embedding_plan): of B tokens of a table of n_rows rows."""
+    n_rows: int
+    B: int
+    buf: object  # device buffer, None for B = 0
+
+
+def embedding_plan(tokens, n_rows, plan: EmbeddingPlan | None = None, stream=None) -> EmbeddingPlan:
+    """The order of the tokens (int32 [B]) of a table of n_rows rows, for embedding_bwd and embedding_masked_bwd.  It depends
+    on the tokens alone, so it can be made beside the forward pass and serves every gradient of the batch.  A plan given
+    is filled again (its buffer, where that is large enough)."""
+    torch = _torch()
+    _dev(tokens, torch.int32, "tokens")
+    index = _device_of(tokens)
+    _vec(tokens, torch.int32, "tokens")
+    B, n_rows = tokens.numel(), int(n_rows)
+    need = workspace_bytes(OP_EMBEDDING_PLAN, n_rows, 0, 0, B)
+    if plan is None:
+        plan = EmbeddingPlan(n_rows, B, None)
+    buf = plan.buf
+    if need > 0 and (buf is None or buf.numel() < need or buf.get_device() != index):
+        buf = _empty_bytes(need, tokens.device, stream)
+    _check(lib().l1csr_embedding_plan(n_rows, B, tokens.data_ptr(), _p(buf), 0 if buf is None else buf.numel(),
+                                      _stream(stream)), "l1csr_embedding_plan")
+    plan.n_rows, plan.B, plan.buf = n_rows, B, buf
+    return plan
+
+
+def _embedding_order(tokens, n_rows, B, plan, index, stream):
+    """The plan of a gradient's call: the caller's, or one made here."""
+    torch = _torch_module
+    if plan is None:
+        _vec_of(tokens, torch.int32, B, index, "tokens", "token (B)")
+        return embedding_plan(tokens, n_rows, stream=stream)
+    if plan.n_rows != n_rows or plan.B != B:
+        raise ValueError("the plan is of another table or batch")
+    if plan.buf is not None:
+        _same_device(index, plan.buf, "the plan")
+    return plan
+
+
+def embedding_bwd(dX, tokens, n_rows, dE=None, scale=1.0, add=None, plan: EmbeddingPlan | None = None, stream=None):
+    """The table's dense gradient, every row of it: dE[v][d] = add[v][d] + scale * sum of dX[d][b] over tokens[b] = v.
+
+    dX [D][B] float32, bfloat16 or float16; dE [n_rows][D] float32 (a new one is) or of dX's type; add (of dE's shape and
+    type, default 0) may be dE itself: then rows without tokens are not touched (a table tied to the output layer:
+    add=dE=dense_wgrad(...)).  tokens int32 [B] (not looked at with a plan, and may be None then).  Sums are fp32 in an
+    order that the tokens fix.  The dense gradient is what prox_l1_recompress and the other l1 updates take.  Returns dE."""
+    torch = _torch()
+    D, B, lddx, code = _typed_mat(dX, "dX")
+    index, n_rows = _device_of(dX), int(n_rows)
+    dE, ldde, ecode = _out_mat(dE, (n_rows, D), (torch.float32, dX.dtype), index, "dE", "[n_rows][D] float32 or of dX's type",
+                               dX.device, stream)
+    ldadd = 0
+    if add is dE:
+        ldadd = ldde
+    elif add is not None:
+        _, ldadd, acode = _out_mat(add, (n_rows, D), (dE.dtype,), index, "add", "of dE's shape and type", dX.device, stream)
+        if n_rows == 1 and add.data_ptr() == dE.data_ptr():
+            ldadd = ldde
+    plan = _embedding_order(tokens, n_rows, B, plan, index, stream)
+    ws, wsb = _workspace(workspace_bytes(OP_EMBEDDING_BWD, n_rows, D, 0, B), dX.device, stream)
+    _check(lib().l1csr_embedding_bwd(n_rows, D, B, code, dX.data_ptr(), lddx, _p(plan.buf),
+                                     0 if plan.buf is None else plan.buf.numel(), scale, ecode, _p(add), ldadd,
+                                     dE.data_ptr(), ldde, _p(ws), wsb, _stream(stream)), "l1csr_embedding_bwd")
+    return dE
+
+
+def embedding_masked_bwd(W: CSR, dX, tokens, gv=None, scale=1.0, plan: EmbeddingPlan | None = None, stream=None):
+    """The gradient of a table kept in CSR, sampled on its pattern (debiasing, as sddmm_masked_wgrad):
+    gv[p] = scale * sum of dX[col p][b] over tokens[b] = row of p.  dX [D][B] float32; tokens, plan as in embedding_bwd.
+    Returns gv (float32 [nnz])."""
+    torch = _torch()
+    D, B, lddx = _mat(dX, "dX")
+    index = _device_of(dX)
+    nnz = W.validate_shapes()
+    _csr_on(W, index)
+    if D != W.n_cols:
+        raise ValueError("dX must have as many rows as W has columns")
+    if gv is None:
+        gv = _new((nnz,), torch.float32, dX.device, stream)
+    _vec(gv, torch.float32, "gv")
+    _same_device(index, gv, "gv")
+    if gv.numel() < nnz:
+        raise ValueError("gv must hold nnz values")
+    plan = _embedding_order(tokens, W.n_rows, B, plan, index, stream)
+    ws, wsb = _workspace(workspace_bytes(OP_EMBEDDING_BWD, W.n_rows, D, 0, B), dX.device, stream)
+    _check(lib().l1csr_embedding_masked_bwd(W.n_rows, D, nnz, _p(W.row_ptr), _p(W.col_idx), B, dX.data_ptr(), lddx,
+                                            _p(plan.buf), 0 if plan.buf is None else plan.buf.numel(), scale, _p(gv), _p(ws),
+                                            wsb, _stream(stream)), "l1csr_embedding_masked_bwd")
+    return gv
+
+
+def _norm_like(t, K, B, dtype, index, name):
+    """A matrix of a norm call; returns its leading dimension."""
+    rows, cols, ld, _ = _typed_mat(t, name)
+    if rows != K or cols != B or t.dtype is not dtype:
+        raise ValueError(f"{name} must have the shape and type of the residual")
+    _same_device(index, t, name)
+    return ld
+
+
+def _same_ld(out, ldo, t, ld, K):
+    """A single row's leading dimension is its own: that of the matrix it is given over."""
+    return ld if t is not None and K == 1 and out.data_ptr() == t.data_ptr() else ldo
+
+
+def _gate_args(gate, y, K, B, dtype, index):
+    """(gate kind, its leading dimension)"""
+    if gate is None:
+        return GATE_NONE, 0
+    if y is None:
+        raise ValueError("a gate needs the block's output y")
+    if gate.dim() == 1:
+        _vec_of(gate, _torch_module.float32, K, index, "gate", "feature (K)")
+        return GATE_ROW, 0
+    return GATE_FULL, _norm_like(gate, K, B, dtype, index, "gate")
+
+
+def _gain(t, K, index, name):
+    return None if t is None else _vec_of(t, _torch_module.float32, K, index, name, "feature (K)")
+
+
+def residual_norm_fwd(r, y=None, gate=None, post_gain=None, pre_gain=None, alpha=1.0, eps=1e-6, sigmoid=False, r_out=None,
+                      h=None, stream=None):
+    """The norms before and after a block with its gate and its residual, per token (column) of activations [K][B]:
+
+        n  = y / sqrt(mean_k y^2 + eps) * post_gain        (y itself without post_gain)
+        r' = r + alpha * a(gate) * n
+        h  = r' / sqrt(mean_k r'^2 + eps) * pre_gain       (left out without pre_gain)
+
+    r is the residual, y the block's output (None: r' is r, the norm alone), h the next block's input; all [K][B] of one
+    type (float32, bfloat16, float16), the gains float32 [K].  gate: None (a = 1), float32 [K] (a gain of the features)
+    or [K][B] of r's type; a(g) = g, or with sigmoid the logistic function.  h comes from the unrounded r'.
+    r_out and h may each be r or y themselves, but not each other.  Returns (r', h); h is None without pre_gain."""
+    K, B, ldr, code = _typed_mat(r, "r")
+    index, dtype, torch = _device_of(r), r.dtype, _torch_module
+    if y is None and (pre_gain is None or post_gain is not None):
+        raise ValueError("without y there is a norm of r alone: pre_gain is needed and post_gain has no meaning")
+    ldy = 0 if y is None else _norm_like(y, K, B, dtype, index, "y")
+    kind, ldg = _gate_args(gate, y, K, B, dtype, index)
+    post_gain, pre_gain = _gain(post_gain, K, index, "post_gain"), _gain(pre_gain, K, index, "pre_gain")
+    if (y is None and r_out is not None) or (pre_gain is None and h is not None):
+        raise ValueError("r_out needs y, h needs pre_gain")
+    ldro = ldh = 0
+    if y is not None:
+        r_out = _new((K, B), dtype, r.device, stream) if r_out is None else r_out
+        ldro = _norm_like(r_out, K, B, dtype, index, "r_out")
+        ldro = _same_ld(r_out, _same_ld(r_out, ldro, y, ldy, K), r, ldr, K)
+    if pre_gain is not None:
+        h = _new((K, B), dtype, r.device, stream) if h is None else h
+        ldh = _norm_like(h, K, B, dtype, index, "h")
+        ldh = _same_ld(h, _same_ld(h, ldh, y, ldy, K), r, ldr, K)
+    ws, wsb = _workspace(workspace_bytes(OP_RESIDUAL_NORM, K, 0, 0, B), r.device, stream)
+    _check(lib().l1csr_residual_norm_fwd(K, B, code, r.data_ptr(), ldr, _p(y), ldy, kind, 1 if sigmoid else 0, _p(gate), ldg,
+                                         _p(post_gain), _p(pre_gain), alpha, eps, _p(r_out), ldro, _p(h), ldh, _p(ws), wsb,
+                                         _stream(stream)), "l1csr_residual_norm_fwd")
+    return (r if y is None else r_out), h
+
+
+@dataclass
+class ResidualNormGrads:
+    """Gradients of residual_norm_fwd's arguments; None for what was not given."""
+    r: object
+    y: object
+    gate: object
+    post_gain: object
+    pre_gain: object
+
+
+def residual_norm_bwd(r_out, dr_out=None, dh=None, y=None, gate=None, post_gain=None, pre_gain=None, alpha=1.0, eps=1e-6,
+                      sigmoid=False, dr=None, dy=None, dgate=None, stream=None) -> ResidualNormGrads:
+    """The gradients of residual_norm_fwd: r_out is the r' it gave (the residual r itself where it had no y), dr_out the
+    gradient of the loss with respect to r' from its further uses (None: none), dh that with respect to h (with
+    pre_gain; one of both is needed); y, gate, post_gain, pre_gain, alpha, eps, sigmoid as there.
+
+    The gate's gradient has its shape; it and the gains' are sums over the tokens where one serves all.  dr may be dr_out
+    or dh itself, dy y itself and dgate a [K][B] gate itself; without pre_gain the gradient of r is dr_out, and
+    none is stored.  Returns ResidualNormGrads."""
+    K, B, ldr, code = _typed_mat(r_out, "r_out")
+    index, dtype, torch = _device_of(r_out), r_out.dtype, _torch_module
+    if y is None and (pre_gain is None or post_gain is not None):
+        raise ValueError("without y there is a norm of r alone: pre_gain is needed and post_gain has no meaning")
+    if (pre_gain is None) != (dh is None):
+        raise ValueError("dh goes with pre_gain")
+    if pre_gain is None and dr_out is None:
+        raise ValueError("dr_out is needed without pre_gain")
+    if (pre_gain is None and dr is not None) or (y is None and dy is not None) or (gate is None and dgate is not None):
+        raise ValueError("an output is given for a gradient that this call has not")
+    lddro = 0 if dr_out is None else _norm_like(dr_out, K, B, dtype, index, "dr_out")
+    lddh = 0 if dh is None else _norm_like(dh, K, B, dtype, index, "dh")
+    ldy = 0 if y is None else _norm_like(y, K, B, dtype, index, "y")
+    kind, ldg = _gate_args(gate, y, K, B, dtype, index)
+    post_gain, pre_gain = _gain(post_gain, K, index, "post_gain"), _gain(pre_gain, K, index, "pre_gain")
+    lddr = lddy = lddg = 0
+    if pre_gain is not None:
+        dr = _new((K, B), dtype, r_out.device, stream) if dr is None else dr
+        lddr = _norm_like(dr, K, B, dtype, index, "dr")
+        lddr = _same_ld(dr, _same_ld(dr, lddr, dr_out, lddro, K), dh, lddh, K)
+    if y is not None:
+        dy = _new((K, B), dtype, r_out.device, stream) if dy is None else dy
+        lddy = _same_ld(dy, _norm_like(dy, K, B, dtype, index, "dy"), y, ldy, K)
+    if kind == GATE_ROW:
+        dgate = _new((K,), torch.float32, r_out.device, stream) if dgate is None else dgate
+        _vec_of(dgate, torch.float32, K, index, "dgate", "feature (K)")
+    elif kind == GATE_FULL:
+        dgate = _new((K, B), dtype, r_out.device, stream) if dgate is None else dgate
+        lddg = _same_ld(dgate, _norm_like(dgate, K, B, dtype, index, "dgate"), gate, ldg, K)
+    dpost = None if post_gain is None else _new((K,), torch.float32, r_out.device, stream)
+    dpre = None if pre_gain is None else _new((K,), torch.float32, r_out.device, stream)
+    ws, wsb = _workspace(workspace_bytes(OP_RESIDUAL_NORM, K, 0, 0, B), r_out.device, stream)
+    _check(lib().l1csr_residual_norm_bwd(K, B, code, r_out.data_ptr(), ldr, _p(dr_out), lddro, _p(dh), lddh, _p(y), ldy, kind,
+                                         1 if sigmoid else 0, _p(gate), ldg, _p(post_gain), _p(pre_gain), alpha, eps, _p(dr),
+                                         lddr, _p(dy), lddy, _p(dgate), lddg, _p(dpost), _p(dpre), _p(ws), wsb,
+                                         _stream(stream)), "l1csr_residual_norm_bwd")
+    return ResidualNormGrads(dr_out if pre_gain is None else dr, dy, dgate, dpost, dpre)
+
+
+def _flat(t, index, name):
+    """(address, rows, columns, leading dimension, l1csr_dtype) of a gradient: a whole buffer is one row."""
+    code = _dtype_code(t, name)
+    if t.get_device() != index:
+        _same_device(index, t, name)
+    n = t.numel()
+    if t.is_contiguous():
+        return t.data_ptr(), 1, n, n, code
+    if t.dim() == 1 and t.stride(0) != 1 or t.dim() != 2:
+        raise ValueError(f"{name} must be contiguous, or 2-D with a contiguous last dimension")
+    rows, cols, ld, code = _typed_mat(t, name)
+    return t.data_ptr(), rows, cols, ld, code
+
+
+def _grad_args(grads):
+    """The tensors of a norm call as the C arrays of their addresses and sizes; returns (n, arrays, first tensor's index)."""
+    n = len(grads)
+    if n == 0:
+        raise ValueError("no gradients are given")
+    _dtype_code(grads[0], "grads[0]")
+    index = _device_of(grads[0])
+    return n, [_flat(t, index, f"grads[{i}]") for i, t in enumerate(grads)], index
+
+
+def _arrays(flat):
+    n = len(flat)
+    p, rows, cols, ld, code = zip(*flat)
+    return (C.c_void_p * n)(*p), (C.c_int64 * n)(*rows), (C.c_int64 * n)(*cols), (C.c_int64 * n)(*ld), (C.c_int32 * n)(*code)
+
+
+def grad_norm(grads, grad_scale=1.0, stats=None, stream=None):
+    """The norm of many gradients together, sqrt(sum of all squares) / grad_scale (grad_scale: a factor that they hold, as
+    the losses' grad_scale).  grads: a sequence of tensors (float32, bfloat16, float16; contiguous of any shape, or
+    [N][K] with a leading dimension).  Returns stats (float32 [2], on the device): the norm and 1 / grad_scale."""
+    grads = list(grads)
+    n, flat, index = _grad_args(grads)
+    torch = _torch_module
+    stats = _result(stats, 2, grads[0], index, "stats", "statistic (2)", stream)
+    ws, wsb = _workspace(workspace_bytes(OP_GRAD_NORM, n, 0, 0, 0), grads[0].device, stream)
+    _check(lib().l1csr_grad_norm(n, *_arrays(flat), grad_scale, stats.data_ptr(), _p(ws), wsb, _stream(stream)),
+           "l1csr_grad_norm")
+    return stats
+
+
+def clip_grad_norm(grads, max_norm, grad_scale=1.0, eps=1e-6, out=None, zero_nonfinite=False, stats=None, stream=None):
+    """Clips many gradients to a norm that they have together, in place or into `out`:
+
+        norm = sqrt(sum of all squares) / grad_scale,  f = min(1, max_norm / (norm + eps)) / grad_scale,  out = f * g
+
+    grads and grad_scale as in grad_norm: a factor that they hold is taken out.  out: a sequence of tensors of the same
+    shapes, each of its gradient's type or float32 (what the solvers take).  A norm that is not finite gives what the
+    formula gives; with zero_nonfinite f = 0 and every result 0, so that nothing of the step reaches a
+    momentum.  No tensor may be given twice.  Nothing waits: stats (float32 [2], on the device) = the norm and f."""
+    grads = list(grads)
+    n, flat, index = _grad_args(grads)
+    torch = _torch_module
+    targets = [None] * 3
+    if out is not None:
+        out = list(out)
+        if len(out) != n:
+            raise ValueError("out must hold one tensor per gradient")
+        flat_out = []
+        for i, (g, o) in enumerate(zip(grads, out)):
+            _dtype_code(o, f"out[{i}]")
+            if o.shape != g.shape or (o.dtype is not g.dtype and o.dtype is not torch.float32):
+                raise ValueError(f"out[{i}] must have the shape of grads[{i}] and its type or float32")
+            f = _flat(o, index, f"out[{i}]")
+            if f[1] != flat[i][1]:  # one of both is whole, the other has rows: both by rows
+                rows, cols = g.shape
+                flat[i] = (flat[i][0], rows, cols, flat[i][3] if flat[i][1] == rows else cols, flat[i][4])
+                f = (f[0], rows, cols, f[3] if f[1] == rows else cols, f[4])
+            flat_out.append(f)
+        p, _, _, ld, code = _arrays(flat_out)
+        targets = [p, ld, code]
+    stats = _result(stats, 2, grads[0], index, "stats", "statistic (2)", stream)
+    ws, wsb = _workspace(workspace_bytes(OP_GRAD_NORM, n, 0, 0, 0), grads[0].device, stream)
+    _check(lib().l1csr_clip_grad_norm(n, *_arrays(flat), *targets, max_norm, grad_scale, eps, 1 if zero_nonfinite else 0,
+                                      stats.data_ptr(), _p(ws), wsb, _stream(stream)), "l1csr_clip_grad_norm")
+    return stats
 
 
 # the two-stream l1 step over the entry points above

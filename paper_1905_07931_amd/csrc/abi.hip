@@ -4,7 +4,10 @@
 // stream (csr_recompress with a short capacity is the one documented wait).
 #include <math.h>
 
+#include <algorithm>
+#include <memory>
 #include <mutex>
+#include <new>
 
 #include "../../include/l1csr.h"
 #include "common.hpp"
@@ -114,6 +117,147 @@ bool share_memory(const matrix_span &a, const matrix_span &b, int64_t rows) {
     const uintptr_t pa = reinterpret_cast<uintptr_t>(a.p), pb = reinterpret_cast<uintptr_t>(b.p);
     const size_t d = pa <= pb ? (pb - pa) % a.pitch : (a.pitch - (pa - pb) % a.pitch) % a.pitch;  // b behind a in a row
     return d < a.row || a.pitch - d < b.row;
+}
+
+// matrices of different numbers of rows
+bool share_memory(const matrix_span &a, int64_t rows_a, const matrix_span &b, int64_t rows_b) {
+    if (a.row == 0 || b.row == 0 || rows_a <= 0 || rows_b <= 0) return false;
+    if (!bytes_overlap(a.p, (size_t)(rows_a - 1) * a.pitch + a.row, b.p, (size_t)(rows_b - 1) * b.pitch + b.row)) return false;
+    return rows_a == 1 || rows_b == 1 || share_memory(a, b, std::max(rows_a, rows_b));
+}
+
+// What the embedding calls check alike of the table, the activations and the tokens' order
+int embedding_check(const embedding_args &a, const void *plan, size_t plan_bytes) {
+    if (a.V < 0 || a.D < 0 || a.B < 0 || !finite_f(a.scale)) return L1CSR_EINVAL;
+    if (!embedding_fits(a.V, a.D, a.B)) return L1CSR_EUNSUPPORTED;
+    if (a.B > 0 && (plan == nullptr || plan_bytes < embedding_plan_bytes(a.B) || (uintptr_t)plan % 4 != 0))
+        return L1CSR_EINVAL;
+    return L1CSR_OK;
+}
+
+int embedding_ws_check(const embedding_args &a, const void *ws, size_t ws_bytes) {
+    const size_t need = embedding_bwd_workspace_bytes(a.D, a.B);
+    return need > 0 && (ws == nullptr || ws_bytes < need || !aligned16(ws)) ? L1CSR_EINVAL : L1CSR_OK;
+}
+
+// The kernels' grids: column blocks of up to 512 tokens and ranges of rows
+bool norm_fits(int64_t K, int64_t B) { return K <= 1 << 24 && B <= 1 << 24; }
+
+// a matrix of a norm call: absent, or of K rows and B columns
+struct norm_matrix {
+    const void *p;
+    int64_t ld;
+};
+
+// What the residual norm calls check alike: `in` are read; out[i] is written, and may be the matrices of
+// in that `same` has bits for
+int norm_check(const norm_args &a, const norm_matrix *in, int n_in, const norm_matrix *out, const unsigned *same,
+               int n_out, const float *const *vec, int n_vec, float *const *vec_out, int n_vec_out, const void *ws,
+               size_t ws_bytes) {
+    if (a.K < 0 || a.B < 0 || bad_dtype(a.dtype)) return L1CSR_EINVAL;
+    if (a.gate_kind != kGateNone && a.gate_kind != kGateRow && a.gate_kind != kGateFull) return L1CSR_EINVAL;
+    if (!finite_f(a.alpha) || !finite_f(a.eps) || !(a.eps > 0.f)) return L1CSR_EINVAL;
+    if (a.K > 0 && a.B > 0) {  // (an empty matrix may have no address)
+        if (a.y == nullptr && (a.gate_kind != kGateNone || a.post_gain != nullptr || a.pre_gain == nullptr)) return L1CSR_EINVAL;
+        if (a.gate_kind != kGateNone && a.gate == nullptr) return L1CSR_EINVAL;
+    }
+    if (!norm_fits(a.K, a.B)) return L1CSR_EUNSUPPORTED;
+    for (int i = 0; i < n_in; ++i)
+        if (in[i].p != nullptr && in[i].ld < a.B) return L1CSR_EINVAL;
+    const int64_t e = dtype_bytes(a.dtype);
+    auto bytes = [&](const norm_matrix &m) { return m.p && a.K > 0 && a.B > 0 ? (size_t)(((a.K - 1) * m.ld + a.B) * e) : 0; };
+    const size_t gain = sizeof(float) * (size_t)a.K;
+    for (int o = 0; o < n_out; ++o) {
+        if (out[o].p == nullptr) continue;
+        if (out[o].ld < a.B) return L1CSR_EINVAL;
+        const matrix_span s = span_of(out[o].p, a.B, out[o].ld, a.dtype);
+        for (int i = 0; i < n_in; ++i) {
+            if (in[i].p == nullptr) continue;
+            if (in[i].p == out[o].p && in[i].ld == out[o].ld && (same[o] >> i & 1)) continue;
+            if (share_memory(s, span_of(in[i].p, a.B, in[i].ld, a.dtype), a.K)) return L1CSR_EINVAL;
+        }
+        for (int q = o + 1; q < n_out; ++q)
+            if (out[q].p && share_memory(s, span_of(out[q].p, a.B, out[q].ld, a.dtype), a.K)) return L1CSR_EINVAL;
+        for (int i = 0; i < n_vec; ++i)
+            if (bytes_overlap(out[o].p, bytes(out[o]), vec[i], gain)) return L1CSR_EINVAL;
+    }
+    for (int o = 0; o < n_vec_out; ++o) {
+        for (int i = 0; i < n_in; ++i)
+            if (bytes_overlap(vec_out[o], gain, in[i].p, bytes(in[i]))) return L1CSR_EINVAL;
+        for (int i = 0; i < n_out; ++i)
+            if (bytes_overlap(vec_out[o], gain, out[i].p, bytes(out[i]))) return L1CSR_EINVAL;
+        for (int i = 0; i < n_vec; ++i)
+            if (bytes_overlap(vec_out[o], gain, vec[i], gain)) return L1CSR_EINVAL;
+        for (int i = o + 1; i < n_vec_out; ++i)
+            if (bytes_overlap(vec_out[o], gain, vec_out[i], gain)) return L1CSR_EINVAL;
+    }
+    const size_t need = residual_norm_workspace_bytes(a.K, a.B);
+    if (need > 0 && (ws == nullptr || ws_bytes < need || !aligned16(ws))) return L1CSR_EINVAL;
+    return L1CSR_OK;
+}
+
+// The tensors of a clipping call: every one well formed, and what is written apart from all others
+// (a tensor's result may be the tensor itself)
+int clip_check(const grad_tensor *t, int n) {
+    struct span {
+        matrix_span m;
+        int64_t rows;
+        int tensor;
+        bool written;
+    };
+    std::unique_ptr<span[]> all(new (std::nothrow) span[2 * (size_t)n + 1]);
+    if (!all) return L1CSR_EHIP;
+    int count = 0;
+    for (int i = 0; i < n; ++i) {
+        const grad_tensor &g = t[i];
+        if (g.rows == 0 || g.cols == 0) continue;
+        const bool same = g.out == g.g;
+        if (same && (g.dtype != g.out_dtype || (g.rows > 1 && g.ld != g.ldo))) return L1CSR_EINVAL;
+        all[count++] = {span_of(g.g, g.cols, g.ld, g.dtype), g.rows, i, same};
+        if (g.out != nullptr && !same) all[count++] = {span_of(g.out, g.cols, g.ldo, g.out_dtype), g.rows, i, true};
+    }
+    std::sort(all.get(), all.get() + count, [](const span &a, const span &b) { return (uintptr_t)a.m.p < (uintptr_t)b.m.p; });
+    for (int i = 0; i < count; ++i) {
+        const uintptr_t end = (uintptr_t)all[i].m.p + (size_t)(all[i].rows - 1) * all[i].m.pitch + all[i].m.row;
+        for (int j = i + 1; j < count && (uintptr_t)all[j].m.p < end; ++j)
+            if ((all[i].written || all[j].written) && share_memory(all[i].m, all[i].rows, all[j].m, all[j].rows))
+                return L1CSR_EINVAL;
+    }
+    return L1CSR_OK;
+}
+
+// l1csr_grad_norm and l1csr_clip_grad_norm: the tensors gathered and checked
+int clip_run(int32_t n, const void *const *grads, const int64_t *rows, const int64_t *cols, const int64_t *ld,
+             const int32_t *dtype, void *const *out, const int64_t *ld_out, const int32_t *dtype_out, const clip_args &a,
+             void *ws, size_t ws_bytes, hipStream_t stream) {
+    if (n < 0 || a.stats == nullptr) return L1CSR_EINVAL;
+    if (n > 0 && (grads == nullptr || rows == nullptr || cols == nullptr || ld == nullptr || dtype == nullptr))
+        return L1CSR_EINVAL;
+    if (ws == nullptr || ws_bytes < grad_norm_workspace_bytes(n) || !aligned16(ws)) return L1CSR_EINVAL;
+    std::unique_ptr<grad_tensor[]> t(new (std::nothrow) grad_tensor[(size_t)n + 1]);
+    if (!t) return L1CSR_EHIP;
+    for (int i = 0; i < n; ++i) {
+        grad_tensor &g = t[i];
+        g = {grads[i], rows[i], cols[i], ld[i], dtype[i], nullptr, 0, dtype[i]};
+        if (a.clip) {
+            g.out = out ? out[i] : const_cast<void *>(grads[i]);
+            g.ldo = out ? (ld_out ? ld_out[i] : cols[i]) : ld[i];
+            g.out_dtype = out && dtype_out ? dtype_out[i] : dtype[i];
+        }
+        if (g.rows < 0 || g.cols < 0 || bad_dtype(g.dtype)) return L1CSR_EINVAL;
+        if (g.out_dtype != g.dtype && g.out_dtype != L1CSR_DTYPE_F32) return L1CSR_EINVAL;
+        if (bad_dense(g.g, g.rows, g.cols, g.ld)) return L1CSR_EINVAL;
+        if (a.clip && bad_dense(g.out, g.rows, g.cols, g.ldo)) return L1CSR_EINVAL;
+        if (g.rows > INT32_MAX || g.cols > (int64_t)1 << 40) return L1CSR_EUNSUPPORTED;
+    }
+    const int rc = clip_check(t.get(), n);
+    if (rc != L1CSR_OK) return rc;
+    for (int i = 0; i < n; ++i)
+        for (const void *p : {t[i].g, (const void *)t[i].out})
+            if (bytes_overlap(a.stats, 2 * sizeof(float), p, typed_bytes(t[i].rows, t[i].cols, p == t[i].g ? t[i].ld : t[i].ldo,
+                                                                        p == t[i].g ? t[i].dtype : t[i].out_dtype)))
+                return L1CSR_EINVAL;
+    return hip_status(launch_clip_grad_norm(n, t.get(), a, ws, stream));
 }
 
 // What the calls over logits check alike; n_out: floats of a.out
@@ -352,6 +496,11 @@ size_t l1csr_workspace_bytes(int op, int32_t n_rows, int32_t n_cols, int64_t nnz
         case L1CSR_OP_MUON: return round_up(muon_workspace_bytes(n_rows, n_cols, 2));
         case L1CSR_OP_MUON_F16: return round_up(muon_workspace_bytes(n_rows, n_cols, 1));
         case L1CSR_OP_TOKEN_LOSS: return round_up(token_loss_workspace_bytes(n_rows, B, n_cols));
+        case L1CSR_OP_EMBEDDING_PLAN: return embedding_fits(0, 0, B) ? round_up(embedding_plan_bytes(B)) : 0;
+        case L1CSR_OP_EMBEDDING_BWD:
+            return embedding_fits(0, n_cols, B) ? round_up(embedding_bwd_workspace_bytes(n_cols, B)) : 0;
+        case L1CSR_OP_RESIDUAL_NORM: return norm_fits(n_rows, B) ? round_up(residual_norm_workspace_bytes(n_rows, B)) : 0;
+        case L1CSR_OP_GRAD_NORM: return round_up(grad_norm_workspace_bytes(n_rows));
         case L1CSR_OP_SOFTMAX_XENT: return round_up(sizeof(float) * (size_t)(ceil_div(B, 256) + 1));
         default: return 0;
     }
@@ -996,6 +1145,173 @@ int muon_update(int32_t N, int32_t K, int dtype, const void *G, int64_t ldg, con
     a.eps = eps; a.scale = scale; a.parts = parts;
     a.O = O; a.ldo = ldo;
     return hip_status(launch_muon(a, ws, stream));
+}
+
+int l1csr_embedding_fwd(int32_t V, int32_t D, int32_t B, int dtype, const void *E, int64_t lde, const int32_t *tokens,
+                        float scale, int x_dtype, void *X, int64_t ldx, hipStream_t stream) {
+    embedding_args a{};
+    a.V = V; a.D = D; a.B = B; a.dtype = dtype;
+    a.E = E; a.lde = lde; a.tokens = tokens; a.scale = scale;
+    a.X_out = X; a.ldx = ldx; a.x_dtype = x_dtype;
+    if (V < 0 || D < 0 || B < 0 || !finite_f(scale)) return L1CSR_EINVAL;
+    if (bad_dtype(dtype) || (x_dtype != dtype && x_dtype != L1CSR_DTYPE_F32)) return L1CSR_EINVAL;
+    if (!embedding_fits(V, D, B)) return L1CSR_EUNSUPPORTED;
+    if (bad_dense(E, V, D, lde) || bad_dense(X, D, B, ldx) || (B > 0 && tokens == nullptr)) return L1CSR_EINVAL;
+    const size_t out = typed_bytes(D, B, ldx, x_dtype);
+    if (share_memory(span_of(X, B, ldx, x_dtype), D, span_of(E, D, lde, dtype), V) ||
+        bytes_overlap(X, out, tokens, sizeof(int32_t) * (size_t)B))
+        return L1CSR_EINVAL;
+    return hip_status(launch_embedding_fwd(a, stream));
+}
+
+int l1csr_embedding_csr_fwd(int32_t V, int32_t D, int64_t nnz, const int32_t *row_ptr, const int32_t *col_idx,
+                            const float *vals, int32_t B, const int32_t *tokens, float scale, float *X, int64_t ldx,
+                            hipStream_t stream) {
+    embedding_args a{};
+    a.V = V; a.D = D; a.B = B;
+    a.tokens = tokens; a.scale = scale;
+    a.X_out = X; a.ldx = ldx;
+    if (bad_csr(V, D, nnz, row_ptr, col_idx, vals, true) || B < 0 || !finite_f(scale)) return L1CSR_EINVAL;
+    if (!embedding_fits(V, D, B)) return L1CSR_EUNSUPPORTED;
+    if (bad_dense(X, D, B, ldx) || (B > 0 && tokens == nullptr)) return L1CSR_EINVAL;
+    const size_t out = dense_bytes(D, B, ldx), n = sizeof(float) * (size_t)nnz;
+    if (bytes_overlap(X, out, tokens, sizeof(int32_t) * (size_t)B) || bytes_overlap(X, out, col_idx, n) ||
+        bytes_overlap(X, out, vals, n) || bytes_overlap(X, out, row_ptr, sizeof(int32_t) * ((size_t)V + 1)))
+        return L1CSR_EINVAL;
+    return hip_status(launch_embedding_csr_fwd(a, (int)nnz, row_ptr, col_idx, vals, stream));
+}
+
+int l1csr_embedding_plan(int32_t V, int32_t B, const int32_t *tokens, void *plan, size_t plan_bytes, hipStream_t stream) {
+    embedding_args a{};
+    a.V = V; a.B = B;
+    const int rc = embedding_check(a, plan, plan_bytes);
+    if (rc != L1CSR_OK) return rc;
+    if (B > 0 && tokens == nullptr) return L1CSR_EINVAL;
+    if (bytes_overlap(plan, embedding_plan_bytes(B), tokens, sizeof(int32_t) * (size_t)B)) return L1CSR_EINVAL;
+    return hip_status(launch_embedding_plan(V, B, tokens, plan, stream));
+}
+
+int l1csr_embedding_bwd(int32_t V, int32_t D, int32_t B, int dtype, const void *dX, int64_t lddx, const void *plan,
+                        size_t plan_bytes, float scale, int e_dtype, const void *add, int64_t ldadd, void *dE, int64_t ldde,
+                        void *ws, size_t ws_bytes, hipStream_t stream) {
+    embedding_args a{};
+    a.V = V; a.D = D; a.B = B; a.dtype = dtype;
+    a.scale = scale;
+    a.X = dX; a.ldx = lddx;
+    a.add = add; a.ldadd = ldadd; a.dE = dE; a.ldde = ldde; a.e_dtype = e_dtype;
+    if (bad_dtype(dtype) || (e_dtype != dtype && e_dtype != L1CSR_DTYPE_F32)) return L1CSR_EINVAL;
+    int rc = embedding_check(a, plan, plan_bytes);
+    if (rc != L1CSR_OK) return rc;
+    if (bad_dense(dX, D, B, lddx) || bad_dense(dE, V, D, ldde) || (add != nullptr && ldadd < D)) return L1CSR_EINVAL;
+    const matrix_span e = span_of(dE, D, ldde, e_dtype);
+    if (add != nullptr && (add == dE ? ldadd != ldde : share_memory(e, span_of(add, D, ldadd, e_dtype), V))) return L1CSR_EINVAL;
+    if (share_memory(e, V, span_of(dX, B, lddx, dtype), D) ||
+        bytes_overlap(dE, typed_bytes(V, D, ldde, e_dtype), plan, B > 0 ? embedding_plan_bytes(B) : 0))
+        return L1CSR_EINVAL;
+    rc = embedding_ws_check(a, ws, ws_bytes);
+    if (rc != L1CSR_OK) return rc;
+    return hip_status(launch_embedding_bwd(a, plan, ws, stream));
+}
+
+int l1csr_embedding_masked_bwd(int32_t V, int32_t D, int64_t nnz, const int32_t *row_ptr, const int32_t *col_idx, int32_t B,
+                               const float *dX, int64_t lddx, const void *plan, size_t plan_bytes, float scale, float *gv,
+                               void *ws, size_t ws_bytes, hipStream_t stream) {
+    embedding_args a{};
+    a.V = V; a.D = D; a.B = B; a.dtype = L1CSR_DTYPE_F32;
+    a.scale = scale;
+    a.X = dX; a.ldx = lddx;
+    if (bad_csr(V, D, nnz, row_ptr, col_idx, nullptr, false) || (nnz > 0 && gv == nullptr)) return L1CSR_EINVAL;
+    int rc = embedding_check(a, plan, plan_bytes);
+    if (rc != L1CSR_OK) return rc;
+    if (bad_dense(dX, D, B, lddx)) return L1CSR_EINVAL;
+    const size_t out = sizeof(float) * (size_t)nnz;
+    if (bytes_overlap(gv, out, dX, dense_bytes(D, B, lddx)) || bytes_overlap(gv, out, col_idx, out) ||
+        bytes_overlap(gv, out, row_ptr, sizeof(int32_t) * ((size_t)V + 1)) ||
+        bytes_overlap(gv, out, plan, B > 0 ? embedding_plan_bytes(B) : 0))
+        return L1CSR_EINVAL;
+    rc = embedding_ws_check(a, ws, ws_bytes);
+    if (rc != L1CSR_OK) return rc;
+    return hip_status(launch_embedding_masked_bwd(a, (int)nnz, row_ptr, col_idx, gv, plan, ws, stream));
+}
+
+int l1csr_residual_norm_fwd(int32_t K, int32_t B, int dtype, const void *r, int64_t ldr, const void *y, int64_t ldy,
+                            int gate_kind, int gate_sigmoid, const void *gate, int64_t ldg, const float *post_gain,
+                            const float *pre_gain, float alpha, float eps, void *r_out, int64_t ldro, void *h, int64_t ldh,
+                            void *ws, size_t ws_bytes, hipStream_t stream) {
+    norm_args a{};
+    a.K = K; a.B = B; a.dtype = dtype;
+    a.r = r; a.ldr = ldr; a.y = y; a.ldy = ldy;
+    a.gate = gate; a.ldg = ldg; a.gate_kind = gate_kind; a.sigmoid = gate_sigmoid != 0;
+    a.post_gain = post_gain; a.pre_gain = pre_gain; a.alpha = alpha; a.eps = eps;
+    a.r_out = r_out; a.ldro = ldro; a.h = h; a.ldh = ldh;
+    const bool full = gate_kind == kGateFull, some = K > 0 && B > 0;
+    if (some && ((y == nullptr && r_out != nullptr) || (pre_gain == nullptr && h != nullptr))) return L1CSR_EINVAL;
+    if (some && (r == nullptr || (y != nullptr && r_out == nullptr) || (pre_gain != nullptr && h == nullptr))) return L1CSR_EINVAL;
+    const norm_matrix in[] = {{r, ldr}, {y, ldy}, {full ? gate : nullptr, ldg}}, out[] = {{r_out, ldro}, {h, ldh}};
+    const unsigned same[] = {3, 3};  // either of r and y
+    const float *const vec[] = {post_gain, pre_gain, gate_kind == kGateRow ? static_cast<const float *>(gate) : nullptr};
+    const int rc = norm_check(a, in, 3, out, same, 2, vec, 3, nullptr, 0, ws, ws_bytes);
+    if (rc != L1CSR_OK) return rc;
+    return hip_status(launch_residual_norm_fwd(a, ws, stream));
+}
+
+int l1csr_residual_norm_bwd(int32_t K, int32_t B, int dtype, const void *r_out, int64_t ldr, const void *dr_out, int64_t lddro,
+                            const void *dh, int64_t lddh, const void *y, int64_t ldy, int gate_kind, int gate_sigmoid,
+                            const void *gate, int64_t ldg, const float *post_gain, const float *pre_gain, float alpha,
+                            float eps, void *dr, int64_t lddr, void *dy, int64_t lddy, void *dgate, int64_t lddg,
+                            float *dpost_gain, float *dpre_gain, void *ws, size_t ws_bytes, hipStream_t stream) {
+    norm_args a{};
+    a.K = K; a.B = B; a.dtype = dtype;
+    a.r_out = const_cast<void *>(r_out); a.ldro = ldr;
+    a.dr_out = dr_out; a.lddro = lddro; a.dh = dh; a.lddh = lddh; a.y = y; a.ldy = ldy;
+    a.gate = gate; a.ldg = ldg; a.gate_kind = gate_kind; a.sigmoid = gate_sigmoid != 0;
+    a.post_gain = post_gain; a.pre_gain = pre_gain; a.alpha = alpha; a.eps = eps;
+    a.dr = dr; a.lddr = lddr; a.dy = dy; a.lddy = lddy; a.dgate = dgate; a.lddg = lddg;
+    a.dpost_gain = dpost_gain; a.dpre_gain = dpre_gain;
+    const bool full = gate_kind == kGateFull, row = gate_kind == kGateRow, some = K > 0 && B > 0;
+    if ((dpre_gain == nullptr) != (pre_gain == nullptr) || (dpost_gain == nullptr) != (post_gain == nullptr)) {
+        if (K > 0) return L1CSR_EINVAL;
+    }
+    if (row && K > 0 && dgate == nullptr) return L1CSR_EINVAL;
+    if (some) {
+        if ((gate_kind == kGateNone && dgate != nullptr) || (y == nullptr && dy != nullptr)) return L1CSR_EINVAL;
+        if (pre_gain != nullptr ? (r_out == nullptr || dh == nullptr || dr == nullptr) : (dr_out == nullptr || dh != nullptr))
+            return L1CSR_EINVAL;
+        if ((y != nullptr && dy == nullptr) || (full && dgate == nullptr)) return L1CSR_EINVAL;
+    }
+    const norm_matrix in[] = {{pre_gain ? r_out : nullptr, ldr}, {dr_out, lddro}, {dh, lddh}, {y, ldy}, {full ? gate : nullptr, ldg}};
+    const norm_matrix out[] = {{dr, lddr}, {dy, lddy}, {full ? dgate : nullptr, lddg}};
+    const unsigned same[] = {1u << 1 | 1u << 2, 1u << 3, 1u << 4};  // dr: dr_out or dh; dy: y; dgate: the gate
+    const float *const vec[] = {post_gain, pre_gain, row ? static_cast<const float *>(gate) : nullptr};
+    float *const vec_out[] = {dpost_gain, dpre_gain, row ? static_cast<float *>(dgate) : nullptr};
+    const int rc = norm_check(a, in, 5, out, same, 3, vec, 3, vec_out, 3, ws, ws_bytes);
+    if (rc != L1CSR_OK) return rc;
+    return hip_status(launch_residual_norm_bwd(a, ws, stream));
+}
+
+int l1csr_grad_norm(int32_t n, const void *const *grads, const int64_t *rows, const int64_t *cols, const int64_t *ld,
+                    const int32_t *dtype, float grad_scale, float *stats, void *ws, size_t ws_bytes, hipStream_t stream) {
+    if (!finite_f(grad_scale) || !(grad_scale > 0.f)) return L1CSR_EINVAL;
+    clip_args a{};
+    a.inv_scale = 1 / (double)grad_scale;
+    a.stats = stats;
+    return clip_run(n, grads, rows, cols, ld, dtype, nullptr, nullptr, nullptr, a, ws, ws_bytes, stream);
+}
+
+int l1csr_clip_grad_norm(int32_t n, const void *const *grads, const int64_t *rows, const int64_t *cols, const int64_t *ld,
+                         const int32_t *dtype, void *const *out, const int64_t *ld_out, const int32_t *dtype_out,
+                         float max_norm, float grad_scale, float eps, int zero_nonfinite, float *stats, void *ws,
+                         size_t ws_bytes, hipStream_t stream) {
+    if (!finite_f(grad_scale) || !(grad_scale > 0.f)) return L1CSR_EINVAL;
+    if (!(max_norm >= 0.f) || !finite_f(eps) || !(eps > 0.f)) return L1CSR_EINVAL;
+    clip_args a{};
+    a.max_norm = max_norm;
+    a.inv_scale = 1 / (double)grad_scale;
+    a.eps = eps;
+    a.clip = true;
+    a.zero_nonfinite = zero_nonfinite != 0;
+    a.stats = stats;
+    return clip_run(n, grads, rows, cols, ld, dtype, out, ld_out, dtype_out, a, ws, ws_bytes, stream);
 }
 
 }  // extern "C"

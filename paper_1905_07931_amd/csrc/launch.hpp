@@ -309,4 +309,79 @@ bool muon_fits(int N, int K);  // else it has no workspace either
 size_t muon_workspace_bytes(int N, int K, int parts);
 hipError_t launch_muon(const muon_args &a, void *ws, hipStream_t s);
 
+// embedding.hip ------------------------------------------------------------
+struct embedding_args {
+    int V, D, B, dtype;   // dtype: of the table (forward) or of dX (backward)
+    const void *E;        // [V][lde]
+    int64_t lde;
+    const int *tokens;    // [B]
+    float scale;
+    const void *X;        // backward: dX [D][ldx]
+    void *X_out;          // forward: X [D][ldx]
+    int64_t ldx;
+    int x_dtype;          // of X_out: fp32 or dtype
+    const void *add;      // [V][ldadd], null or dE itself; of dE's type
+    int64_t ldadd;
+    void *dE;             // [V][ldde]
+    int64_t ldde;
+    int e_dtype;          // of dE: fp32 or dtype
+};
+bool embedding_fits(int64_t V, int64_t D, int64_t B);
+size_t embedding_plan_bytes(int B);
+size_t embedding_bwd_workspace_bytes(int D, int B);
+hipError_t launch_embedding_fwd(const embedding_args &a, hipStream_t s);
+hipError_t launch_embedding_csr_fwd(const embedding_args &a, int nnz, const int *ptr, const int *col, const float *val,
+                                    hipStream_t s);
+hipError_t launch_embedding_plan(int V, int B, const int *tokens, void *plan, hipStream_t s);
+hipError_t launch_embedding_bwd(const embedding_args &a, const void *plan, void *ws, hipStream_t s);
+hipError_t launch_embedding_masked_bwd(const embedding_args &a, int nnz, const int *ptr, const int *col, float *gv,
+                                       const void *plan, void *ws, hipStream_t s);
+
+// residual_norm.hip --------------------------------------------------------
+constexpr int kGateNone = 0;
+constexpr int kGateRow = 1;   // float [K]
+constexpr int kGateFull = 2;  // [K][ldg] of the activations' type
+struct norm_args {
+    int K, B, dtype;
+    const void *r;            // forward: [K][ldr]
+    int64_t ldr;
+    const void *y;            // [K][ldy], null: the norm of r alone
+    int64_t ldy;
+    const void *gate;
+    int64_t ldg;
+    int gate_kind;
+    bool sigmoid;
+    const float *post_gain, *pre_gain;  // [K], null: no such norm
+    float alpha, eps;
+    void *r_out;              // [K][ldro]; backward: read
+    int64_t ldro;
+    void *h;                  // [K][ldh]
+    int64_t ldh;
+    const void *dr_out, *dh;  // backward: [K][lddro] (null: 0), [K][lddh]
+    int64_t lddro, lddh;
+    void *dr, *dy, *dgate;    // [K][lddr] (null: not stored), [K][lddy], as the gate
+    int64_t lddr, lddy, lddg;
+    float *dpre_gain, *dpost_gain;  // [K]
+};
+size_t residual_norm_workspace_bytes(int K, int B);
+hipError_t launch_residual_norm_fwd(const norm_args &a, void *ws, hipStream_t s);
+hipError_t launch_residual_norm_bwd(const norm_args &a, void *ws, hipStream_t s);
+
+// grad_clip.hip ------------------------------------------------------------
+struct grad_tensor {
+    const void *g;       // [rows][ld]
+    int64_t rows, cols, ld;
+    int dtype;
+    void *out;           // [rows][ldo], null: the norm alone; may be g
+    int64_t ldo;
+    int out_dtype;       // fp32 or dtype
+};
+struct clip_args {
+    double max_norm, inv_scale, eps;
+    bool clip, zero_nonfinite;
+    float *stats;        // 2 values
+};
+size_t grad_norm_workspace_bytes(int n);
+hipError_t launch_clip_grad_norm(int n, const grad_tensor *t, const clip_args &a, void *ws, hipStream_t s);
+
 }  // namespace l1csr
