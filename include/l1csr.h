@@ -721,7 +721,7 @@ int l1csr_preference_loss_scaled(int32_t C, int32_t B, int dtype, const void *lo
  * l1csr_embedding_masked_bwd: the gradient on the pattern of a table kept in CSR (debiasing, as sddmm_masked_wgrad),
  *     gv[p] = scale sum_{b: tokens[b] = row of p} dX[col_idx[p]][b]
  * ws, 16-byte aligned, as l1csr_workspace_bytes(L1CSR_OP_EMBEDDING_BWD, V, D, 0, B).  No output may overlap an
- * input (add = dE aside).  V, D <= 2^30 and B <= 2^24 (L1CSR_EUNSUPPORTED).  Results are reproducible.
+ * input (add = dE aside).  V <= 2^30, D <= 2^25 and B <= 2^24 (L1CSR_EUNSUPPORTED).  Results are reproducible.
  */
 int l1csr_embedding_fwd(int32_t V, int32_t D, int32_t B, int dtype, const void *E, int64_t lde, const int32_t *tokens,
                         float scale, int x_dtype, void *X, int64_t ldx, hipStream_t stream);

@@ -136,7 +136,7 @@ int embedding_check(const embedding_args &a, const void *plan, size_t plan_bytes
 }
 
 int embedding_ws_check(const embedding_args &a, const void *ws, size_t ws_bytes) {
-    const size_t need = embedding_bwd_workspace_bytes(a.D, a.B);
+    const size_t need = embedding_bwd_workspace_bytes(a.V, a.D, a.B);
     return need > 0 && (ws == nullptr || ws_bytes < need || !aligned16(ws)) ? L1CSR_EINVAL : L1CSR_OK;
 }
 
@@ -498,7 +498,7 @@ size_t l1csr_workspace_bytes(int op, int32_t n_rows, int32_t n_cols, int64_t nnz
         case L1CSR_OP_TOKEN_LOSS: return round_up(token_loss_workspace_bytes(n_rows, B, n_cols));
         case L1CSR_OP_EMBEDDING_PLAN: return embedding_fits(0, 0, B) ? round_up(embedding_plan_bytes(B)) : 0;
         case L1CSR_OP_EMBEDDING_BWD:
-            return embedding_fits(0, n_cols, B) ? round_up(embedding_bwd_workspace_bytes(n_cols, B)) : 0;
+            return embedding_fits(n_rows, n_cols, B) ? round_up(embedding_bwd_workspace_bytes(n_rows, n_cols, B)) : 0;
         case L1CSR_OP_RESIDUAL_NORM: return norm_fits(n_rows, B) ? round_up(residual_norm_workspace_bytes(n_rows, B)) : 0;
         case L1CSR_OP_GRAD_NORM: return round_up(grad_norm_workspace_bytes(n_rows));
         case L1CSR_OP_SOFTMAX_XENT: return round_up(sizeof(float) * (size_t)(ceil_div(B, 256) + 1));

@@ -25,32 +25,34 @@ constexpr int kMaxGrid = 1 << 20;      // workgroups of a launch; they step over
 
 __device__ __forceinline__ bool in_table(int token, int V) { return (unsigned)token < (unsigned)V; }
 
-// A tile's features d0 .. d0 + 63 of the tokens b0 .. b0 + 63, from LDS [feature][token] to X[d][b]
-template <typename T, typename F>
-__device__ __forceinline__ void store_columns(const float (&tile)[kTile * kPitch], int D, int B, int d0, int b0, T *X,
-                                              int64_t ldx, F value) {
-    constexpr int V = 4, lanes = kTile / V;
-    const int b = (threadIdx.x & (lanes - 1)) * V;
-#pragma unroll
-    for (int d = threadIdx.x / lanes; d < kTile; d += kThreads / lanes) {
-        if (d0 + d >= D || b0 + b >= B) continue;
-        const float *row = tile + d * kPitch + b;
-        T x[V];
-#pragma unroll
-        for (int v = 0; v < V; ++v) x[v] = (T)value(row[v]);
-        store_some<T, V>(X + (int64_t)(d0 + d) * ldx + b0 + b, B - b0 - b, x);
+// The tile of workgroup (or step) i: tiles side by side along the tokens first.  Rows of X are often a power of two long, and
+// 64 rows of such a matrix lie in the same few memory channels: neighbours along the features would all wait for those
+// (4096 x 8192 fp32, columns to rows: 88 us with the features first, 43 so).
+struct tile_at {
+    int d0, b0;
+    __device__ __forceinline__ tile_at(int64_t i, int b_tiles) {
+        const int64_t q = i / b_tiles;
+        d0 = (int)q * kTile;
+        b0 = (int)(i - q * b_tiles) * kTile;
     }
-}
+};
 
-template <typename TE, typename TX>
+// Results of this size are stored past the caches: they would only displace each other
+constexpr int64_t kPastBytes = 32 << 20;
+
+// A workgroup a tile.  131072 x 4096 bf16, 8192 tokens to fp32: 41 us from cold memory (165 MB, 4.0 TB/s; storing X alone
+// takes 20).  Larger tiles (59) and several tiles of the same tokens, their loads ahead (45 to 58), leave fewer
+// waves to wait for the rows.
+template <typename TE, typename TX, bool PAST>
 __global__ __launch_bounds__(kThreads) void gather_kernel(int V, int D, int B, const TE *__restrict__ E, int64_t lde,
                                                           const int *__restrict__ tokens, float scale,
-                                                          TX *__restrict__ X, int64_t ldx, int d_tiles, int64_t tiles) {
+                                                          TX *__restrict__ X, int64_t ldx, int b_tiles, int64_t tiles) {
     __shared__ float tile[kTile * kPitch];
     constexpr int N = kPer16<TE>, lanes = kTile / N;
     const int d = (threadIdx.x & (lanes - 1)) * N;
     for (int64_t i = blockIdx.x; i < tiles; i += gridDim.x) {
-        const int d0 = (int)(i % d_tiles) * kTile, b0 = (int)(i / d_tiles) * kTile;
+        const tile_at at(i, b_tiles);
+        const int d0 = at.d0, b0 = at.b0;
 #pragma unroll
         for (int b = threadIdx.x / lanes; b < kTile; b += kThreads / lanes) {
             const int t = b0 + b < B ? tokens[b0 + b] : -1;
@@ -60,7 +62,19 @@ __global__ __launch_bounds__(kThreads) void gather_kernel(int V, int D, int B, c
             for (int n = 0; n < N; ++n) tile[(d + n) * kPitch + b] = widen(e[n]);
         }
         __syncthreads();
-        store_columns(tile, D, B, d0, b0, X, ldx, [&](float x) { return scale * x; });
+        constexpr int M = 4, across = kTile / M;
+        const int b = (threadIdx.x & (across - 1)) * M;
+#pragma unroll
+        for (int k = threadIdx.x / across; k < kTile; k += kThreads / across) {
+            if (d0 + k >= D || b0 + b >= B) continue;
+            const float *row = tile + k * kPitch + b;
+            TX x[M];
+#pragma unroll
+            for (int m = 0; m < M; ++m) x[m] = (TX)(scale * row[m]);
+            TX *p = X + (int64_t)(d0 + k) * ldx + b0 + b;
+            if (PAST && b0 + b + M <= B) store_past<TX, M>(p, x);
+            else store_some<TX, M>(p, B - b0 - b, x);
+        }
         __syncthreads();
     }
 }
@@ -95,12 +109,12 @@ __global__ __launch_bounds__(kCsrThreads) void gather_csr_kernel(int V, int D, i
                                                                  const int *__restrict__ col,
                                                                  const float *__restrict__ val,
                                                                  const int *__restrict__ tokens, float scale,
-                                                                 float *__restrict__ X, int64_t ldx, int d_tiles,
+                                                                 float *__restrict__ X, int64_t ldx, int b_tiles,
                                                                  int64_t tiles) {
     __shared__ float tile[kCsrFeatures * kCsrPitch];
     const int lane = lane_id(), wave = uniform(threadIdx.x >> 6);
     for (int64_t i = blockIdx.x; i < tiles; i += gridDim.x) {
-        const int d0 = (int)(i % d_tiles) * kCsrFeatures, b0 = (int)(i / d_tiles) * kCsrTokens;
+        const int d0 = (int)(i / b_tiles) * kCsrFeatures, b0 = (int)(i % b_tiles) * kCsrTokens;
         for (int j = threadIdx.x; j < kCsrFeatures * kCsrPitch; j += kCsrThreads) tile[j] = 0.f;
         __syncthreads();
         for (int b = wave; b < kCsrTokens && b0 + b < B; b += kCsrThreads / kWave) {
@@ -130,38 +144,33 @@ __global__ __launch_bounds__(kCsrThreads) void gather_csr_kernel(int V, int D, i
 // the order of the tokens
 // ---------------------------------------------------------------------------
 
-constexpr int kRun = 8192;         // tokens that are ranked by counting
+constexpr int kRun = 1024;         // tokens that are ranked by counting
+constexpr int kWays = 8;           // runs that are merged at a time
 constexpr int kRankThreads = 1024;
 
 // what the tokens are sorted by: those of no row come last
-__device__ __forceinline__ int key_of(int token, int V) { return in_table(token, V) ? token : V; }
+__device__ __forceinline__ int key_of(int token, int V) { return (int)min((unsigned)token, (unsigned)V); }
 
-// Ranks within runs of kRun tokens by counting the smaller ones (and the equal ones ahead): a lane a token, the waves
-// of a workgroup share the run, whose tokens are read as scalars.
+// Ranks within runs of kRun tokens by counting the smaller ones (and the equal ones ahead): a lane a token, each wave of a
+// workgroup goes through 64 tokens of the run.
 __global__ __launch_bounds__(kRankThreads) void rank_kernel(int V, int B, const int *__restrict__ tokens,
                                                             int *__restrict__ rank, int *__restrict__ sorted) {
     constexpr int waves = kRankThreads / kWave;
+    static_assert(waves * kWave == kRun, "a wave for every 64 tokens of a run");
     __shared__ int part[waves][kWave];
     const int lane = lane_id(), wave = uniform(threadIdx.x >> 6);
-    const int own = blockIdx.x * kWave, base = own / kRun * kRun, n = min(kRun, B - base);
-    const int b = own + lane, key = key_of(b < B ? tokens[b] : -1, V);
+    const int own = blockIdx.x * kWave, base = own / kRun * kRun, at = base + wave * kWave, n = min(kWave, B - at);
+    const int b = own + lane;
+    const int key = b < B ? key_of(tokens[b], V) : V, others = lane < n ? key_of(tokens[at + lane], V) : 0;
     int less = 0;
-    for (int j0 = wave * kWave; j0 < n; j0 += waves * kWave) {  // 64 tokens at a time
-        const int at = base + j0, m = min(kWave, n - j0);
-        if (at == own) {
-            for (int j = 0; j < m; ++j) {
-                const int other = key_of(tokens[at + j], V);
-                less += other < key || (other == key && j < lane) ? 1 : 0;
-            }
-        } else {
-            const int limit = key + (at < own ? 1 : 0);  // equal tokens ahead count
-            if (m == kWave) {
-#pragma unroll 16
-                for (int j = 0; j < kWave; ++j) less += key_of(tokens[at + j], V) < limit ? 1 : 0;
-            } else {
-                for (int j = 0; j < m; ++j) less += key_of(tokens[at + j], V) < limit ? 1 : 0;
-            }
+    if (at == own) {
+        for (int j = 0; j < n; ++j) {
+            const int other = lane_bcast(others, j);
+            less += other < key || (other == key && j < lane) ? 1 : 0;
         }
+    } else {
+        const int limit = key + (at < own ? 1 : 0);  // equal tokens ahead count
+        for (int j = 0; j < n; ++j) less += lane_bcast(others, j) < limit ? 1 : 0;
     }
     part[wave][lane] = less;
     __syncthreads();
@@ -186,19 +195,53 @@ __device__ __forceinline__ int lower_bound(const int *__restrict__ s, int n, int
     return lo;
 }
 
-// Two sorted runs of `run` tokens become one: a token's rank grows by what goes before it in the other run.
+// Eight sorted runs of `run` tokens become one: a token's rank grows by what goes before it in each of the others, whose
+// searches go side by side.  The first round searches in LDS (FIRST: run = kRun), where a step's 64 x 7 scattered words
+// do not queue at the cache (8192 tokens: 16.6 us from memory).
+template <bool FIRST>
 __global__ __launch_bounds__(kThreads) void merge_kernel(int V, int B, int64_t run, const int *__restrict__ tokens,
                                                          int *__restrict__ rank, const int *__restrict__ sorted,
                                                          int *__restrict__ merged) {
-    const int64_t b = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    __shared__ __align__(16) int runs[FIRST ? kRun * kWays : 4];
+    const int64_t b0 = (int64_t)blockIdx.x * kThreads, b = b0 + threadIdx.x;
+    const int64_t first = b0 / (run * kWays) * (run * kWays);  // (a run is a multiple of kThreads tokens)
+    if constexpr (FIRST) {
+        const int n = (int)min((int64_t)kRun * kWays, B - first);
+        constexpr int N = 4, loads = kRun * kWays / (N * kThreads);
+        int x[loads][N];
+#pragma unroll
+        for (int i = 0; i < loads; ++i) {
+            const int at = (i * kThreads + (int)threadIdx.x) * N;
+            load_some<int, N>(sorted + first + at, n - at, x[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < loads; ++i) store_values<int, N>(runs + (i * kThreads + (int)threadIdx.x) * N, x[i]);
+        __syncthreads();
+    }
     if (b >= B) return;
-    const int key = key_of(tokens[b], V);
-    const int64_t q = b / run, other = (q ^ 1) * run;
-    const int n = (int)min((int64_t)run, max((int64_t)0, B - other));
-    // equal tokens of an earlier run go before
-    const int r = rank[b] + lower_bound(sorted + other, n, key + (q & 1 ? 1 : 0));
+    const int key = key_of(tokens[b], V), q = (int)((b - first) / run);
+    int lo[kWays], n[kWays];
+#pragma unroll
+    for (int w = 0; w < kWays; ++w) {
+        lo[w] = 0;
+        n[w] = w == q ? 0 : (int)min(run, max((int64_t)0, B - first - w * run));
+    }
+    for (int64_t left = run; left > 0; left >>= 1) {  // (a search of n values takes no more steps than n has bits)
+#pragma unroll
+        for (int w = 0; w < kWays; ++w) {
+            const int half = n[w] >> 1;
+            const int64_t at = w * run + lo[w] + half;
+            // equal tokens of an earlier run go before
+            const bool below = n[w] > 0 && (FIRST ? runs[at] : sorted[first + at]) < key + (w < q ? 1 : 0);
+            lo[w] = below ? lo[w] + half + 1 : lo[w];
+            n[w] = below ? n[w] - half - 1 : half;
+        }
+    }
+    int r = rank[b];
+#pragma unroll
+    for (int w = 0; w < kWays; ++w) r += lo[w];
     rank[b] = r;
-    merged[(q & ~1ll) * run + r] = key;
+    merged[first + r] = key;
 }
 
 // The plan's parts: rank[B] of every token, sorted[B] the tokens in order (V: of no row).  (Merged
@@ -209,7 +252,7 @@ struct plan_parts {
 plan_parts carve_plan(int B, void *plan) {
     int *p = static_cast<int *>(plan);
     plan_parts r{p, p + B, p + 2 * (size_t)B};
-    for (int64_t run = kRun; run < B; run *= 2) std::swap(r.sorted, r.other);
+    for (int64_t run = kRun; run < B; run *= kWays) std::swap(r.sorted, r.other);
     return r;
 }
 
@@ -224,49 +267,106 @@ template <typename T>
 struct run_rows {
     const T *rows;          // [B][ld]
     const float *groups;    // [B / 32][ld], a group's where its rows are of one token
-    const float *blocks;    // [B / 1024][ld], of 32 groups
+    const float *blocks;    // [B / 1024][ld], of 32 groups; null: not summed
     int64_t ld;
 };
 
-// sum over rows lo .. hi - 1 of the values at d .. d + N - 1, in one order
+// adds n rows of ld values at p, kAhead loads under way
+constexpr int kAhead = 8;
+template <typename T, int N>
+__device__ __forceinline__ void add_rows(const T *p, int64_t ld, int n, float (&sum)[N]) {
+    for (; n >= kAhead; n -= kAhead, p += kAhead * ld) {
+        T x[kAhead][N];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) load_values<T, N>(p + i * ld, x[i]);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+            for (int k = 0; k < N; ++k) sum[k] += widen(x[i][k]);
+    }
+    for (; n > 0; --n, p += ld) {
+        T x[N];
+        load_values<T, N>(p, x);
+#pragma unroll
+        for (int k = 0; k < N; ++k) sum[k] += widen(x[k]);
+    }
+}
+
+// sum over rows lo .. hi - 1 of the values at d .. d + N - 1, in one order: the rows ahead of the first whole group,
+// groups (blocks of them where they are whole and summed), the rows behind
 template <typename T, int N>
 __device__ __forceinline__ void sum_run(const run_rows<T> &r, int lo, int hi, int64_t d, float (&sum)[N]) {
 #pragma unroll
     for (int n = 0; n < N; ++n) sum[n] = 0.f;
-    int i = lo;
-    while (i < hi) {
-        if (i % kGroup == 0 && hi - i >= kGroup) {
-            float x[N];
-            if (i % (kGroup * kGroup) == 0 && hi - i >= kGroup * kGroup) {
-                load_values<float, N>(r.blocks + (int64_t)(i / (kGroup * kGroup)) * r.ld + d, x);
-                i += kGroup * kGroup;
-            } else {
-                load_values<float, N>(r.groups + (int64_t)(i / kGroup) * r.ld + d, x);
-                i += kGroup;
-            }
-#pragma unroll
-            for (int n = 0; n < N; ++n) sum[n] += x[n];
-        } else {
-            T x[N];
-            load_values<T, N>(r.rows + (int64_t)i * r.ld + d, x);
-            ++i;
-#pragma unroll
-            for (int n = 0; n < N; ++n) sum[n] += widen(x[n]);
+    const T *rows = r.rows + d;
+    int g = (lo + kGroup - 1) / kGroup;
+    const int end = hi / kGroup;
+    if (g >= end) {
+        add_rows<T, N>(rows + lo * r.ld, r.ld, hi - lo, sum);
+        return;
+    }
+    add_rows<T, N>(rows + lo * r.ld, r.ld, g * kGroup - lo, sum);
+    const float *groups = r.groups + d;
+    const int b = r.blocks ? (g + kGroup - 1) / kGroup : 0, b_end = r.blocks ? end / kGroup : 0;
+    if (b < b_end) {
+        add_rows<float, N>(groups + g * r.ld, r.ld, b * kGroup - g, sum);
+        add_rows<float, N>(r.blocks + d + b * r.ld, r.ld, b_end - b, sum);
+        g = b_end * kGroup;
+    }
+    add_rows<float, N>(groups + g * r.ld, r.ld, end - g, sum);
+    add_rows<T, N>(rows + end * kGroup * r.ld, r.ld, hi - end * kGroup, sum);
+}
+
+// bounds[v] = the first place of row v of the table in the order (row v's run is bounds[v] .. bounds[v + 1] - 1), by
+// workgroup `block` of `grid`.  Where the table is not much larger than the batch every place fills in the rows since the
+// one before it (a wave 64 places, each gap by all lanes), else every row is searched for.
+constexpr int kRowsAPlace = 32;
+__device__ __forceinline__ void fill_bounds(int V, int B, const int *__restrict__ sorted, int *__restrict__ bounds, int block,
+                                            int grid) {
+    const int64_t stride = (int64_t)grid * kThreads;
+    if (V > (int64_t)kRowsAPlace * (B + 1)) {
+        for (int64_t v = (int64_t)block * kThreads + threadIdx.x; v <= V; v += stride) bounds[v] = lower_bound(sorted, B, (int)v);
+        return;
+    }
+    const int lane = lane_id();
+    for (int64_t i0 = (int64_t)block * kThreads + (threadIdx.x & ~63); i0 <= B; i0 += stride) {
+        const int64_t i = i0 + lane;
+        const int from = i == 0 ? 0 : i <= B ? sorted[i - 1] + 1 : V + 1, to = i < B ? sorted[i] : V;
+        for (uint64_t some = wave_ballot(i <= B && from <= to); some != 0; some &= some - 1) {
+            const int j = __builtin_ctzll(some);
+            const int last = lane_bcast(to, j);
+            for (int v = lane_bcast(from, j) + lane; v <= last; v += kWave) bounds[v] = (int)(i0 + j);
         }
     }
 }
 
-// rows[rank of b][d] = dX[d][b]
+// rows[rank of b][d] = dX[d][b]; the last workgroups fill the bounds
 template <typename T>
 __global__ __launch_bounds__(kThreads) void sort_columns_kernel(int V, int D, int B, const T *__restrict__ dX, int64_t ldx,
                                                                 const int *__restrict__ rank,
                                                                 const int *__restrict__ sorted, T *__restrict__ rows,
-                                                                int64_t ld, int d_tiles, int64_t tiles) {
+                                                                int64_t ld, int b_tiles, int64_t tiles, int tile_grid,
+                                                                int *__restrict__ bounds) {
     __shared__ float tile[kTile * kPitch];  // [token][feature]
+    if ((int)blockIdx.x >= tile_grid) {
+        fill_bounds(V, B, sorted, bounds, blockIdx.x - tile_grid, gridDim.x - tile_grid);
+        return;
+    }
     constexpr int N = kPer16<T>, lanes = kTile / N;
     const int c = (threadIdx.x & (lanes - 1)) * N;
-    for (int64_t i = blockIdx.x; i < tiles; i += gridDim.x) {
-        const int d0 = (int)(i % d_tiles) * kTile, b0 = (int)(i / d_tiles) * kTile;
+    constexpr int step = kThreads / lanes;
+    for (int64_t i = blockIdx.x; i < tiles; i += tile_grid) {
+        const tile_at at(i, b_tiles);
+        const int d0 = at.d0, b0 = at.b0;
+        int to[kTile / step];  // the rows that this thread stores, -1: of no token that counts
+#pragma unroll
+        for (int j = 0; j < kTile / step; ++j) {
+            const int b = b0 + threadIdx.x / lanes + j * step;
+            to[j] = b < B ? rank[b] : -1;
+        }
+#pragma unroll
+        for (int j = 0; j < kTile / step; ++j)
+            if ((unsigned)to[j] >= (unsigned)B || sorted[to[j]] >= V) to[j] = -1;
 #pragma unroll
         for (int d = threadIdx.x / lanes; d < kTile; d += kThreads / lanes) {
             T x[N] = {};
@@ -276,14 +376,12 @@ __global__ __launch_bounds__(kThreads) void sort_columns_kernel(int V, int D, in
         }
         __syncthreads();
 #pragma unroll
-        for (int b = threadIdx.x / lanes; b < kTile; b += kThreads / lanes) {
-            if (b0 + b >= B) continue;
-            const int r = rank[b0 + b];
-            if ((unsigned)r >= (unsigned)B || sorted[r] >= V) continue;
+        for (int j = 0; j < kTile / step; ++j) {
+            const int b = threadIdx.x / lanes + j * step;
             T x[N];
 #pragma unroll
             for (int n = 0; n < N; ++n) x[n] = (T)tile[b * kPitch + c + n];
-            if (d0 + c < ld) store_values<T, N>(rows + (int64_t)r * ld + d0 + c, x);  // ld: D up to a multiple of 8
+            if (to[j] >= 0 && d0 + c < ld) store_values<T, N>(rows + to[j] * ld + d0 + c, x);  // ld: D up to a multiple of 8
         }
         __syncthreads();
     }
@@ -313,73 +411,75 @@ __global__ __launch_bounds__(kThreads) void group_kernel(int V, int B, int width
     }
 }
 
-constexpr int kRowBlock = 8;  // least rows of a workgroup, whose runs are searched side by side
+constexpr int kRowBlock = 4;  // rows of a workgroup that lie one behind the other
 
-// dE, every row of it (all), or dE += where only the rows that have tokens change: then a workgroup's rows are
-// places in the order, of which the first of each run has work.
-template <typename T, typename TE, bool ALL>
+// dE, every row of it (ALL), or dE += where only the rows that have tokens change: then a workgroup's rows are
+// places in the order, of which the first of each run has work.  blockIdx.y: a range of features.
+template <typename T, typename TE, bool ALL, bool PAST>
 __global__ __launch_bounds__(kThreads) void table_rows_kernel(int V, int D, int B, run_rows<T> r,
-                                                              const int *__restrict__ sorted, float scale,
-                                                              const TE *add, int64_t ldadd, TE *dE, int64_t ldde,
-                                                              int tx_shift) {
+                                                              const int *__restrict__ sorted,
+                                                              const int *__restrict__ bounds, float scale, const TE *add,
+                                                              int64_t ldadd, TE *dE, int64_t ldde, int tx_shift) {
     constexpr int N = 4;
-    __shared__ int bound[kThreads + 1];
-    const int TX = 1 << tx_shift, TY = kThreads >> tx_shift, per = max(TY, kRowBlock);
+    const int TX = 1 << tx_shift, TY = kThreads >> tx_shift;
     const int tx = threadIdx.x & (TX - 1), ty = threadIdx.x >> tx_shift;
-    const int64_t total = ALL ? V : B;
-    for (int64_t v0 = (int64_t)blockIdx.x * per; v0 < total; v0 += (int64_t)gridDim.x * per) {
-        __syncthreads();
-        for (int i = threadIdx.x; i < per + ALL; i += kThreads) {
-            const int64_t v = v0 + i;
-            if constexpr (ALL) {
-                bound[i] = lower_bound(sorted, B, (int)min(v, (int64_t)V));
+    const int64_t total = ALL ? V : B, d = ((int64_t)blockIdx.y * TX + tx) * N;
+    if (d >= D) return;
+    for (int64_t v0 = ((int64_t)blockIdx.x * TY + ty) * kRowBlock; v0 < total; v0 += (int64_t)gridDim.x * TY * kRowBlock) {
+        // the runs of the rows and what is added to them, all loads ahead of the first sum
+        int64_t row[kRowBlock];
+        int lo[kRowBlock], hi[kRowBlock];  // lo < 0: no work
+        TE e[kRowBlock][N];
+#pragma unroll
+        for (int i = 0; i < kRowBlock; ++i) {
+            const int64_t v = min(v0 + i, total - 1);
+            row[i] = ALL ? v : sorted[v];
+        }
+#pragma unroll
+        for (int i = 0; i < kRowBlock; ++i) {
+            const bool on = v0 + i < total && row[i] < V;
+            lo[i] = on ? bounds[row[i]] : -1;
+            hi[i] = on ? bounds[row[i] + 1] : -1;
+            if (!ALL && lo[i] != v0 + i) lo[i] = -1;
+        }
+#pragma unroll
+        for (int i = 0; i < kRowBlock; ++i) {
+            if (add && lo[i] >= 0) {
+                load_some<TE, N>(add + row[i] * ldadd + d, D - d, e[i]);
             } else {
-                // the end of the run that begins here; 0 where none does
-                int end = 0;
-                if (v < B && sorted[v] < V && (v == 0 || sorted[v - 1] != sorted[v]))
-                    end = (int)v + lower_bound(sorted + v, B - (int)v, sorted[v] + 1);
-                bound[i] = end;
+#pragma unroll
+                for (int n = 0; n < N; ++n) e[i][n] = (TE)0.f;
             }
         }
-        __syncthreads();
-        for (int y = ty; y < per && v0 + y < total; y += TY) {
-            int lo, hi;
-            int64_t v = v0 + y;
-            if constexpr (ALL) {
-                lo = bound[y];
-                hi = bound[y + 1];
-            } else {
-                lo = (int)v;
-                hi = bound[y];
-                if (hi <= lo) continue;
-                v = sorted[lo];
-            }
-            for (int64_t d = tx * N; d < D; d += TX * N) {
-                float s[N];
-                sum_run<T, N>(r, lo, hi, d, s);
-                TE e[N] = {};
-                if (add) load_some<TE, N>(add + v * ldadd + d, D - d, e);
 #pragma unroll
-                for (int n = 0; n < N; ++n) e[n] = (TE)(widen(e[n]) + scale * s[n]);
-                store_some<TE, N>(dE + v * ldde + d, D - d, e);
-            }
+        for (int i = 0; i < kRowBlock; ++i) {
+            if (lo[i] < 0) continue;
+            float s[N] = {};
+            if (lo[i] < hi[i]) sum_run<T, N>(r, lo[i], hi[i], d, s);
+#pragma unroll
+            for (int n = 0; n < N; ++n) e[i][n] = (TE)(widen(e[i][n]) + scale * s[n]);
+            TE *p = dE + row[i] * ldde + d;
+            if (PAST && D - d >= N) store_past<TE, N>(p, e[i]);
+            else store_some<TE, N>(p, D - d, e[i]);
         }
     }
 }
 
-// gv on the pattern: a wave a row of the table
-__global__ __launch_bounds__(kThreads) void table_pattern_kernel(int V, int D, int B, int nnz, run_rows<float> r,
-                                                                 const int *__restrict__ sorted, float scale,
+// gv on the pattern: 2^tx_shift threads a row of the table
+__global__ __launch_bounds__(kThreads) void table_pattern_kernel(int V, int D, int nnz, run_rows<float> r,
+                                                                 const int *__restrict__ bounds, float scale,
                                                                  const int *__restrict__ ptr, const int *__restrict__ col,
-                                                                 float *__restrict__ gv) {
-    const int lane = lane_id(), wave = uniform(threadIdx.x >> 6);
-    for (int64_t v = (int64_t)blockIdx.x * (kThreads / kWave) + wave; v < V; v += (int64_t)gridDim.x * (kThreads / kWave)) {
-        const int p0 = max(ptr[v], 0), p1 = min(ptr[v + 1], nnz);
-        if (p0 >= p1) continue;
-        const int lo = lower_bound(sorted, B, (int)v), hi = lo + lower_bound(sorted + lo, B - lo, (int)v + 1);
-        for (int p = p0 + lane; p < p1; p += kWave) {
+                                                                 float *__restrict__ gv, int tx_shift) {
+    const int TX = 1 << tx_shift, TY = kThreads >> tx_shift;
+    const int tx = threadIdx.x & (TX - 1), ty = threadIdx.x >> tx_shift;
+    for (int64_t v = (int64_t)blockIdx.x * TY + ty; v < V; v += (int64_t)gridDim.x * TY) {
+        const int p0 = max(ptr[v], 0), p1 = min(ptr[v + 1], nnz), lo = bounds[v], hi = bounds[v + 1];
+        for (int p = p0 + tx; p < p1; p += TX) {
             float s[1] = {};
-            if (lo < hi && (unsigned)col[p] < (unsigned)D) sum_run<float, 1>(r, lo, hi, col[p], s);
+            if (lo < hi) {
+                const int c = col[p];
+                if ((unsigned)c < (unsigned)D) sum_run<float, 1>(r, lo, hi, c, s);
+            }
             gv[p] = scale * s[0];
         }
     }
@@ -396,18 +496,27 @@ int pow2_shift(int64_t n, int most) {
 int grid_of(int64_t work) { return (int)std::min<int64_t>(std::max<int64_t>(work, 1), kMaxGrid); }
 
 struct bwd_parts {
-    char *rows;
+    int *bounds;
     float *groups, *blocks;
+    char *rows;
+    size_t bytes;
 };
-bwd_parts carve_bwd(int D, int B, void *ws) {
+bwd_parts carve_bwd(int V, int D, int B, void *ws) {
     char *p = static_cast<char *>(ws);
-    const int64_t ld = padded(D);
+    const size_t row = sizeof(float) * (size_t)padded(D);
     bwd_parts w;
-    w.groups = reinterpret_cast<float *>(p);
-    w.blocks = w.groups + B / kGroup * ld;
-    w.rows = reinterpret_cast<char *>(w.blocks + B / (kGroup * kGroup) * ld);
+    w.bounds = reinterpret_cast<int *>(p);
+    size_t at = (sizeof(int) * ((size_t)V + 1) + 63) & ~(size_t)63;
+    w.groups = reinterpret_cast<float *>(p + at);
+    at += row * (B / kGroup);
+    w.blocks = reinterpret_cast<float *>(p + at);
+    at += row * (B / (kGroup * kGroup));
+    w.rows = p + at;
+    w.bytes = at + row * B;
     return w;
 }
+
+constexpr int kBlocksFrom = 1 << 14;  // tokens from which on groups are summed once more
 
 // the columns of dX as rows in the tokens' order, and the sums of their groups
 template <typename T>
@@ -415,12 +524,13 @@ hipError_t sort_columns(const embedding_args &a, const plan_parts &plan, const b
                         hipStream_t s) {
     const int64_t ld = padded(a.D);
     T *rows = reinterpret_cast<T *>(w.rows);
-    *r = {rows, w.groups, w.blocks, ld};
-    const int d_tiles = (int)ceil_div(a.D, kTile);
-    const int64_t tiles = d_tiles * ceil_div(a.B, kTile);
-    sort_columns_kernel<T><<<grid_of(tiles), kThreads, 0, s>>>(a.V, a.D, a.B, static_cast<const T *>(a.X), a.ldx, plan.rank,
-                                                               plan.sorted, rows, ld, d_tiles, tiles);
-    const int groups = a.B / kGroup, blocks = a.B / (kGroup * kGroup);
+    const int b_tiles = (int)ceil_div(a.B, kTile);
+    const int64_t tiles = b_tiles * ceil_div(a.D, kTile);
+    const int tile_grid = a.B > 0 ? grid_of(tiles) : 0, bound_grid = grid_of(ceil_div(std::max(a.V, a.B) + 1ll, kThreads));
+    sort_columns_kernel<T><<<tile_grid + bound_grid, kThreads, 0, s>>>(
+        a.V, a.D, a.B, static_cast<const T *>(a.X), a.ldx, plan.rank, plan.sorted, rows, ld, b_tiles, tiles, tile_grid, w.bounds);
+    const int groups = a.B / kGroup, blocks = a.B >= kBlocksFrom ? a.B / (kGroup * kGroup) : 0;
+    *r = {rows, w.groups, blocks > 0 ? w.blocks : nullptr, ld};
     if (groups > 0)
         group_kernel<T><<<grid_of(groups), kThreads, 0, s>>>(a.V, a.B, 1, rows, plan.sorted, w.groups, ld, groups);
     if (blocks > 0)
@@ -432,27 +542,27 @@ hipError_t sort_columns(const embedding_args &a, const plan_parts &plan, const b
 }  // namespace
 
 bool embedding_fits(int64_t V, int64_t D, int64_t B) {
-    constexpr int64_t most = 1 << 30;
-    return V <= most && D <= most && B <= 1 << 24;  // (a launch has fewer than 2^32 threads)
+    // (a launch has fewer than 2^32 threads, and fewer than 2^16 ranges of features)
+    return V <= 1 << 30 && D <= 1 << 25 && B <= 1 << 24;
 }
 
 size_t embedding_plan_bytes(int B) { return sizeof(int) * 3 * (size_t)std::max(B, 0); }
 
-size_t embedding_bwd_workspace_bytes(int D, int B) {
-    if (D <= 0 || B <= 0) return 0;
-    return (size_t)padded(D) * sizeof(float) * ((size_t)B + B / kGroup + B / (kGroup * kGroup));
+size_t embedding_bwd_workspace_bytes(int V, int D, int B) {
+    return V <= 0 || D <= 0 ? 0 : carve_bwd(V, D, std::max(B, 0), nullptr).bytes;
 }
 
 hipError_t launch_embedding_fwd(const embedding_args &a, hipStream_t s) {
     if (a.D == 0 || a.B == 0) return hipSuccess;
-    const int d_tiles = (int)ceil_div(a.D, kTile);
-    const int64_t tiles = d_tiles * ceil_div(a.B, kTile);
+    const int b_tiles = (int)ceil_div(a.B, kTile);
     return with_types(a.dtype, a.x_dtype, [&](auto e, auto x) {
         using TE = decltype(e);
         using TX = decltype(x);
-        gather_kernel<TE, TX><<<grid_of(tiles), kThreads, 0, s>>>(a.V, a.D, a.B, static_cast<const TE *>(a.E), a.lde,
-                                                                  a.tokens, a.scale, static_cast<TX *>(a.X_out), a.ldx,
-                                                                  d_tiles, tiles);
+        const int64_t tiles = b_tiles * ceil_div(a.D, kTile);
+        const bool past = (int64_t)a.D * a.B * (int64_t)sizeof(TX) > kPastBytes;
+        (past ? gather_kernel<TE, TX, true> : gather_kernel<TE, TX, false>)<<<grid_of(tiles), kThreads, 0, s>>>(
+            a.V, a.D, a.B, static_cast<const TE *>(a.E), a.lde, a.tokens, a.scale, static_cast<TX *>(a.X_out), a.ldx, b_tiles,
+            tiles);
         return hipGetLastError();
     });
 }
@@ -460,10 +570,10 @@ hipError_t launch_embedding_fwd(const embedding_args &a, hipStream_t s) {
 hipError_t launch_embedding_csr_fwd(const embedding_args &a, int nnz, const int *ptr, const int *col, const float *val,
                                     hipStream_t s) {
     if (a.D == 0 || a.B == 0) return hipSuccess;
-    const int d_tiles = (int)ceil_div(a.D, kCsrFeatures);
-    const int64_t tiles = d_tiles * ceil_div(a.B, kCsrTokens);
+    const int b_tiles = (int)ceil_div(a.B, kCsrTokens);
+    const int64_t tiles = b_tiles * ceil_div(a.D, kCsrFeatures);
     gather_csr_kernel<<<grid_of(tiles), kCsrThreads, 0, s>>>(a.V, a.D, a.B, nnz, ptr, col, val, a.tokens, a.scale,
-                                                             static_cast<float *>(a.X_out), a.ldx, d_tiles, tiles);
+                                                             static_cast<float *>(a.X_out), a.ldx, b_tiles, tiles);
     return hipGetLastError();
 }
 
@@ -471,8 +581,9 @@ hipError_t launch_embedding_plan(int V, int B, const int *tokens, void *plan, hi
     if (B == 0) return hipSuccess;
     int *rank = static_cast<int *>(plan), *from = rank + B, *to = from + B;
     rank_kernel<<<(int)ceil_div(B, kWave), kRankThreads, 0, s>>>(V, B, tokens, rank, from);
-    for (int64_t run = kRun; run < B; run *= 2) {
-        merge_kernel<<<(int)ceil_div(B, kThreads), kThreads, 0, s>>>(V, B, run, tokens, rank, from, to);
+    for (int64_t run = kRun; run < B; run *= kWays) {
+        (run == kRun ? merge_kernel<true> : merge_kernel<false>)<<<(int)ceil_div(B, kThreads), kThreads, 0, s>>>(
+            V, B, run, tokens, rank, from, to);
         std::swap(from, to);
     }
     return hipGetLastError();
@@ -480,43 +591,41 @@ hipError_t launch_embedding_plan(int V, int B, const int *tokens, void *plan, hi
 
 hipError_t launch_embedding_bwd(const embedding_args &a, const void *plan_mem, void *ws, hipStream_t s) {
     if (a.D == 0 || a.V == 0) return hipSuccess;
+    const bool in_place = a.add != nullptr && a.add == a.dE;
+    if (in_place && a.B == 0) return hipSuccess;
     const plan_parts plan = carve_plan(a.B, const_cast<void *>(plan_mem));
-    const bwd_parts w = carve_bwd(a.D, a.B, ws);
+    const bwd_parts w = carve_bwd(a.V, a.D, a.B, ws);
     return with_types(a.dtype, a.e_dtype, [&](auto x, auto e) {
         using T = decltype(x);
         using TE = decltype(e);
-        run_rows<T> r{};
-        if (a.B > 0) {
-            const hipError_t err = sort_columns<T>(a, plan, w, &r, s);
-            if (err != hipSuccess) return err;
-        }
-        const int shift = pow2_shift(ceil_div(a.D, 4), 8), per = std::max(kThreads >> shift, kRowBlock);
+        run_rows<T> r;
+        const hipError_t err = sort_columns<T>(a, plan, w, &r, s);
+        if (err != hipSuccess) return err;
+        const int shift = pow2_shift(ceil_div(a.D, 4), 8), per = (kThreads >> shift) * kRowBlock;
+        const int64_t chunks = ceil_div(a.D, (int64_t)4 << shift);
         const TE *add = static_cast<const TE *>(a.add);
         TE *dE = static_cast<TE *>(a.dE);
-        if (a.add != nullptr && a.add == a.dE) {
-            if (a.B > 0)
-                table_rows_kernel<T, TE, false><<<grid_of(ceil_div(a.B, per)), kThreads, 0, s>>>(
-                    a.V, a.D, a.B, r, plan.sorted, a.scale, add, a.ldadd, dE, a.ldde, shift);
-        } else {
-            table_rows_kernel<T, TE, true><<<grid_of(ceil_div(a.V, per)), kThreads, 0, s>>>(
-                a.V, a.D, a.B, r, plan.sorted, a.scale, add, a.ldadd, dE, a.ldde, shift);
-        }
+        const int64_t rows = in_place ? a.B : a.V, most = std::max<int64_t>(1, kMaxGrid / chunks);
+        const dim3 grid((unsigned)std::min(ceil_div(rows, per), most), (unsigned)chunks);
+        const bool past = (int64_t)a.V * a.D * (int64_t)sizeof(TE) > kPastBytes;
+        const auto kernel = in_place ? table_rows_kernel<T, TE, false, false>
+                                     : past ? table_rows_kernel<T, TE, true, true> : table_rows_kernel<T, TE, true, false>;
+        kernel<<<grid, kThreads, 0, s>>>(a.V, a.D, a.B, r, plan.sorted, w.bounds, a.scale, add, a.ldadd, dE, a.ldde, shift);
         return hipGetLastError();
     });
 }
 
 hipError_t launch_embedding_masked_bwd(const embedding_args &a, int nnz, const int *ptr, const int *col, float *gv,
                                        const void *plan_mem, void *ws, hipStream_t s) {
-    if (a.V == 0 || nnz == 0) return hipSuccess;
+    if (a.V == 0 || a.D == 0 || nnz == 0) return hipSuccess;
     const plan_parts plan = carve_plan(a.B, const_cast<void *>(plan_mem));
-    const bwd_parts w = carve_bwd(a.D, a.B, ws);
-    run_rows<float> r{};
-    if (a.B > 0) {
-        const hipError_t err = sort_columns<float>(a, plan, w, &r, s);
-        if (err != hipSuccess) return err;
-    }
-    table_pattern_kernel<<<grid_of(ceil_div(a.V, kThreads / kWave)), kThreads, 0, s>>>(a.V, a.D, a.B, nnz, r, plan.sorted,
-                                                                                       a.scale, ptr, col, gv);
+    const bwd_parts w = carve_bwd(a.V, a.D, a.B, ws);
+    run_rows<float> r;
+    const hipError_t err = sort_columns<float>(a, plan, w, &r, s);
+    if (err != hipSuccess) return err;
+    const int shift = std::max(3, pow2_shift(nnz / a.V, 8));
+    table_pattern_kernel<<<grid_of(ceil_div(a.V, kThreads >> shift)), kThreads, 0, s>>>(a.V, a.D, nnz, r, w.bounds, a.scale,
+                                                                                       ptr, col, gv, shift);
     return hipGetLastError();
 }
 

@@ -328,7 +328,7 @@ struct embedding_args {
 };
 bool embedding_fits(int64_t V, int64_t D, int64_t B);
 size_t embedding_plan_bytes(int B);
-size_t embedding_bwd_workspace_bytes(int D, int B);
+size_t embedding_bwd_workspace_bytes(int V, int D, int B);
 hipError_t launch_embedding_fwd(const embedding_args &a, hipStream_t s);
 hipError_t launch_embedding_csr_fwd(const embedding_args &a, int nnz, const int *ptr, const int *col, const float *val,
                                     hipStream_t s);

@@ -19,6 +19,15 @@ template <typename T, int V>
 __device__ __forceinline__ void load_values(const T *p, T (&x)[V]) {
     __builtin_memcpy(x, p, sizeof(T) * V);
 }
+// Loads that are used once and leave the caches to what is read again
+template <typename T, int V>
+__device__ __forceinline__ void load_past(const T *p, T (&x)[V]) {
+    constexpr int bytes = (int)sizeof(T) * V;
+    static_assert(bytes % 4 == 0, "whole words");
+    typedef unsigned words __attribute__((ext_vector_type(bytes / 4), aligned(2)));
+    const words w = __builtin_nontemporal_load(reinterpret_cast<const words *>(p));
+    __builtin_memcpy(x, &w, bytes);
+}
 template <typename T, int V>
 __device__ __forceinline__ void store_values(T *p, const T (&x)[V]) {
     __builtin_memcpy(p, x, sizeof(T) * V);
@@ -50,8 +59,7 @@ template <typename T, int V>
 __device__ __forceinline__ void store_past(T *p, const T (&x)[V]) {
     constexpr int bytes = (int)sizeof(T) * V;
     if constexpr (bytes % 4 == 0) {
-        typedef unsigned word __attribute__((aligned(2)));
-        typedef word words __attribute__((ext_vector_type(bytes / 4), aligned(2)));
+        typedef unsigned words __attribute__((ext_vector_type(bytes / 4), aligned(2)));
         words w;
         __builtin_memcpy(&w, x, bytes);
         __builtin_nontemporal_store(w, reinterpret_cast<words *>(p));

@@ -35,7 +35,7 @@ def test_workspace_sizes(lib):
         assert ws(OP_BWD, 100, 10, 0, B) >= 40 * B
         assert ws(OP_NORM, 100, 0, 0, B) > 0
     assert ws(OP_PLAN, 100, 0, 0, (1 << 24) + 1) == 0 and ws(OP_BWD, 100, 10, 0, (1 << 24) + 1) == 0
-    assert ws(OP_BWD, 100, 0, 0, 5) == 0 and ws(OP_BWD, 100, 5, 0, 0) == 0 and ws(OP_NORM, 0, 0, 0, 5) == 0
+    assert ws(OP_BWD, 100, 0, 0, 5) == 0 and ws(OP_BWD, 0, 5, 0, 5) == 0 and ws(OP_NORM, 0, 0, 0, 5) == 0
     assert ws(OP_NORM, (1 << 24) + 1, 0, 0, 4) == 0
     assert 0 < ws(OP_CLIP, 1, 0, 0, 0) <= ws(OP_CLIP, 1000, 0, 0, 0)
 
