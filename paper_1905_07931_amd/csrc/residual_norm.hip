@@ -8,11 +8,16 @@
 //   k = alpha a w_post,  e = mean(k y t),  dy = q k t - q^3 e y     (without post gain: dy = alpha a t)
 //   dgate = alpha t n' a'(gate),  n' = y q w_post;  dw_pre = sum_b dh r' s;  dw_post = sum_b alpha a t y q
 //
-// Both means of a call come from one pass.  Forward: with x = alpha a w_post y, r' = r + q x and
-// sum r'^2 = sum r^2 + 2 q sum r x + q^2 sum x^2.  Backward: sum k y t = sum k y dr' + s sum k y u - s^3 c sum k y r'.
-// The sums are in double (the forward one cancels where a block takes back what the residual holds), in a fixed order.
-// Three launches: the sums of ranges of rows, their join to a column's factors, the results.
+// Two ways, by whether a strip of columns stays on the chip:
+// - strips: a workgroup of 1024 threads holds a few columns, all their rows, in registers; every mean is taken in its turn
+//   and everything is read once (the backward gate twice).
+// - two passes, for longer columns: both means of a call come from one pass over ranges of rows.  Forward: with
+//   x = alpha a w_post y, r' = r + q x and sum r'^2 = sum r^2 + 2 q sum r x + q^2 sum x^2.  Backward:
+//   sum k y t = sum k y dr' + s sum k y u - s^3 c sum k y r'.
+// Sums over a column are in double (the forward expansion cancels where a block takes back what the residual holds), in
+// a fixed order.
 #include <algorithm>
+#include <type_traits>
 
 #include "common.hpp"
 #include "launch.hpp"
@@ -23,102 +28,502 @@ namespace l1csr {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kSums = 6;       // most sums of a column
-constexpr int kFactors = 4;    // most factors of a column
-constexpr int kMaxSplits = 64; // most ranges of rows that a column's sums are taken over
+constexpr int kSums = 6;        // most sums of a column
+constexpr int kFactors = 4;     // most factors of a column
+constexpr int kMaxSplits = 64;  // most ranges of rows that a column's sums are taken over
+
+// The logistic function and its complement.  For fp32 from exp(-|g|) (the rounding of the exponent's product put back) and
+// a reciprocal refined once: each within about 4 steps of 2^-24.  For 16-bit gates as the instructions give it, within
+// (6 + |g|) steps of 2^-24, a quarter of the instructions.
+__device__ __forceinline__ void logistic(float g, float, float &a, float &b) {
+    constexpr float log2e = 1.44269504088896340736f, log2e_rest = 1.92596299112661746887e-8f, ln2 = 0.69314718055994530942f;
+    const float x = -fabsf(g), y = x * log2e;
+    const float rest = fmaf(x, log2e_rest, fmaf(x, log2e, -y)) * ln2;
+    float e = __builtin_amdgcn_exp2f(y);
+    if (x > -INFINITY) e = fmaf(e, rest, e);
+    const float d = 1.f + e, r0 = __builtin_amdgcn_rcpf(d), r = fmaf(fmaf(-d, r0, 1.f), r0, r0), small = e * r;
+    a = g >= 0.f ? r : small;  // (a NaN is in both)
+    b = g >= 0.f ? small : r;
+}
+template <typename T>
+__device__ __forceinline__ void logistic(float g, T, float &a, float &b) {
+    const float y = g * 1.44269504088896340736f;
+    a = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-y));
+    b = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(y));
+}
+
+// The gate of a row's columns from its values (a row of them, or one for all): a(g), and a'(g)
+template <typename T, int V>
+struct gate_values {
+    float a[V], da[V];
+    __device__ __forceinline__ gate_values(const norm_args &A, int k, const T (&raw)[V]) {
+        if (A.gate_kind == kGateFull) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                a[v] = widen(raw[v]);
+                da[v] = 1.f;
+            }
+            if (A.sigmoid) {
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    float b;
+                    logistic(a[v], T{}, a[v], b);
+                    da[v] = a[v] * b;
+                }
+            }
+        } else {
+            float one = 1.f, d = 0.f;
+            if (A.gate_kind == kGateRow) {
+                one = static_cast<const float *>(A.gate)[k];
+                d = 1.f;
+                if (A.sigmoid) {
+                    float b;
+                    logistic(one, 0.f, one, b);
+                    d = one * b;
+                }
+            }
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                a[v] = one;
+                da[v] = d;
+            }
+        }
+    }
+};
+
+// rounded to nearest even, two 16-bit values an instruction
+template <typename T, int V>
+__device__ __forceinline__ void narrow(const float (&x)[V], T (&t)[V]) {
+    if constexpr (sizeof(T) == 2 && V % 2 == 0) {
+        typedef float f2 __attribute__((ext_vector_type(2)));
+        typedef T t2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+        for (int v = 0; v < V; v += 2) {
+            const t2 y = __builtin_convertvector((f2{x[v], x[v + 1]}), t2);
+            __builtin_memcpy(&t[v], &y, 4);
+        }
+    } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v) t[v] = (T)x[v];
+    }
+}
+
+// ---------------------------------------------------------------------------
+// strips
+// ---------------------------------------------------------------------------
+
+constexpr int kStripThreads = 1024;
+constexpr int kStripWaves = kStripThreads / kWave;
+constexpr int kMaxStripColumns = 64;
+
+// 2^tx_shift threads of V columns each side by side, the others over the rows: thread row ty has the rows ty, ty + TY, ...
+// The strips of a cache line go to workgroups of one XCD that start together (32-byte pieces of rows: 4.4 to 6.0 TB/s so,
+// 1.6 to 1.9 where neighbours lie on other XCDs).
+struct strip_grid {
+    int tx_shift, strips, line;  // line: strips of 128 bytes
+    int blocks() const { return (int)(ceil_div(strips, 8 * line) * 8 * line); }
+};
+
+struct strip_place {
+    int strip, tx, ty, TY;
+    __device__ __forceinline__ explicit strip_place(const strip_grid &g) {
+        const int x = blockIdx.x & 7, j = blockIdx.x >> 3;
+        strip = (j / g.line * 8 + x) * g.line + j % g.line;
+        tx = threadIdx.x & ((1 << g.tx_shift) - 1);
+        ty = threadIdx.x >> g.tx_shift;
+        TY = kStripThreads >> g.tx_shift;
+    }
+};
+
+struct strip_shared {
+    double part[kStripWaves][kMaxStripColumns];
+    float factor[2][kMaxStripColumns];
+};
+
+// Adds up a wave's values over its rows: while a lane holds several columns each step halves them (V = 8: 9 exchanges
+// for 40); col: the column that is left.
+template <int D, int HELD, int V>
+__device__ __forceinline__ void fold(double (&x)[V], int lane, int TX, int &col) {
+    if constexpr (HELD > 1) {
+        constexpr int half = HELD / 2;
+        const bool upper = (lane & D) != 0;
+#pragma unroll
+        for (int i = 0; i < half; ++i) {
+            const double keep = upper ? x[i + half] : x[i], send = upper ? x[i] : x[i + half];
+            x[i] = keep + __shfl_xor(send, D, kWave);
+        }
+        col += upper ? half : 0;
+        fold<D / 2, half, V>(x, lane, TX, col);
+    } else if constexpr (D >= 1) {
+        if (D >= TX) x[0] += __shfl_xor(x[0], D, kWave);
+        fold<D / 2, 1, V>(x, lane, TX, col);
+    }
+}
+
+// Sums over the rows of NS values of each of a thread's V columns; f(column of the strip, its sums) in one thread a column.
+template <int V, int NS, typename F>
+__device__ __forceinline__ void strip_sums(double (&sum)[NS][V], int tx_shift, strip_shared (&sh)[NS], F f) {
+    const int lane = lane_id(), wave = threadIdx.x >> 6, TX = 1 << tx_shift;
+#pragma unroll
+    for (int q = 0; q < NS; ++q) {
+        int col = 0;
+        fold<kWave / 2, V, V>(sum[q], lane, TX, col);
+        // one lane of each column: those whose bits above tx that chose no column are 0
+        constexpr int chosen = (kWave - 1) & ~(kWave / V - 1);
+        if ((lane & ~chosen & ~(TX - 1)) == 0) sh[q].part[wave][(lane & (TX - 1)) * V + col] = sum[q][0];
+    }
+    __syncthreads();
+    if ((int)threadIdx.x < TX * V) {
+        double t[NS];
+#pragma unroll
+        for (int q = 0; q < NS; ++q) {
+            t[q] = 0;
+#pragma unroll
+            for (int w = 0; w < kStripWaves; ++w) t[q] += sh[q].part[w][threadIdx.x];
+        }
+        f((int)threadIdx.x, t);
+    }
+    __syncthreads();
+}
+
+// A thread's columns of a matrix, row after row of its own: byte offsets of 32 bits, the last row again past the end.  Loads are
+// whole vectors: where the columns end inside one it lies further back, over the neighbour's columns, whose values
+// are not used.
+template <typename T, int V>
+struct strip_rows {
+    unsigned first, step, last;
+    __device__ __forceinline__ strip_rows(const norm_args &A, int64_t ld, int at_col, int ty, int TY)
+        : first((unsigned)((ty * ld + at_col) * sizeof(T))), step((unsigned)(TY * ld * sizeof(T))),
+          last((unsigned)(((A.K - 1) * ld + at_col) * sizeof(T))) {}
+    __device__ __forceinline__ void load(const void *p, int j, T (&x)[V]) const {
+        load_values<T, V>(reinterpret_cast<const T *>(static_cast<const char *>(p) + min(first + j * step, last)), x);
+    }
+    // own: the first of the values that is a column of this thread
+    __device__ __forceinline__ void store(void *p, int j, const float (&x)[V], int own) const {
+        T t[V];
+        narrow<T, V>(x, t);
+        T *q = reinterpret_cast<T *>(static_cast<char *>(p) + (first + j * step));
+        if (own == 0) {
+            store_values<T, V>(q, t);
+        } else {
+#pragma unroll
+            for (int v = 1; v < V; ++v)
+                if (v >= own) q[v] = t[v];
+        }
+    }
+};
+
+// a value of a vector over the rows, by an offset of 32 bits
+__device__ __forceinline__ float row_value(const float *p, int k) {
+    return *reinterpret_cast<const float *>(reinterpret_cast<const char *>(p) + 4u * (unsigned)k);
+}
+
+// The same row of a thread, as the compiler cannot know: offsets of one phase are not kept for the next
+__device__ __forceinline__ int anew(int ty) {
+    asm volatile("" : "+v"(ty));
+    return ty;
+}
+
+// Forward: y stays in registers and becomes r'.  J rows of V columns a thread (J V <= 72 of 128 registers); r and the gate
+// come ahead, the first of them before the first mean is known.
+template <typename T, int V, int J>
+__global__ __launch_bounds__(kStripThreads) void forward_strip_kernel(norm_args A, strip_grid g) {
+    __shared__ strip_shared sh[1];
+    constexpr int P = J * V > 64 ? 1 : 2;  // rows of r and the gate that are under way
+    using partial = std::conditional_t<sizeof(T) == 4, double, float>;  // a thread's sum over its rows, 9 at most in 16 bits
+    const strip_place at(g);
+    if (at.strip >= g.strips) return;
+    const int64_t c = (((int64_t)at.strip << g.tx_shift) + at.tx) * V;
+    const int col = (int)min(c, (int64_t)A.B - V), own = (int)min(c - col, (int64_t)V);
+    const bool has_y = A.y != nullptr, post = A.post_gain != nullptr, pre = A.pre_gain != nullptr, full = A.gate_kind == kGateFull;
+    const int rows = at.ty < A.K ? (A.K - 1 - at.ty) / at.TY + 1 : 0;  // of this thread
+    T raw[J][V];  // y, or r without it
+    {
+        const strip_rows<T, V> m(A, has_y ? A.ldy : A.ldr, col, at.ty, at.TY);
+#pragma unroll
+        for (int j = 0; j < J; ++j) m.load(has_y ? A.y : A.r, j, raw[j]);
+    }
+    const int ty2 = anew(at.ty);
+    const strip_rows<T, V> mr(A, A.ldr, col, ty2, at.TY), mg(A, full ? A.ldg : 0, full ? col : 0, ty2, at.TY),
+        mo(A, A.ldro, col, ty2, at.TY);
+    T r[P][V], gate[P][V];
+    auto ahead = [&](int j) {
+        if (j >= J) return;
+        mr.load(A.r, j, r[j % P]);
+        if (full) mg.load(A.gate, j, gate[j % P]);
+    };
+    float x[J][V], q[V];
+    const float *factor = sh[0].factor[0] + at.tx * V;
+    auto mean_square = [&](auto value) {
+        partial part[V] = {};
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            if (j >= rows) continue;
+#pragma unroll
+            for (int v = 0; v < V; ++v) part[v] += (partial)value(j, v) * value(j, v);
+        }
+        double sum[1][V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) sum[0][v] = part[v];
+        strip_sums<V, 1>(sum, g.tx_shift, sh, [&](int i, const double(&t)[1]) {
+            sh[0].factor[0][i] = (float)(1 / sqrt(t[0] / A.K + A.eps));
+        });
+    };
+    if (has_y) {
+#pragma unroll
+        for (int j = 0; j < P; ++j) ahead(j);
+        if (post) mean_square([&](int j, int v) { return widen(raw[j][v]); });
+#pragma unroll
+        for (int v = 0; v < V; ++v) q[v] = post ? factor[v] : 1.f;
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const int k = min(ty2 + j * at.TY, A.K - 1);
+            const gate_values<T, V> a(A, k, gate[j % P]);
+            const float w = A.alpha * (post ? row_value(A.post_gain, k) : 1.f);
+#pragma unroll
+            for (int v = 0; v < V; ++v) x[j][v] = widen(r[j % P][v]) + a.a[v] * w * (widen(raw[j][v]) * q[v]);
+            ahead(j + P);
+            if (j < rows) mo.store(A.r_out, j, x[j], own);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+#pragma unroll
+            for (int v = 0; v < V; ++v) x[j][v] = widen(raw[j][v]);
+    }
+    if (!pre) return;
+    mean_square([&](int j, int v) { return x[j][v]; });
+    float s[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) s[v] = factor[v];
+    const int ty3 = anew(at.ty);
+    const strip_rows<T, V> mh(A, A.ldh, col, ty3, at.TY);
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+        if (j >= rows) continue;
+        const float w = row_value(A.pre_gain, ty3 + j * at.TY);
+#pragma unroll
+        for (int v = 0; v < V; ++v) x[j][v] = x[j][v] * s[v] * w;
+        mh.store(A.h, j, x[j], own);
+    }
+}
+
+// A row's sum over the threads side by side, stored by the first: rows[i][block][K]
+__device__ __forceinline__ void store_row_sum(const norm_args &A, float *rows, int i, int blocks, int block, int k, int tx,
+                                              int TX, float x) {
+    for (int d = TX / 2; d >= 1; d >>= 1) x += __shfl_xor(x, d, kWave);
+    if (tx == 0 && k < A.K) rows[((int64_t)i * blocks + block) * A.K + k] = x;
+}
+
+// Backward, for small matrices: r' and dh stay in registers and become t and y (J V <= 16 of each)
+template <typename T, int V, int J>
+__global__ __launch_bounds__(kStripThreads) void backward_strip_kernel(norm_args A, strip_grid g, float *__restrict__ rows) {
+    __shared__ strip_shared sh[2];
+    const strip_place at(g);
+    if (at.strip >= g.strips) return;
+    const int TX = 1 << g.tx_shift;
+    const int64_t c = (((int64_t)at.strip << g.tx_shift) + at.tx) * V;
+    const int col = (int)min(c, (int64_t)A.B - V), own = (int)min(c - col, (int64_t)V);
+    const bool has_y = A.y != nullptr, post = A.post_gain != nullptr, pre = A.pre_gain != nullptr;
+    const bool full = A.gate_kind == kGateFull, row = A.gate_kind == kGateRow;
+    const int held = at.ty < A.K ? (A.K - 1 - at.ty) / at.TY + 1 : 0;  // rows of this thread
+    float t[J][V], y[J][V];
+    float s[V] = {}, f[V] = {};
+    double sum[2][V] = {};
+    if (pre) {
+        const strip_rows<T, V> mr(A, A.ldro, col, at.ty, at.TY), mh(A, A.lddh, col, at.ty, at.TY);
+        T raw[J][V], raw2[J][V];
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            mr.load(A.r_out, j, raw[j]);
+            mh.load(A.dh, j, raw2[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const float w = row_value(A.pre_gain, min(at.ty + j * at.TY, A.K - 1));
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                t[j][v] = j < held ? widen(raw[j][v]) : 0.f;
+                y[j][v] = j < held ? widen(raw2[j][v]) : 0.f;
+                sum[0][v] += (double)t[j][v] * t[j][v];
+                sum[1][v] += (double)(y[j][v] * w) * t[j][v];
+            }
+        }
+        strip_sums<V, 2>(sum, g.tx_shift, sh, [&](int i, const double(&x)[2]) {
+            const double s2 = 1 / (x[0] / A.K + A.eps);
+            sh[0].factor[0][i] = (float)sqrt(s2);
+            sh[0].factor[1][i] = (float)(s2 * x[1] / A.K);
+        });
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            s[v] = sh[0].factor[0][at.tx * V + v];
+            f[v] = sh[0].factor[1][at.tx * V + v];
+            sum[0][v] = sum[1][v] = 0;
+        }
+    }
+    // t; y is read behind it
+    const void *dr_out = A.dr_out ? A.dr_out : A.r_out, *yp = has_y ? A.y : dr_out;
+    const int ty2 = anew(at.ty);
+    const strip_rows<T, V> md(A, A.dr_out ? A.lddro : A.ldro, col, ty2, at.TY),
+        my(A, has_y ? A.ldy : A.dr_out ? A.lddro : A.ldro, col, ty2, at.TY),
+        mg(A, full ? A.ldg : 0, full ? col : 0, ty2, at.TY), mo(A, A.lddr, col, ty2, at.TY);
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+        T dr[V], yr[V], gate[V];
+        md.load(dr_out, j, dr);
+        if (has_y) my.load(yp, j, yr);
+        if (full && post) mg.load(A.gate, j, gate);
+        const int k = min(ty2 + j * at.TY, A.K - 1);
+        float z[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) z[v] = A.dr_out && j < held ? widen(dr[v]) : 0.f;
+        if (pre) {
+            const float w = row_value(A.pre_gain, k);
+            float sums = 0.f;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const float rs = t[j][v] * s[v], dh = y[j][v];
+                sums += v >= own ? dh * rs : 0.f;
+                z[v] += s[v] * (dh * w) - f[v] * rs;
+            }
+            store_row_sum(A, rows, 0, g.strips, at.strip, ty2 + j * at.TY, at.tx, TX, sums);
+            if (j < held) mo.store(A.dr, j, z, own);
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) t[j][v] = z[v];
+        if (!has_y) continue;
+#pragma unroll
+        for (int v = 0; v < V; ++v) y[j][v] = j < held ? widen(yr[v]) : 0.f;
+        if (!post) continue;
+        const gate_values<T, V> a(A, k, gate);
+        const float w = A.alpha * row_value(A.post_gain, k);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            sum[0][v] += (double)y[j][v] * y[j][v];
+            sum[1][v] += j < held ? (double)(a.a[v] * w * t[j][v]) * y[j][v] : 0;
+        }
+    }
+    if (!has_y) return;
+    float q[V], e[V];
+    if (post)
+        strip_sums<V, 2>(sum, g.tx_shift, sh, [&](int i, const double(&x)[2]) {
+            const double q2 = 1 / (x[0] / A.K + A.eps);
+            sh[0].factor[0][i] = (float)sqrt(q2);
+            sh[0].factor[1][i] = (float)(q2 * x[1] / A.K);
+        });
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        q[v] = post ? sh[0].factor[0][at.tx * V + v] : 1.f;
+        e[v] = post ? sh[0].factor[1][at.tx * V + v] : 0.f;
+    }
+    const int ty3 = anew(at.ty);
+    const strip_rows<T, V> mdy(A, A.lddy, col, ty3, at.TY), mdg(A, A.lddg, col, ty3, at.TY),
+        mg3(A, full ? A.ldg : 0, full ? col : 0, ty3, at.TY);
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+        T gate[V];
+        if (full) mg3.load(A.gate, j, gate);
+        const int k = min(ty3 + j * at.TY, A.K - 1);
+        const gate_values<T, V> a(A, k, gate);
+        const float w = post ? row_value(A.post_gain, k) : 1.f;
+        float dy[V], dg[V], sums[2] = {};
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const float at_ = A.alpha * t[j][v], yq = y[j][v] * q[v];
+            dy[v] = a.a[v] * at_ * w * q[v] - e[v] * yq;
+            dg[v] = at_ * yq * w * a.da[v];
+            sums[0] += v >= own ? a.a[v] * at_ * yq : 0.f;
+            sums[1] += v >= own ? dg[v] : 0.f;
+        }
+        if (post) store_row_sum(A, rows, 1, g.strips, at.strip, ty3 + j * at.TY, at.tx, TX, sums[0]);
+        if (row) store_row_sum(A, rows, 2, g.strips, at.strip, ty3 + j * at.TY, at.tx, TX, sums[1]);
+        if (j >= held) continue;
+        mdy.store(A.dy, j, dy, own);
+        if (full) mdg.store(A.dgate, j, dg, own);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// two passes
+// ---------------------------------------------------------------------------
+
+constexpr int kPassThreads = 512;
+constexpr int kPassVector = 4;  // columns of a thread of the two passes (the sums of 8 take 96 registers)
 
 // How a workgroup lies over [K][B]: 2^tx_shift threads of V columns each side by side, the others over the rows;
 // blockIdx.y a range of rows.
 struct norm_grid {
-    int tx_shift, splits, rows;
+    int tx_shift, col_blocks, splits, rows;
 };
 
-template <int V>
+// A thread's columns.  Loads are whole vectors as in the strips: own is the first of the values that is a column of
+// this thread.  They go past the caches, which hold nothing that is read again: the backward sums of 9216 x 2048 fp32 (378
+// MB) take 67 us so and 96 through them.
+template <typename T, int V>
 struct columns {
-    int col0, n;  // the first column of this thread, how many of its V exist
+    int col, own;
     __device__ columns(int tx, int tx_shift, int B) {
         const int64_t c = (((int64_t)blockIdx.x << tx_shift) + tx) * V;
-        col0 = (int)min(c, (int64_t)B);
-        n = min(V, B - col0);
+        col = (int)min(c, (int64_t)B - V);
+        own = (int)min(c - col, (int64_t)V);
     }
-};
-
-template <typename T, int V>
-__device__ __forceinline__ void load_columns(const T *p, int n, float (&x)[V]) {
-    T t[V];
-    load_some<T, V>(p, n, t);
-#pragma unroll
-    for (int v = 0; v < V; ++v) x[v] = widen(t[v]);
-}
-
-template <typename T, int V>
-__device__ __forceinline__ void store_columns(T *p, int n, const float (&x)[V]) {
-    T t[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) t[v] = (T)x[v];
-    store_some<T, V>(p, n, t);
-}
-
-// The gate of a row's columns: a(g), and its derivative
-template <typename T, int V, int GATE, bool SIGMOID>
-struct gate_values {
-    float a[V], da[V];
-    __device__ __forceinline__ void set(int v, float g) {
-        if constexpr (SIGMOID) {
-            a[v] = 1.f / (1.f + expf(-g));
-            da[v] = a[v] * (1.f / (1.f + expf(g)));
-        } else {
-            a[v] = g;
-            da[v] = 1.f;
-        }
+    __device__ __forceinline__ void load(const void *p, int64_t ld, int k, T (&x)[V]) const {
+        const T *q = static_cast<const T *>(p) + (int64_t)k * ld + col;
+        if constexpr (V > 1) load_past<T, V>(q, x);
+        else load_values<T, V>(q, x);
     }
-    __device__ __forceinline__ gate_values(const norm_args &A, int k, int col0, int n) {
-        if constexpr (GATE == kGateFull) {
-            float g[V];
-            load_columns<T, V>(static_cast<const T *>(A.gate) + (int64_t)k * A.ldg + col0, n, g);
-#pragma unroll
-            for (int v = 0; v < V; ++v) set(v, g[v]);
-        } else if constexpr (GATE == kGateRow) {
-            set(0, static_cast<const float *>(A.gate)[k]);
-#pragma unroll
-            for (int v = 1; v < V; ++v) {
-                a[v] = a[0];
-                da[v] = da[0];
-            }
+    __device__ __forceinline__ void store(void *p, int64_t ld, int k, const float (&x)[V]) const {
+        T t[V];
+        narrow<T, V>(x, t);
+        T *q = static_cast<T *>(p) + (int64_t)k * ld + col;
+        if (own == 0) {
+            store_values<T, V>(q, t);
         } else {
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                a[v] = 1.f;
-                da[v] = 0.f;
-            }
+            for (int v = 1; v < V; ++v)
+                if (v >= own) q[v] = t[v];
         }
     }
 };
 
-template <typename T, int V>
-__device__ __forceinline__ void load_row(const void *p, int64_t ld, int k, int col0, int n, float (&x)[V]) {
-    load_columns<T, V>(static_cast<const T *>(p) + (int64_t)k * ld + col0, n, x);
+// f(rows, k): the rows k, k + TY, ... of a range, U of them at a time while there are as many
+template <int U, typename F>
+__device__ __forceinline__ void for_rows(int k, int k1, int TY, F f) {
+    for (; k + (U - 1) * TY < k1; k += U * TY) f(std::integral_constant<int, U>{}, k);
+    for (; k < k1; k += TY) f(std::integral_constant<int, 1>{}, k);
 }
 
-// Joins the sums of a workgroup's threads over the rows and stores them: part[q][split][B]
-template <int V, int NS>
-__device__ __forceinline__ void store_sums(const double (&sum)[NS][V], const norm_grid &g, const columns<V> &c, int B,
+// Joins the sums of a workgroup's threads over the rows and stores them: part[q][split][B].  Two sums at a time lie in LDS,
+// and every thread joins a column of them.
+template <int V>
+constexpr int kSumsValues = 2 * V * kPassThreads;
+template <typename T, int V, int NS>
+__device__ __forceinline__ void store_sums(const double (&sum)[NS][V], const norm_grid &g, const columns<T, V> &c, int B,
                                            double *lds, double *part) {
-    const int TX = 1 << g.tx_shift, TY = kThreads >> g.tx_shift;
-    const int tx = threadIdx.x & (TX - 1), ty = threadIdx.x >> g.tx_shift;
+    static_assert(NS % 2 == 0, "two sums at a time");
+    const int TX = 1 << g.tx_shift, TY = kPassThreads >> g.tx_shift, width = TX * V;
+    const int ty = threadIdx.x >> g.tx_shift;
+    const int64_t first = ((int64_t)blockIdx.x << g.tx_shift) * V;
+    // (the place of a column: its thread's within those of the same v)
+    auto place = [&](int column) { return column % V * TX + column / V; };
 #pragma unroll
-    for (int q = 0; q < NS; ++q) {
+    for (int q = 0; q < NS; q += 2) {
         __syncthreads();
 #pragma unroll
-        for (int v = 0; v < V; ++v) lds[v * kThreads + threadIdx.x] = sum[q][v];
-        __syncthreads();
-        if (ty == 0) {
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                double t = 0;
-                for (int y = 0; y < TY; ++y) t += lds[v * kThreads + (y << g.tx_shift) + tx];
-                if (v < c.n) part[((int64_t)q * g.splits + blockIdx.y) * B + c.col0 + v] = t;
+        for (int v = 0; v < V; ++v)
+            if (v >= c.own) {
+                const int at = place((int)(c.col + v - first));
+                lds[ty * width + at] = sum[q][v];
+                lds[(TY + ty) * width + at] = sum[q + 1][v];
             }
+        __syncthreads();
+        for (int j = threadIdx.x; j < 2 * width; j += kPassThreads) {
+            const int i = j >= width ? 1 : 0, at = j - i * width;
+            const int64_t col = first + (at & (TX - 1)) * V + (at >> g.tx_shift);
+            if (col >= B) continue;
+            double t = 0;
+            for (int y = 0; y < TY; ++y) t += lds[(i * TY + y) * width + at];
+            part[((int64_t)(q + i) * g.splits + blockIdx.y) * B + col] = t;
         }
     }
 }
@@ -135,6 +540,7 @@ __device__ __forceinline__ bool join_sums(const double *__restrict__ part, int s
     for (int q = 0; q < NS; ++q) {
         double t = 0;
         if (col < B)
+#pragma unroll 8
             for (int i = way; i < splits; i += ways) t += part[((int64_t)q * splits + i) * B + col];
         lds[q * kThreads + threadIdx.x] = t;
     }
@@ -148,47 +554,60 @@ __device__ __forceinline__ bool join_sums(const double *__restrict__ part, int s
     return true;
 }
 
-// ---------------------------------------------------------------------------
-// forward
-// ---------------------------------------------------------------------------
-
-// what a call has: y (with gate), a norm of y, a norm of r'
+// What a call has: y, a norm of y, a norm of r'
 enum { kHasY = 1, kHasPost = 2, kHasPre = 4 };
 
-template <typename T, int V, int GATE, bool SIGMOID, int HAS>
-__global__ __launch_bounds__(kThreads) void forward_sums_kernel(norm_args A, norm_grid g, double *__restrict__ part) {
+template <typename T, int V, int HAS>
+__global__ __launch_bounds__(kPassThreads) void forward_sums_kernel(norm_args A, norm_grid g, double *__restrict__ part) {
     constexpr int NS = 4;  // y^2; r^2, r x, x^2 (without post: r'^2 alone)
-    __shared__ double lds[kThreads * V];
-    const int TX = 1 << g.tx_shift, TY = kThreads >> g.tx_shift;
+    constexpr bool has_y = (HAS & kHasY) != 0, post = (HAS & kHasPost) != 0, pre = (HAS & kHasPre) != 0;
+    __shared__ double lds[kSumsValues<V>];
+    const int TX = 1 << g.tx_shift, TY = kPassThreads >> g.tx_shift;
     const int tx = threadIdx.x & (TX - 1), ty = threadIdx.x >> g.tx_shift;
-    const columns<V> c(tx, g.tx_shift, A.B);
+    const columns<T, V> c(tx, g.tx_shift, A.B);
+    const int k0 = blockIdx.y * g.rows + ty, k1 = (int)min((int64_t)A.K, (int64_t)(blockIdx.y + 1) * g.rows);
+    const bool full = A.gate_kind == kGateFull;
     double sum[NS][V] = {};
-    const int k1 = min(A.K, (int)(blockIdx.y + 1) * g.rows);
-    if (c.n > 0)
-        for (int k = blockIdx.y * g.rows + ty; k < k1; k += TY) {
-            float r[V], y[V];
-            if constexpr (HAS & kHasPre) load_row<T, V>(A.r, A.ldr, k, c.col0, c.n, r);
-            if constexpr (HAS & kHasY) load_row<T, V>(A.y, A.ldy, k, c.col0, c.n, y);
-            const gate_values<T, V, GATE, SIGMOID> gate(A, k, c.col0, c.n);
-            const float w = HAS & kHasPost ? A.post_gain[k] : 1.f;
+    for_rows<2>(k0, k1, TY, [&](auto rows, int k) {
+        constexpr int U = decltype(rows)::value;
+        T r[U][V], y[U][V], gate[U][V];
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                if constexpr (HAS & kHasPost) sum[0][v] += (double)y[v] * y[v];
-                if constexpr (HAS & kHasPre) {
-                    if constexpr (HAS & kHasPost) {
-                        const double x = (double)(A.alpha * gate.a[v] * w) * y[v];
-                        sum[1][v] += (double)r[v] * r[v];
-                        sum[2][v] += r[v] * x;
+        for (int u = 0; u < U; ++u) {
+            if (pre) c.load(A.r, A.ldr, k + u * TY, r[u]);
+            if (has_y) c.load(A.y, A.ldy, k + u * TY, y[u]);
+        }
+        if (full && pre) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) c.load(A.gate, A.ldg, k + u * TY, gate[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if constexpr (post) {
+#pragma unroll
+                for (int v = 0; v < V; ++v) sum[0][v] += (double)widen(y[u][v]) * widen(y[u][v]);
+            }
+            if constexpr (pre && !has_y) {
+#pragma unroll
+                for (int v = 0; v < V; ++v) sum[1][v] += (double)widen(r[u][v]) * widen(r[u][v]);
+            }
+            if constexpr (pre && has_y) {
+                const gate_values<T, V> a(A, k + u * TY, gate[u]);
+                const float w = A.alpha * (post ? A.post_gain[k + u * TY] : 1.f);
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    const double x = (double)(a.a[v] * w) * widen(y[u][v]), rr = widen(r[u][v]);
+                    if constexpr (post) {
+                        sum[1][v] += rr * rr;
+                        sum[2][v] += rr * x;
                         sum[3][v] += x * x;
                     } else {
-                        double x = r[v];
-                        if constexpr (HAS & kHasY) x += (double)(A.alpha * gate.a[v]) * y[v];
-                        sum[1][v] += x * x;
+                        sum[1][v] += (rr + x) * (rr + x);
                     }
                 }
             }
         }
-    store_sums<V, NS>(sum, g, c, A.B, lds, part);
+    });
+    store_sums<T, V, NS>(sum, g, c, A.B, lds, part);
 }
 
 // a column's factors: q, s
@@ -205,85 +624,111 @@ __global__ __launch_bounds__(kThreads) void forward_join_kernel(int K, int B, fl
     fac[B + col] = (float)(1 / sqrt((square < 0 ? 0 : square) / K + eps));  // (a NaN stays one)
 }
 
-template <typename T, int V, int GATE, bool SIGMOID, int HAS>
-__global__ __launch_bounds__(kThreads) void forward_kernel(norm_args A, norm_grid g, const float *__restrict__ fac) {
-    const int TX = 1 << g.tx_shift, TY = kThreads >> g.tx_shift;
+template <typename T, int V>
+__global__ __launch_bounds__(kPassThreads) void forward_kernel(norm_args A, norm_grid g, const float *__restrict__ fac) {
+    const int TX = 1 << g.tx_shift, TY = kPassThreads >> g.tx_shift;
     const int tx = threadIdx.x & (TX - 1), ty = threadIdx.x >> g.tx_shift;
-    const columns<V> c(tx, g.tx_shift, A.B);
-    if (c.n <= 0) return;
+    const columns<T, V> c(tx, g.tx_shift, A.B);
+    const int k0 = blockIdx.y * g.rows + ty, k1 = (int)min((int64_t)A.K, (int64_t)(blockIdx.y + 1) * g.rows);
+    if (c.own >= V) return;
+    const bool has_y = A.y != nullptr, post = A.post_gain != nullptr, pre = A.pre_gain != nullptr, full = A.gate_kind == kGateFull;
     float q[V], s[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        const int col = c.col0 + min(v, c.n - 1);
-        q[v] = HAS & kHasPost ? fac[col] : 1.f;
-        s[v] = HAS & kHasPre ? fac[A.B + col] : 0.f;
+        q[v] = post ? fac[c.col + v] : 1.f;
+        s[v] = pre ? fac[A.B + c.col + v] : 0.f;
     }
-    const int k1 = min(A.K, (int)(blockIdx.y + 1) * g.rows);
-    for (int k = blockIdx.y * g.rows + ty; k < k1; k += TY) {
-        float r[V], y[V];
-        load_row<T, V>(A.r, A.ldr, k, c.col0, c.n, r);
-        if constexpr (HAS & kHasY) {
-            load_row<T, V>(A.y, A.ldy, k, c.col0, c.n, y);
-            const gate_values<T, V, GATE, SIGMOID> gate(A, k, c.col0, c.n);
-            const float w = HAS & kHasPost ? A.post_gain[k] : 1.f;
+    for_rows<2>(k0, k1, TY, [&](auto rows, int k) {
+        constexpr int U = decltype(rows)::value;
+        T r[U][V], y[U][V], gate[U][V];
 #pragma unroll
-            for (int v = 0; v < V; ++v) r[v] += A.alpha * gate.a[v] * w * (y[v] * q[v]);
-            store_columns<T, V>(static_cast<T *>(A.r_out) + (int64_t)k * A.ldro + c.col0, c.n, r);
+        for (int u = 0; u < U; ++u) {
+            c.load(A.r, A.ldr, k + u * TY, r[u]);
+            if (has_y) c.load(A.y, A.ldy, k + u * TY, y[u]);
         }
-        if constexpr (HAS & kHasPre) {
-            const float w = A.pre_gain[k];
+        if (full) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) r[v] = r[v] * s[v] * w;
-            store_columns<T, V>(static_cast<T *>(A.h) + (int64_t)k * A.ldh + c.col0, c.n, r);
+            for (int u = 0; u < U; ++u) c.load(A.gate, A.ldg, k + u * TY, gate[u]);
         }
-    }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float x[V];
+#pragma unroll
+            for (int v = 0; v < V; ++v) x[v] = widen(r[u][v]);
+            if (has_y) {
+                const gate_values<T, V> a(A, k + u * TY, gate[u]);
+                const float w = A.alpha * (post ? A.post_gain[k + u * TY] : 1.f);
+#pragma unroll
+                for (int v = 0; v < V; ++v) x[v] += a.a[v] * w * (widen(y[u][v]) * q[v]);
+                c.store(A.r_out, A.ldro, k + u * TY, x);
+            }
+            if (pre) {
+                const float w = A.pre_gain[k + u * TY];
+#pragma unroll
+                for (int v = 0; v < V; ++v) x[v] = x[v] * s[v] * w;
+                c.store(A.h, A.ldh, k + u * TY, x);
+            }
+        }
+    });
 }
 
-// ---------------------------------------------------------------------------
-// backward
-// ---------------------------------------------------------------------------
-
-template <typename T, int V, int GATE, bool SIGMOID, int HAS>
-__global__ __launch_bounds__(kThreads) void backward_sums_kernel(norm_args A, norm_grid g, double *__restrict__ part) {
+template <typename T, int V, int HAS>
+__global__ __launch_bounds__(kPassThreads) void backward_sums_kernel(norm_args A, norm_grid g, double *__restrict__ part) {
     constexpr int NS = kSums;  // r'^2, u r'; y^2, k y dr', k y u, k y r'
-    __shared__ double lds[kThreads * V];
-    const int TX = 1 << g.tx_shift, TY = kThreads >> g.tx_shift;
+    constexpr bool post = (HAS & kHasPost) != 0, pre = (HAS & kHasPre) != 0;
+    __shared__ double lds[kSumsValues<V>];
+    const int TX = 1 << g.tx_shift, TY = kPassThreads >> g.tx_shift;
     const int tx = threadIdx.x & (TX - 1), ty = threadIdx.x >> g.tx_shift;
-    const columns<V> c(tx, g.tx_shift, A.B);
+    const columns<T, V> c(tx, g.tx_shift, A.B);
+    const int k0 = blockIdx.y * g.rows + ty, k1 = (int)min((int64_t)A.K, (int64_t)(blockIdx.y + 1) * g.rows);
+    const bool full = A.gate_kind == kGateFull, more = A.dr_out != nullptr;
+    // (without dr_out r' is read in its place and not used: zeros put there instead would wait for every load ahead)
+    const void *dr_out = more ? A.dr_out : A.r_out;
+    const int64_t lddro = more ? A.lddro : A.ldro;
     double sum[NS][V] = {};
-    const int k1 = min(A.K, (int)(blockIdx.y + 1) * g.rows);
-    if (c.n > 0)
-        for (int k = blockIdx.y * g.rows + ty; k < k1; k += TY) {
-            float r[V], u[V] = {}, y[V], dr[V] = {};
-            if constexpr (HAS & kHasPre) {
-                load_row<T, V>(A.r_out, A.ldro, k, c.col0, c.n, r);
-                load_row<T, V>(A.dh, A.lddh, k, c.col0, c.n, u);
-                const float w = A.pre_gain[k];
+    for_rows<2>(k0, k1, TY, [&](auto rows, int k) {
+        constexpr int U = decltype(rows)::value;
+        T r[U][V], dh[U][V], y[U][V], dr[U][V], gate[U][V];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (pre) c.load(A.r_out, A.ldro, k + u * TY, r[u]);
+            if (pre) c.load(A.dh, A.lddh, k + u * TY, dh[u]);
+            if (post) c.load(A.y, A.ldy, k + u * TY, y[u]);
+            if (post) c.load(dr_out, lddro, k + u * TY, dr[u]);
+        }
+        if (post && full) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) c.load(A.gate, A.ldg, k + u * TY, gate[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float d[V];
+            if constexpr (pre) {
+                const float w = A.pre_gain[k + u * TY];
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
-                    u[v] *= w;
-                    sum[0][v] += (double)r[v] * r[v];
-                    sum[1][v] += (double)u[v] * r[v];
+                    d[v] = widen(dh[u][v]) * w;
+                    sum[0][v] += (double)widen(r[u][v]) * widen(r[u][v]);
+                    sum[1][v] += (double)d[v] * widen(r[u][v]);
                 }
             }
-            if constexpr (HAS & kHasPost) {
-                load_row<T, V>(A.y, A.ldy, k, c.col0, c.n, y);
-                if (A.dr_out) load_row<T, V>(A.dr_out, A.lddro, k, c.col0, c.n, dr);
-                const gate_values<T, V, GATE, SIGMOID> gate(A, k, c.col0, c.n);
-                const float w = A.post_gain[k];
+            if constexpr (post) {
+                const gate_values<T, V> a(A, k + u * TY, gate[u]);
+                const float w = A.alpha * A.post_gain[k + u * TY];
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
-                    const double ky = (double)(A.alpha * gate.a[v] * w) * y[v];
-                    sum[2][v] += (double)y[v] * y[v];
-                    sum[3][v] += ky * dr[v];
-                    if constexpr (HAS & kHasPre) {
-                        sum[4][v] += ky * u[v];
-                        sum[5][v] += ky * r[v];
+                    const double yy = widen(y[u][v]), ky = (double)(a.a[v] * w) * yy;
+                    sum[2][v] += yy * yy;
+                    sum[3][v] += more ? ky * widen(dr[u][v]) : 0;
+                    if constexpr (pre) {
+                        sum[4][v] += ky * d[v];
+                        sum[5][v] += ky * widen(r[u][v]);
                     }
                 }
             }
         }
-    store_sums<V, NS>(sum, g, c, A.B, lds, part);
+    });
+    store_sums<T, V, NS>(sum, g, c, A.B, lds, part);
 }
 
 // a column's factors: s, f = s^2 c, q, g = q^2 e
@@ -308,79 +753,105 @@ __global__ __launch_bounds__(kThreads) void backward_join_kernel(int K, int B, f
 }
 
 // Sums over a workgroup's columns of a row go to rows[i][column block][K], i = dw_pre, dw_post, dgate
-template <typename T, int V, int GATE, bool SIGMOID, int HAS>
-__global__ __launch_bounds__(kThreads) void backward_kernel(norm_args A, norm_grid g, const float *__restrict__ fac,
-                                                            float *__restrict__ rows) {
-    const int TX = 1 << g.tx_shift, TY = kThreads >> g.tx_shift;
+template <typename T, int V>
+__global__ __launch_bounds__(kPassThreads) void backward_kernel(norm_args A, norm_grid g, const float *__restrict__ fac,
+                                                                float *__restrict__ rows_out) {
+    const int TX = 1 << g.tx_shift, TY = kPassThreads >> g.tx_shift;
     const int tx = threadIdx.x & (TX - 1), ty = threadIdx.x >> g.tx_shift;
-    const columns<V> c(tx, g.tx_shift, A.B);
-    float s[V] = {}, f[V] = {}, q[V], e[V] = {};
+    const columns<T, V> c(tx, g.tx_shift, A.B);
+    const int k0 = blockIdx.y * g.rows + ty, k1 = (int)min((int64_t)A.K, (int64_t)(blockIdx.y + 1) * g.rows);
+    const bool has_y = A.y != nullptr, post = A.post_gain != nullptr, pre = A.pre_gain != nullptr, more = A.dr_out != nullptr;
+    const bool full = A.gate_kind == kGateFull, row = A.gate_kind == kGateRow;
+    const void *dr_out = more ? A.dr_out : A.r_out;  // (as in the sums)
+    const int64_t lddro = more ? A.lddro : A.ldro;
+    float s[V], f[V], q[V], e[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        const int col = min(c.col0 + v, A.B - 1);
-        s[v] = HAS & kHasPre ? fac[col] : 0.f;
-        f[v] = HAS & kHasPre ? fac[A.B + col] : 0.f;
-        q[v] = HAS & kHasPost ? fac[2 * (int64_t)A.B + col] : 1.f;
-        e[v] = HAS & kHasPost ? fac[3 * (int64_t)A.B + col] : 0.f;
+        const int col = c.col + v;
+        s[v] = pre ? fac[col] : 0.f;
+        f[v] = pre ? fac[A.B + col] : 0.f;
+        q[v] = post ? fac[2 * (int64_t)A.B + col] : 1.f;
+        e[v] = post ? fac[3 * (int64_t)A.B + col] : 0.f;
     }
-    const int k1 = min(A.K, (int)(blockIdx.y + 1) * g.rows);
-    for (int k = blockIdx.y * g.rows + ty; k < k1; k += TY) {
-        float t[V] = {}, sums[3] = {};
-        if (c.n > 0) {
-            if (A.dr_out) load_row<T, V>(A.dr_out, A.lddro, k, c.col0, c.n, t);
-            if constexpr (HAS & kHasPre) {
-                float r[V], dh[V];
-                load_row<T, V>(A.r_out, A.ldro, k, c.col0, c.n, r);
-                load_row<T, V>(A.dh, A.lddh, k, c.col0, c.n, dh);
+    for_rows<2>(k0, k1, TY, [&](auto rows, int k2) {
+        constexpr int U = decltype(rows)::value;
+        T r[U][V], dh[U][V], y[U][V], dr[U][V], gate[U][V];
+#pragma unroll
+        for (int u = 0; u < U; ++u) c.load(dr_out, lddro, k2 + u * TY, dr[u]);
+        if (pre) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                c.load(A.r_out, A.ldro, k2 + u * TY, r[u]);
+                c.load(A.dh, A.lddh, k2 + u * TY, dh[u]);
+            }
+        }
+        if (has_y) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) c.load(A.y, A.ldy, k2 + u * TY, y[u]);
+        }
+        if (full) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) c.load(A.gate, A.ldg, k2 + u * TY, gate[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int k = k2 + u * TY;
+            float t[V];
+#pragma unroll
+            for (int v = 0; v < V; ++v) t[v] = more ? widen(dr[u][v]) : 0.f;
+            if (pre) {
                 const float w = A.pre_gain[k];
+                float sums = 0.f;
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
-                    const float rs = r[v] * s[v];
-                    sums[0] += v < c.n ? dh[v] * rs : 0.f;
-                    t[v] += s[v] * (dh[v] * w) - f[v] * rs;
+                    const float rs = widen(r[u][v]) * s[v], d = widen(dh[u][v]);
+                    sums += v >= c.own ? d * rs : 0.f;
+                    t[v] += s[v] * (d * w) - f[v] * rs;
                 }
+                c.store(A.dr, A.lddr, k, t);
+                store_row_sum(A, rows_out, 0, g.col_blocks, blockIdx.x, k, tx, TX, sums);
             }
-            if (A.dr) store_columns<T, V>(static_cast<T *>(A.dr) + (int64_t)k * A.lddr + c.col0, c.n, t);
-            if constexpr (HAS & kHasY) {
-                float y[V], dy[V], dg[V];
-                load_row<T, V>(A.y, A.ldy, k, c.col0, c.n, y);
-                const gate_values<T, V, GATE, SIGMOID> gate(A, k, c.col0, c.n);
-                const float w = HAS & kHasPost ? A.post_gain[k] : 1.f;
+            if (!has_y) continue;
+            const gate_values<T, V> a(A, k, gate[u]);
+            const float w = post ? A.post_gain[k] : 1.f;
+            float dy[V], dg[V], sums[2] = {};
 #pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    const float at = A.alpha * t[v], yq = y[v] * q[v];
-                    dy[v] = gate.a[v] * at * w * q[v] - e[v] * yq;
-                    dg[v] = at * yq * w * gate.da[v];
-                    sums[1] += v < c.n ? gate.a[v] * at * yq : 0.f;
-                    sums[2] += v < c.n ? dg[v] : 0.f;
-                }
-                store_columns<T, V>(static_cast<T *>(A.dy) + (int64_t)k * A.lddy + c.col0, c.n, dy);
-                if constexpr (GATE == kGateFull)
-                    store_columns<T, V>(static_cast<T *>(A.dgate) + (int64_t)k * A.lddg + c.col0, c.n, dg);
+            for (int v = 0; v < V; ++v) {
+                const float at = A.alpha * t[v], yq = widen(y[u][v]) * q[v];
+                dy[v] = a.a[v] * at * w * q[v] - e[v] * yq;
+                dg[v] = at * yq * w * a.da[v];
+                sums[0] += v >= c.own ? a.a[v] * at * yq : 0.f;
+                sums[1] += v >= c.own ? dg[v] : 0.f;
             }
+            c.store(A.dy, A.lddy, k, dy);
+            if (full) c.store(A.dgate, A.lddg, k, dg);
+            if (post) store_row_sum(A, rows_out, 1, g.col_blocks, blockIdx.x, k, tx, TX, sums[0]);
+            if (row) store_row_sum(A, rows_out, 2, g.col_blocks, blockIdx.x, k, tx, TX, sums[1]);
         }
-        const int lanes = min(TX, kWave);
-#pragma unroll
-        for (int i = 0; i < 3; ++i) {
-            if (i == 0 ? !(HAS & kHasPre) : i == 1 ? !(HAS & kHasPost) : GATE != kGateRow) continue;
-            for (int d = lanes / 2; d >= 1; d >>= 1) sums[i] += __shfl_xor(sums[i], d, kWave);
-            if (tx == 0) rows[((int64_t)i * gridDim.x + blockIdx.x) * A.K + k] = sums[i];
-        }
-    }
+    });
 }
 
-// a row's sum over the column blocks
+// a row's sum over the blocks of columns: 32 rows and 8 threads to each of a workgroup, blockIdx.y one of the three sums
 __global__ __launch_bounds__(kThreads) void row_sums_kernel(int K, int blocks, const float *__restrict__ rows,
                                                             float *pre, float *post, float *gate) {
-    const int k = blockIdx.x * kThreads + threadIdx.x;
-    if (k >= K) return;
-    float *out[3] = {pre, post, gate};
-    for (int i = 0; i < 3; ++i) {
-        if (out[i] == nullptr) continue;
-        double t = 0;
-        for (int b = 0; b < blocks; ++b) t += rows[((int64_t)i * blocks + b) * K + k];
-        out[i][k] = (float)t;
+    constexpr int width = 32, ways = kThreads / width;
+    __shared__ double lds[kThreads];
+    float *out = blockIdx.y == 0 ? pre : blockIdx.y == 1 ? post : gate;
+    if (out == nullptr) return;
+    const int64_t k = (int64_t)blockIdx.x * width + threadIdx.x % width;
+    const int way = threadIdx.x / width;
+    double t = 0;
+    if (k < K) {
+        const float *p = rows + (int64_t)blockIdx.y * blocks * K + k;
+#pragma unroll 8
+        for (int b = way; b < blocks; b += ways) t += p[(int64_t)b * K];
     }
+    lds[threadIdx.x] = t;
+    __syncthreads();
+    if (way != 0 || k >= K) return;
+    t = 0;
+    for (int i = 0; i < ways; ++i) t += lds[i * width + threadIdx.x];
+    out[k] = (float)t;
 }
 
 // ---------------------------------------------------------------------------
@@ -392,115 +863,180 @@ int vector_of(int B, int dtype) {
     return B >= v ? v : 1;
 }
 
-norm_grid grid_for(int K, int B, int dtype, int *col_blocks) {
+norm_grid grid_for(int K, int B) {
     norm_grid g;
-    const int64_t lanes = ceil_div(B, vector_of(B, dtype));
+    const int64_t lanes = ceil_div(B, B < kPassVector ? 1 : kPassVector);
     g.tx_shift = 0;
     while (g.tx_shift < 6 && (1 << g.tx_shift) < lanes) ++g.tx_shift;
-    *col_blocks = (int)ceil_div(lanes, 1 << g.tx_shift);
-    const int TY = kThreads >> g.tx_shift;
-    // about 2048 workgroups, of 8 rows a thread at least
+    g.col_blocks = (int)ceil_div(lanes, 1 << g.tx_shift);
+    const int TY = kPassThreads >> g.tx_shift;
+    // two workgroups a CU, of 8 rows a thread at least (twice as many leave the join twice the sums and gain nothing)
     const int64_t most = std::min<int64_t>(kMaxSplits, ceil_div(K, 8 * TY));
-    const int64_t splits = std::max<int64_t>(1, std::min<int64_t>(most, 2048 / *col_blocks));
+    const int64_t splits = std::max<int64_t>(1, std::min<int64_t>(most, 512 / g.col_blocks));
     g.rows = (int)(ceil_div(ceil_div(K, splits), TY) * TY);
     g.splits = (int)ceil_div(K, g.rows);
     return g;
 }
 
-template <typename F>
-hipError_t with_gate(int gate, bool sigmoid, F f) {
-    using std::integral_constant;
-    using std::false_type;
-    using std::true_type;
-    if (gate == kGateRow) return sigmoid ? f(integral_constant<int, kGateRow>{}, true_type{}) : f(integral_constant<int, kGateRow>{}, false_type{});
-    if (gate == kGateFull) return sigmoid ? f(integral_constant<int, kGateFull>{}, true_type{}) : f(integral_constant<int, kGateFull>{}, false_type{});
-    return f(integral_constant<int, kGateNone>{}, false_type{});
+constexpr int kStripValues = 72;    // of a thread of the forward strips
+constexpr int kBackwardValues = 16;  // of each of both matrices of the backward ones
+constexpr int kStripFill = 256;      // strips that fill the card
+
+// The widest strips that leave kStripFill of them (a thread's V columns at least) and whose rows are `held` values of a
+// thread at most; returns its rows, 0: there are none
+int rows_held(int K, int B, int V, int dtype, int held, strip_grid *g) {
+    const int64_t lanes = ceil_div(B, V);
+    int shift = 3;
+    auto rows = [&] { return ceil_div(K, kStripThreads >> shift); };
+    if (V == 1) {
+        shift = 0;
+        while ((1 << shift) < lanes) ++shift;  // (fewer than 8 columns)
+    } else {
+        while (shift > 0 && (ceil_div(lanes, 1 << shift) < kStripFill || rows() * V > held || (V == 8 && rows() > 8))) --shift;
+    }
+    if (rows() * V > held || (V == 8 && rows() > 8)) return 0;
+    *g = {shift, (int)ceil_div(lanes, 1 << shift), std::max(1, 128 / (V * (dtype == kTypeF32 ? 4 : 2) << shift))};
+    return (int)rows();
 }
 
-// f(T, V, GATE, SIGMOID, HAS) as compile-time values
-template <typename F>
-hipError_t with_variant(const norm_args &a, F f) {
+// f(T, V, J) as compile-time values, J at least the rows; V is 1 or WIDE (0: 16 bytes)
+template <int HELD, int WIDE, typename F>
+hipError_t with_rows(int V, int dtype, int rows, F f) {
     using std::integral_constant;
-    auto typed = [&](auto t) {
-        using T = decltype(t);
-        auto wide = [&](auto v) {
-            if (a.y == nullptr) return f(t, v, integral_constant<int, kGateNone>{}, std::false_type{}, integral_constant<int, kHasPre>{});
-            return with_gate(a.gate_kind, a.sigmoid, [&](auto gate, auto sig) {
-                if (a.post_gain && a.pre_gain) return f(t, v, gate, sig, integral_constant<int, kHasY | kHasPost | kHasPre>{});
-                if (a.post_gain) return f(t, v, gate, sig, integral_constant<int, kHasY | kHasPost>{});
-                if (a.pre_gain) return f(t, v, gate, sig, integral_constant<int, kHasY | kHasPre>{});
-                return f(t, v, gate, sig, integral_constant<int, kHasY>{});
-            });
-        };
-        return vector_of(a.B, a.dtype) == 1 ? wide(integral_constant<int, 1>{}) : wide(integral_constant<int, kPer16<T>>{});
+    auto by_rows = [&](auto t, auto v) {
+        constexpr int most = HELD / decltype(v)::value;
+        if (rows <= 2) return f(t, v, integral_constant<int, 2>{});
+        if (rows <= 4) return f(t, v, integral_constant<int, 4>{});
+        if constexpr (most >= 8) {
+            if (rows <= 8) return f(t, v, integral_constant<int, 8>{});
+        }
+        if constexpr (most >= 18) {
+            if (rows <= 18) return f(t, v, integral_constant<int, 18>{});
+        }
+        return hipErrorInvalidValue;
     };
-    if (a.dtype == kTypeF32) return typed(float{});
-    if (a.dtype == kTypeBF16) return typed(__bf16{});
-    return typed(_Float16{});
+    auto by_type = [&](auto t) {
+        constexpr int wide = WIDE > 0 ? WIDE : kPer16<decltype(t)>;
+        return V == 1 ? by_rows(t, integral_constant<int, 1>{}) : by_rows(t, integral_constant<int, wide>{});
+    };
+    if (dtype == kTypeF32) return by_type(float{});
+    if (dtype == kTypeBF16) return by_type(__bf16{});
+    return by_type(_Float16{});
+}
+
+template <typename F>
+hipError_t with_vectors(int B, int dtype, F f) {
+    using std::integral_constant;
+    auto by_type = [&](auto t) {
+        return B < kPassVector ? f(t, integral_constant<int, 1>{}) : f(t, integral_constant<int, kPassVector>{});
+    };
+    if (dtype == kTypeF32) return by_type(float{});
+    if (dtype == kTypeBF16) return by_type(__bf16{});
+    return by_type(_Float16{});
+}
+
+// (offsets within a matrix are 32 bits)
+bool short_enough(const norm_args &a) {
+    const int64_t ld = std::max({a.ldr, a.ldy, a.ldg, a.ldro, a.ldh, a.lddro, a.lddh, a.lddr, a.lddy, a.lddg, (int64_t)a.B});
+    return a.K * ld < (int64_t)1 << 30;
+}
+
+int forward_rows(int K, int B, int dtype, strip_grid *g) {
+    const int V = vector_of(B, dtype);
+    return rows_held(K, B, V, dtype, V == 1 ? 18 : kStripValues, g);
+}
+
+// Small matrices, where the launches are what two passes cost.  Larger ones read the gate twice and leave three sums
+// a row of every strip, in pieces of 32 bytes of a row at most: no less than two passes over whole lines take.
+constexpr int64_t kSmallBytes = 8 << 20;  // of a matrix
+int backward_rows(int K, int B, int dtype, strip_grid *g) {
+    if ((int64_t)K * B * (dtype == kTypeF32 ? 4 : 2) > kSmallBytes) return 0;
+    return rows_held(K, B, B < kPassVector ? 1 : kPassVector, dtype, B < kPassVector ? 8 : kBackwardValues, g);
 }
 
 }  // namespace
 
 size_t residual_norm_workspace_bytes(int K, int B) {
     if (K <= 0 || B <= 0) return 0;
-    size_t most = 0;
+    const norm_grid g = grid_for(K, B);
+    size_t most = sizeof(double) * kSums * (size_t)g.splits * B + sizeof(float) * (kFactors * (size_t)B + 3 * (size_t)g.col_blocks * K);
     for (int dtype : {kTypeF32, kTypeBF16}) {
-        int col_blocks;
-        const norm_grid g = grid_for(K, B, dtype, &col_blocks);
-        most = std::max(most, sizeof(double) * kSums * (size_t)g.splits * B +
-                                  sizeof(float) * (kFactors * (size_t)B + 3 * (size_t)col_blocks * K));
+        strip_grid sg;
+        if (backward_rows(K, B, dtype, &sg) > 0) most = std::max(most, sizeof(float) * 3 * (size_t)sg.strips * K);
     }
     return most;
 }
 
 hipError_t launch_residual_norm_fwd(const norm_args &a, void *ws, hipStream_t s) {
     if (a.K == 0 || a.B == 0) return hipSuccess;
-    int col_blocks;
-    const norm_grid g = grid_for(a.K, a.B, a.dtype, &col_blocks);
-    const dim3 grid(col_blocks, g.splits);
+    strip_grid sg;
+    const int rows = short_enough(a) ? forward_rows(a.K, a.B, a.dtype, &sg) : 0;
+    if (rows > 0)
+        return with_rows<kStripValues, 0>(vector_of(a.B, a.dtype), a.dtype, rows, [&](auto t, auto v, auto j) {
+            forward_strip_kernel<decltype(t), decltype(v)::value, decltype(j)::value><<<sg.blocks(), kStripThreads, 0, s>>>(a, sg);
+            return hipGetLastError();
+        });
+    const norm_grid g = grid_for(a.K, a.B);
+    const dim3 grid(g.col_blocks, g.splits);
+    const bool post = a.post_gain != nullptr, pre = a.pre_gain != nullptr;
     double *part = static_cast<double *>(ws);
     float *fac = reinterpret_cast<float *>(part + kSums * (size_t)g.splits * a.B);
-    return with_variant(a, [&](auto t, auto v, auto gate, auto sig, auto has) {
+    return with_vectors(a.B, a.dtype, [&](auto t, auto v) {
         using T = decltype(t);
-        constexpr int V = decltype(v)::value, G = decltype(gate)::value, H = decltype(has)::value;
-        constexpr bool S = decltype(sig)::value;
-        if constexpr ((H & (kHasPost | kHasPre)) != 0) {
-            forward_sums_kernel<T, V, G, S, H><<<grid, kThreads, 0, s>>>(a, g, part);
-            forward_join_kernel<<<(int)ceil_div(a.B, kJoinColumns), kThreads, 0, s>>>(
-                a.K, a.B, a.eps, g.splits, (H & kHasPost) != 0, (H & kHasPre) != 0, part, fac);
+        constexpr int N = decltype(v)::value;
+        if (post || pre) {
+            (a.y == nullptr  ? forward_sums_kernel<T, N, kHasPre>
+             : !post         ? forward_sums_kernel<T, N, kHasY | kHasPre>
+             : !pre          ? forward_sums_kernel<T, N, kHasY | kHasPost>
+                             : forward_sums_kernel<T, N, kHasY | kHasPost | kHasPre>)<<<grid, kPassThreads, 0, s>>>(a, g, part);
+            forward_join_kernel<<<(int)ceil_div(a.B, kJoinColumns), kThreads, 0, s>>>(a.K, a.B, a.eps, g.splits, post, pre,
+                                                                                    part, fac);
         }
-        forward_kernel<T, V, G, S, H><<<grid, kThreads, 0, s>>>(a, g, fac);
+        forward_kernel<T, N><<<grid, kPassThreads, 0, s>>>(a, g, fac);
         return hipGetLastError();
     });
 }
 
 hipError_t launch_residual_norm_bwd(const norm_args &a, void *ws, hipStream_t s) {
     if (a.K == 0) return hipSuccess;
-    if (a.B == 0) {
-        row_sums_kernel<<<(int)ceil_div(a.K, kThreads), kThreads, 0, s>>>(a.K, 0, nullptr, a.dpre_gain, a.dpost_gain,
-                                                                         a.gate_kind == kGateRow ? static_cast<float *>(a.dgate) : nullptr);
+    const bool post = a.post_gain != nullptr, pre = a.pre_gain != nullptr;
+    float *dgate = a.gate_kind == kGateRow ? static_cast<float *>(a.dgate) : nullptr;
+    auto join_rows = [&](int blocks, const float *rows) {
+        if (a.dpre_gain || a.dpost_gain || dgate)
+            row_sums_kernel<<<dim3((unsigned)ceil_div(a.K, 32), 3), kThreads, 0, s>>>(a.K, blocks, rows, a.dpre_gain, a.dpost_gain,
+                                                                                    dgate);
         return hipGetLastError();
+    };
+    if (a.B == 0) return join_rows(0, nullptr);
+    strip_grid sg;
+    const int held = short_enough(a) ? backward_rows(a.K, a.B, a.dtype, &sg) : 0;
+    if (held > 0) {
+        float *rows = static_cast<float *>(ws);
+        const hipError_t err = with_rows<kBackwardValues, kPassVector>(a.B < kPassVector ? 1 : kPassVector, a.dtype, held, [&](auto t, auto v, auto j) {
+            backward_strip_kernel<decltype(t), decltype(v)::value, decltype(j)::value>
+                <<<sg.blocks(), kStripThreads, 0, s>>>(a, sg, rows);
+            return hipGetLastError();
+        });
+        return err != hipSuccess ? err : join_rows(sg.strips, rows);
     }
-    int col_blocks;
-    const norm_grid g = grid_for(a.K, a.B, a.dtype, &col_blocks);
-    const dim3 grid(col_blocks, g.splits);
+    const norm_grid g = grid_for(a.K, a.B);
+    const dim3 grid(g.col_blocks, g.splits);
     double *part = static_cast<double *>(ws);
     float *fac = reinterpret_cast<float *>(part + kSums * (size_t)g.splits * a.B), *rows = fac + kFactors * (size_t)a.B;
-    return with_variant(a, [&](auto t, auto v, auto gate, auto sig, auto has) {
+    const hipError_t err = with_vectors(a.B, a.dtype, [&](auto t, auto v) {
         using T = decltype(t);
-        constexpr int V = decltype(v)::value, G = decltype(gate)::value, H = decltype(has)::value;
-        constexpr bool S = decltype(sig)::value;
-        if constexpr ((H & (kHasPost | kHasPre)) != 0) {
-            backward_sums_kernel<T, V, G, S, H><<<grid, kThreads, 0, s>>>(a, g, part);
-            backward_join_kernel<<<(int)ceil_div(a.B, kJoinColumns), kThreads, 0, s>>>(
-                a.K, a.B, a.eps, g.splits, (H & kHasPost) != 0, (H & kHasPre) != 0, part, fac);
+        constexpr int N = decltype(v)::value;
+        if (post || pre) {
+            (!post  ? backward_sums_kernel<T, N, kHasPre>
+             : !pre ? backward_sums_kernel<T, N, kHasPost>
+                    : backward_sums_kernel<T, N, kHasPost | kHasPre>)<<<grid, kPassThreads, 0, s>>>(a, g, part);
+            backward_join_kernel<<<(int)ceil_div(a.B, kJoinColumns), kThreads, 0, s>>>(a.K, a.B, a.eps, g.splits, post, pre,
+                                                                                     part, fac);
         }
-        backward_kernel<T, V, G, S, H><<<grid, kThreads, 0, s>>>(a, g, fac, rows);
-        float *dgate = G == kGateRow ? static_cast<float *>(a.dgate) : nullptr;
-        if (a.dpre_gain || a.dpost_gain || dgate)
-            row_sums_kernel<<<(int)ceil_div(a.K, kThreads), kThreads, 0, s>>>(a.K, col_blocks, rows, a.dpre_gain, a.dpost_gain, dgate);
+        backward_kernel<T, N><<<grid, kPassThreads, 0, s>>>(a, g, fac, rows);
         return hipGetLastError();
     });
+    return err != hipSuccess ? err : join_rows(g.col_blocks, rows);
 }
 
 }  // namespace l1csr
