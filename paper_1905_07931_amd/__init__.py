@@ -13,6 +13,7 @@ import ctypes as C
 import functools
 import math
 import os
+from array import array
 from dataclasses import dataclass
 
 __all__ = [
@@ -336,11 +337,18 @@ def _mat(t, name):
 _DTYPES: dict = {}  # torch dtype -> l1csr_dtype
 
 
+def _kinds():
+    """The element types of the calls that take more than float32: torch dtype -> l1csr_dtype."""
+    if not _DTYPES:
+        torch = _torch()
+        _DTYPES.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
+    return _DTYPES
+
+
 def _dtype_code(t, name):
     """l1csr_dtype of a GPU tensor."""
     torch = _torch_module or _torch()
-    if not _DTYPES:
-        _DTYPES.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
+    _kinds()
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if not t.is_cuda:
@@ -1517,10 +1525,24 @@ def prox_muon_recompress(W: CSR, G, st: MuonState, eta, lam, O=None, capacity=No
 # around the layers of a network on tokens
 # ---------------------------------------------------------------------------
 
+def _ld_of(t, rows, cols, dtype, index):
+    """The leading dimension of a sound [rows][cols] matrix of `dtype` on device `index`, -1 for any other."""
+    if not isinstance(t, _torch_module.Tensor) or t.dtype is not dtype or t.shape != (rows, cols) or t.get_device() != index:
+        return -1
+    ld, unit = t.stride()
+    if rows <= 1:
+        ld = max(cols, 1)
+    return ld if (unit == 1 or cols <= 1) and ld >= cols else -1
+
+
 def _out_mat(t, shape, dtypes, index, name, what, device, stream):
     """A call's output matrix, the caller's or a new one of the first type; returns (tensor, ld, l1csr_dtype)."""
     if t is None:
         t = _new(shape, dtypes[0], device, stream)
+    for dtype in dtypes:
+        ld = _ld_of(t, *shape, dtype, index)
+        if ld >= 0:
+            return t, ld, _kinds()[dtype]
     rows, cols, ld, code = _typed_mat(t, name)
     if (rows, cols) != tuple(shape) or t.dtype not in dtypes:
         raise ValueError(f"{name} must be {what}")
@@ -1540,9 +1562,8 @@ def embedding_fwd(E, tokens, X=None, scale=1.0, dtype=None, stream=None):
     E is a table [V][D] (float32, bfloat16 or float16, features contiguous, as a layer's weights) or a CSR (V x D);
     tokens int32 [B]; X [D][B] of the table's type or float32 (dtype: which a new one has; default the table's).  Returns X."""
     torch = _torch()
-    _dev(tokens, torch.int32, "tokens")
-    index = _device_of(tokens)
     _vec(tokens, torch.int32, "tokens")
+    index = _device_of(tokens)
     B = tokens.numel()
     if isinstance(E, CSR):
         nnz = E.validate_shapes()
@@ -1579,9 +1600,8 @@ def embedding_plan(tokens, n_rows, plan: EmbeddingPlan | None = None, stream=Non
     on the tokens alone, so it can be made beside the forward pass and serves every gradient of the batch.  A plan given
     is filled again (its buffer, where that is large enough)."""
     torch = _torch()
-    _dev(tokens, torch.int32, "tokens")
-    index = _device_of(tokens)
     _vec(tokens, torch.int32, "tokens")
+    index = _device_of(tokens)
     B, n_rows = tokens.numel(), int(n_rows)
     need = workspace_bytes(OP_EMBEDDING_PLAN, n_rows, 0, 0, B)
     if plan is None:
@@ -1595,17 +1615,24 @@ def embedding_plan(tokens, n_rows, plan: EmbeddingPlan | None = None, stream=Non
     return plan
 
 
-def _embedding_order(tokens, n_rows, B, plan, index, stream):
-    """The plan of a gradient's call: the caller's, or one made here."""
-    torch = _torch_module
-    if plan is None:
-        _vec_of(tokens, torch.int32, B, index, "tokens", "token (B)")
-        return embedding_plan(tokens, n_rows, stream=stream)
-    if plan.n_rows != n_rows or plan.B != B:
-        raise ValueError("the plan is of another table or batch")
-    if plan.buf is not None:
-        _same_device(index, plan.buf, "the plan")
-    return plan
+def _embedding_scratch(tokens, n_rows, D, B, plan, device, index, stream):
+    """The plan and the workspace of a gradient's call, (address, bytes) each; a plan that the caller has not is made behind
+    the workspace."""
+    need = workspace_bytes(OP_EMBEDDING_BWD, n_rows, D, 0, B)
+    if plan is not None:
+        if plan.n_rows != n_rows or plan.B != B:
+            raise ValueError("the plan is of another table or batch")
+        if plan.buf is not None:
+            _same_device(index, plan.buf, "the plan")
+        ws, _ = _workspace(need, device, stream)
+        return (None, 0) if plan.buf is None else (plan.buf.data_ptr(), plan.buf.numel()), _p(ws), need, plan.buf, ws
+    _vec_of(tokens, _torch_module.int32, B, index, "tokens", "token (B)")
+    room = workspace_bytes(OP_EMBEDDING_PLAN, n_rows, 0, 0, B)
+    ws, _ = _workspace(need + room, device, stream)
+    at = None if ws is None else ws.data_ptr()
+    order = (None, 0) if room == 0 else (at + need, room)
+    _check(lib().l1csr_embedding_plan(n_rows, B, tokens.data_ptr(), *order, _stream(stream)), "l1csr_embedding_plan")
+    return order, at, need, None, ws
 
 
 def embedding_bwd(dX, tokens, n_rows, dE=None, scale=1.0, add=None, plan: EmbeddingPlan | None = None, stream=None):
@@ -1627,11 +1654,10 @@ def embedding_bwd(dX, tokens, n_rows, dE=None, scale=1.0, add=None, plan: Embedd
         _, ldadd, acode = _out_mat(add, (n_rows, D), (dE.dtype,), index, "add", "of dE's shape and type", dX.device, stream)
         if n_rows == 1 and add.data_ptr() == dE.data_ptr():
             ldadd = ldde
-    plan = _embedding_order(tokens, n_rows, B, plan, index, stream)
-    ws, wsb = _workspace(workspace_bytes(OP_EMBEDDING_BWD, n_rows, D, 0, B), dX.device, stream)
-    _check(lib().l1csr_embedding_bwd(n_rows, D, B, code, dX.data_ptr(), lddx, _p(plan.buf),
-                                     0 if plan.buf is None else plan.buf.numel(), scale, ecode, _p(add), ldadd,
-                                     dE.data_ptr(), ldde, _p(ws), wsb, _stream(stream)), "l1csr_embedding_bwd")
+    order, ws, wsb, *_ = held = _embedding_scratch(tokens, n_rows, D, B, plan, dX.device, index, stream)
+    _check(lib().l1csr_embedding_bwd(n_rows, D, B, code, dX.data_ptr(), lddx, *order, scale, ecode, _p(add), ldadd,
+                                     dE.data_ptr(), ldde, ws, wsb, _stream(stream)), "l1csr_embedding_bwd")
+    del held  # (the buffers live until the call has been made)
     return dE
 
 
@@ -1652,16 +1678,18 @@ def embedding_masked_bwd(W: CSR, dX, tokens, gv=None, scale=1.0, plan: Embedding
     _same_device(index, gv, "gv")
     if gv.numel() < nnz:
         raise ValueError("gv must hold nnz values")
-    plan = _embedding_order(tokens, W.n_rows, B, plan, index, stream)
-    ws, wsb = _workspace(workspace_bytes(OP_EMBEDDING_BWD, W.n_rows, D, 0, B), dX.device, stream)
-    _check(lib().l1csr_embedding_masked_bwd(W.n_rows, D, nnz, _p(W.row_ptr), _p(W.col_idx), B, dX.data_ptr(), lddx,
-                                            _p(plan.buf), 0 if plan.buf is None else plan.buf.numel(), scale, _p(gv), _p(ws),
-                                            wsb, _stream(stream)), "l1csr_embedding_masked_bwd")
+    order, ws, wsb, *_ = held = _embedding_scratch(tokens, W.n_rows, D, B, plan, dX.device, index, stream)
+    _check(lib().l1csr_embedding_masked_bwd(W.n_rows, D, nnz, _p(W.row_ptr), _p(W.col_idx), B, dX.data_ptr(), lddx, *order,
+                                            scale, _p(gv), ws, wsb, _stream(stream)), "l1csr_embedding_masked_bwd")
+    del held
     return gv
 
 
 def _norm_like(t, K, B, dtype, index, name):
     """A matrix of a norm call; returns its leading dimension."""
+    ld = _ld_of(t, K, B, dtype, index)
+    if ld >= 0:
+        return ld
     rows, cols, ld, _ = _typed_mat(t, name)
     if rows != K or cols != B or t.dtype is not dtype:
         raise ValueError(f"{name} must have the shape and type of the residual")
@@ -1713,13 +1741,17 @@ def residual_norm_fwd(r, y=None, gate=None, post_gain=None, pre_gain=None, alpha
         raise ValueError("r_out needs y, h needs pre_gain")
     ldro = ldh = 0
     if y is not None:
-        r_out = _new((K, B), dtype, r.device, stream) if r_out is None else r_out
-        ldro = _norm_like(r_out, K, B, dtype, index, "r_out")
-        ldro = _same_ld(r_out, _same_ld(r_out, ldro, y, ldy, K), r, ldr, K)
+        if r_out is None:
+            r_out, ldro = _new((K, B), dtype, r.device, stream), max(B, 1)
+        else:
+            ldro = _norm_like(r_out, K, B, dtype, index, "r_out")
+            ldro = _same_ld(r_out, _same_ld(r_out, ldro, y, ldy, K), r, ldr, K)
     if pre_gain is not None:
-        h = _new((K, B), dtype, r.device, stream) if h is None else h
-        ldh = _norm_like(h, K, B, dtype, index, "h")
-        ldh = _same_ld(h, _same_ld(h, ldh, y, ldy, K), r, ldr, K)
+        if h is None:
+            h, ldh = _new((K, B), dtype, r.device, stream), max(B, 1)
+        else:
+            ldh = _norm_like(h, K, B, dtype, index, "h")
+            ldh = _same_ld(h, _same_ld(h, ldh, y, ldy, K), r, ldr, K)
     ws, wsb = _workspace(workspace_bytes(OP_RESIDUAL_NORM, K, 0, 0, B), r.device, stream)
     _check(lib().l1csr_residual_norm_fwd(K, B, code, r.data_ptr(), ldr, _p(y), ldy, kind, 1 if sigmoid else 0, _p(gate), ldg,
                                          _p(post_gain), _p(pre_gain), alpha, eps, _p(r_out), ldro, _p(h), ldh, _p(ws), wsb,
@@ -1761,22 +1793,32 @@ def residual_norm_bwd(r_out, dr_out=None, dh=None, y=None, gate=None, post_gain=
     ldy = 0 if y is None else _norm_like(y, K, B, dtype, index, "y")
     kind, ldg = _gate_args(gate, y, K, B, dtype, index)
     post_gain, pre_gain = _gain(post_gain, K, index, "post_gain"), _gain(pre_gain, K, index, "pre_gain")
-    lddr = lddy = lddg = 0
-    if pre_gain is not None:
-        dr = _new((K, B), dtype, r_out.device, stream) if dr is None else dr
-        lddr = _norm_like(dr, K, B, dtype, index, "dr")
-        lddr = _same_ld(dr, _same_ld(dr, lddr, dr_out, lddro, K), dh, lddh, K)
+    lddr = lddy = lddg = max(B, 1)  # of new ones
+    device = r_out.device
+    if pre_gain is None:
+        dpre = None
+    else:
+        dpre = _new((K,), torch.float32, device, stream)
+        if dr is None:
+            dr = _new((K, B), dtype, device, stream)
+        else:
+            lddr = _same_ld(dr, _same_ld(dr, _norm_like(dr, K, B, dtype, index, "dr"), dr_out, lddro, K), dh, lddh, K)
     if y is not None:
-        dy = _new((K, B), dtype, r_out.device, stream) if dy is None else dy
-        lddy = _same_ld(dy, _norm_like(dy, K, B, dtype, index, "dy"), y, ldy, K)
+        if dy is None:
+            dy = _new((K, B), dtype, device, stream)
+        else:
+            lddy = _same_ld(dy, _norm_like(dy, K, B, dtype, index, "dy"), y, ldy, K)
     if kind == GATE_ROW:
-        dgate = _new((K,), torch.float32, r_out.device, stream) if dgate is None else dgate
-        _vec_of(dgate, torch.float32, K, index, "dgate", "feature (K)")
+        if dgate is None:
+            dgate = _new((K,), torch.float32, device, stream)
+        else:
+            _vec_of(dgate, torch.float32, K, index, "dgate", "feature (K)")
     elif kind == GATE_FULL:
-        dgate = _new((K, B), dtype, r_out.device, stream) if dgate is None else dgate
-        lddg = _same_ld(dgate, _norm_like(dgate, K, B, dtype, index, "dgate"), gate, ldg, K)
-    dpost = None if post_gain is None else _new((K,), torch.float32, r_out.device, stream)
-    dpre = None if pre_gain is None else _new((K,), torch.float32, r_out.device, stream)
+        if dgate is None:
+            dgate = _new((K, B), dtype, device, stream)
+        else:
+            lddg = _same_ld(dgate, _norm_like(dgate, K, B, dtype, index, "dgate"), gate, ldg, K)
+    dpost = None if post_gain is None else _new((K,), torch.float32, device, stream)
     ws, wsb = _workspace(workspace_bytes(OP_RESIDUAL_NORM, K, 0, 0, B), r_out.device, stream)
     _check(lib().l1csr_residual_norm_bwd(K, B, code, r_out.data_ptr(), ldr, _p(dr_out), lddro, _p(dh), lddh, _p(y), ldy, kind,
                                          1 if sigmoid else 0, _p(gate), ldg, _p(post_gain), _p(pre_gain), alpha, eps, _p(dr),
@@ -1788,31 +1830,47 @@ def residual_norm_bwd(r_out, dr_out=None, dh=None, y=None, gate=None, post_gain=
 def _flat(t, index, name):
     """(address, rows, columns, leading dimension, l1csr_dtype) of a gradient: a whole buffer is one row."""
     code = _dtype_code(t, name)
-    if t.get_device() != index:
-        _same_device(index, t, name)
-    n = t.numel()
+    _same_device(index, t, name)
     if t.is_contiguous():
+        n = t.numel()
         return t.data_ptr(), 1, n, n, code
-    if t.dim() == 1 and t.stride(0) != 1 or t.dim() != 2:
+    if t.dim() != 2:
         raise ValueError(f"{name} must be contiguous, or 2-D with a contiguous last dimension")
     rows, cols, ld, code = _typed_mat(t, name)
     return t.data_ptr(), rows, cols, ld, code
 
 
+def _flat_all(tensors, index, name):
+    """_flat of every tensor (several hundred of them: the common case without calls)."""
+    kinds, tensor = _kinds(), _torch_module.Tensor
+    out = []
+    for i, t in enumerate(tensors):
+        if isinstance(t, tensor) and t.dtype in kinds and t.get_device() == index and t.is_contiguous():
+            n = t.numel()
+            out.append((t.data_ptr(), 1, n, n, kinds[t.dtype]))
+        else:
+            out.append(_flat(t, index, f"{name}[{i}]"))
+    return out
+
+
 def _grad_args(grads):
-    """The tensors of a norm call as the C arrays of their addresses and sizes; returns (n, arrays, first tensor's index)."""
-    n = len(grads)
-    if n == 0:
+    """The tensors of a norm call, flat; returns (n, flat, first tensor's device index)."""
+    if not grads:
         raise ValueError("no gradients are given")
     _dtype_code(grads[0], "grads[0]")
     index = _device_of(grads[0])
-    return n, [_flat(t, index, f"grads[{i}]") for i, t in enumerate(grads)], index
+    return len(grads), _flat_all(grads, index, "grads"), index
 
 
-def _arrays(flat):
-    n = len(flat)
-    p, rows, cols, ld, code = zip(*flat)
-    return (C.c_void_p * n)(*p), (C.c_int64 * n)(*rows), (C.c_int64 * n)(*cols), (C.c_int64 * n)(*ld), (C.c_int32 * n)(*code)
+class _Columns:
+    """Flat tensors as the C arrays of their addresses, rows, columns, leading dimensions and types."""
+
+    def __init__(self, flat):
+        p, rows, cols, ld, code = zip(*flat)
+        n = len(p)
+        self.words, self.codes = array("q", (*p, *rows, *cols, *ld)), array("i", code)
+        at = self.words.buffer_info()[0]
+        self.p, self.rows, self.cols, self.ld, self.code = at, at + 8 * n, at + 16 * n, at + 24 * n, self.codes.buffer_info()[0]
 
 
 def grad_norm(grads, grad_scale=1.0, stats=None, stream=None):
@@ -1824,8 +1882,9 @@ def grad_norm(grads, grad_scale=1.0, stats=None, stream=None):
     torch = _torch_module
     stats = _result(stats, 2, grads[0], index, "stats", "statistic (2)", stream)
     ws, wsb = _workspace(workspace_bytes(OP_GRAD_NORM, n, 0, 0, 0), grads[0].device, stream)
-    _check(lib().l1csr_grad_norm(n, *_arrays(flat), grad_scale, stats.data_ptr(), _p(ws), wsb, _stream(stream)),
-           "l1csr_grad_norm")
+    g = _Columns(flat)
+    _check(lib().l1csr_grad_norm(n, g.p, g.rows, g.cols, g.ld, g.code, grad_scale, stats.data_ptr(), _p(ws), wsb,
+                                 _stream(stream)), "l1csr_grad_norm")
     return stats
 
 
@@ -1841,27 +1900,25 @@ def clip_grad_norm(grads, max_norm, grad_scale=1.0, eps=1e-6, out=None, zero_non
     grads = list(grads)
     n, flat, index = _grad_args(grads)
     torch = _torch_module
-    targets = [None] * 3
+    targets, o = (None, None, None), None
     if out is not None:
         out = list(out)
         if len(out) != n:
             raise ValueError("out must hold one tensor per gradient")
-        flat_out = []
-        for i, (g, o) in enumerate(zip(grads, out)):
-            _dtype_code(o, f"out[{i}]")
+        flat_out = _flat_all(out, index, "out")
+        for i, (g, o, f) in enumerate(zip(grads, out, flat_out)):
             if o.shape != g.shape or (o.dtype is not g.dtype and o.dtype is not torch.float32):
                 raise ValueError(f"out[{i}] must have the shape of grads[{i}] and its type or float32")
-            f = _flat(o, index, f"out[{i}]")
             if f[1] != flat[i][1]:  # one of both is whole, the other has rows: both by rows
                 rows, cols = g.shape
                 flat[i] = (flat[i][0], rows, cols, flat[i][3] if flat[i][1] == rows else cols, flat[i][4])
-                f = (f[0], rows, cols, f[3] if f[1] == rows else cols, f[4])
-            flat_out.append(f)
-        p, _, _, ld, code = _arrays(flat_out)
-        targets = [p, ld, code]
+                flat_out[i] = (f[0], rows, cols, f[3] if f[1] == rows else cols, f[4])
+        o = _Columns(flat_out)
+        targets = (o.p, o.ld, o.code)
+    g = _Columns(flat)
     stats = _result(stats, 2, grads[0], index, "stats", "statistic (2)", stream)
     ws, wsb = _workspace(workspace_bytes(OP_GRAD_NORM, n, 0, 0, 0), grads[0].device, stream)
-    _check(lib().l1csr_clip_grad_norm(n, *_arrays(flat), *targets, max_norm, grad_scale, eps, 1 if zero_nonfinite else 0,
+    _check(lib().l1csr_clip_grad_norm(n, g.p, g.rows, g.cols, g.ld, g.code, *targets, max_norm, grad_scale, eps, 1 if zero_nonfinite else 0,
                                       stats.data_ptr(), _p(ws), wsb, _stream(stream)), "l1csr_clip_grad_norm")
     return stats
 

@@ -85,7 +85,7 @@ __global__ __launch_bounds__(kThreads) void gather_kernel(int V, int D, int B, c
 
 constexpr int kCsrThreads = 1024;
 constexpr int kCsrTokens = 32;     // of a tile: 128 bytes of a row of X
-constexpr int kCsrFeatures = 512;  // of a tile
+constexpr int kCsrFeatures = 256;  // of a tile
 constexpr int kCsrPitch = kCsrTokens + 1;
 
 // first position of [lo, hi) whose column is c or more, by a whole wave: 64 probes a step

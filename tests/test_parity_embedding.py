@@ -394,3 +394,13 @@ def test_graph_replays():
         for g, t, E, dX, X, dE in sets:
             assert torch.equal(X, L1.embedding_fwd(E, t, scale=2.0))
             assert torch.equal(dE, L1.embedding_bwd(dX, t, V, scale=2.0))
+
+
+def test_first_call_of_a_process():
+    """The table of element types is filled by the call that needs it, whichever comes first."""
+    torch = _torch()
+    rng = np.random.default_rng(0)
+    W, dense, _ = csr_table(5, 4, 0.5, rng)
+    L1._DTYPES.clear()
+    X = L1.embedding_fwd(W, ints([1, 2]), X=torch.empty(4, 2, device=cuda()))
+    assert np.array_equal(h64(X), dense[[1, 2]].T)
