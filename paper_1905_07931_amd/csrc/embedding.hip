@@ -202,9 +202,11 @@ template <bool FIRST>
 __global__ __launch_bounds__(kThreads) void merge_kernel(int V, int B, int64_t run, const int *__restrict__ tokens,
                                                          int *__restrict__ rank, const int *__restrict__ sorted,
                                                          int *__restrict__ merged) {
-    __shared__ __align__(16) int runs[FIRST ? kRun * kWays : 4];
+    __shared__ __align__(16) int runs[FIRST ? kRun * kWays + 1 : 4];  // (an empty range's step looks at the place behind it)
     const int64_t b0 = (int64_t)blockIdx.x * kThreads, b = b0 + threadIdx.x;
+    if constexpr (FIRST) run = kRun;
     const int64_t first = b0 / (run * kWays) * (run * kWays);  // (a run is a multiple of kThreads tokens)
+    const int token = b < B ? tokens[b] : 0, own = b < B ? rank[b] : 0;
     if constexpr (FIRST) {
         const int n = (int)min((int64_t)kRun * kWays, B - first);
         constexpr int N = 4, loads = kRun * kWays / (N * kThreads);
@@ -219,7 +221,7 @@ __global__ __launch_bounds__(kThreads) void merge_kernel(int V, int B, int64_t r
         __syncthreads();
     }
     if (b >= B) return;
-    const int key = key_of(tokens[b], V), q = (int)((b - first) / run);
+    const int key = key_of(token, V), q = (int)((b - first) / run);
     int lo[kWays], n[kWays];
 #pragma unroll
     for (int w = 0; w < kWays; ++w) {
@@ -230,14 +232,14 @@ __global__ __launch_bounds__(kThreads) void merge_kernel(int V, int B, int64_t r
 #pragma unroll
         for (int w = 0; w < kWays; ++w) {
             const int half = n[w] >> 1;
-            const int64_t at = w * run + lo[w] + half;
             // equal tokens of an earlier run go before
-            const bool below = n[w] > 0 && (FIRST ? runs[at] : sorted[first + at]) < key + (w < q ? 1 : 0);
+            const int other = FIRST ? runs[w * kRun + lo[w] + half] : n[w] > 0 ? sorted[first + w * run + lo[w] + half] : 0;
+            const bool below = n[w] > 0 && other < key + (w < q ? 1 : 0);
             lo[w] = below ? lo[w] + half + 1 : lo[w];
             n[w] = below ? n[w] - half - 1 : half;
         }
     }
-    int r = rank[b];
+    int r = own;
 #pragma unroll
     for (int w = 0; w < kWays; ++w) r += lo[w];
     rank[b] = r;
@@ -411,7 +413,7 @@ __global__ __launch_bounds__(kThreads) void group_kernel(int V, int B, int width
     }
 }
 
-constexpr int kRowBlock = 4;  // rows of a workgroup that lie one behind the other
+constexpr int kRowBlock = 4;  // rows of a thread, whose loads are under way together; a grid apart: frequent tokens are neighbours
 
 // dE, every row of it (ALL), or dE += where only the rows that have tokens change: then a workgroup's rows are
 // places in the order, of which the first of each run has work.  blockIdx.y: a range of features.
@@ -425,22 +427,23 @@ __global__ __launch_bounds__(kThreads) void table_rows_kernel(int V, int D, int 
     const int tx = threadIdx.x & (TX - 1), ty = threadIdx.x >> tx_shift;
     const int64_t total = ALL ? V : B, d = ((int64_t)blockIdx.y * TX + tx) * N;
     if (d >= D) return;
-    for (int64_t v0 = ((int64_t)blockIdx.x * TY + ty) * kRowBlock; v0 < total; v0 += (int64_t)gridDim.x * TY * kRowBlock) {
+    const int64_t apart = (int64_t)gridDim.x * TY;
+    for (int64_t v0 = (int64_t)blockIdx.x * TY + ty; v0 < total; v0 += apart * kRowBlock) {
         // the runs of the rows and what is added to them, all loads ahead of the first sum
         int64_t row[kRowBlock];
         int lo[kRowBlock], hi[kRowBlock];  // lo < 0: no work
         TE e[kRowBlock][N];
 #pragma unroll
         for (int i = 0; i < kRowBlock; ++i) {
-            const int64_t v = min(v0 + i, total - 1);
+            const int64_t v = min(v0 + i * apart, total - 1);
             row[i] = ALL ? v : sorted[v];
         }
 #pragma unroll
         for (int i = 0; i < kRowBlock; ++i) {
-            const bool on = v0 + i < total && row[i] < V;
+            const bool on = v0 + i * apart < total && row[i] < V;
             lo[i] = on ? bounds[row[i]] : -1;
             hi[i] = on ? bounds[row[i] + 1] : -1;
-            if (!ALL && lo[i] != v0 + i) lo[i] = -1;
+            if (!ALL && lo[i] != v0 + i * apart) lo[i] = -1;
         }
 #pragma unroll
         for (int i = 0; i < kRowBlock; ++i) {
@@ -472,16 +475,27 @@ __global__ __launch_bounds__(kThreads) void table_pattern_kernel(int V, int D, i
                                                                  float *__restrict__ gv, int tx_shift) {
     const int TX = 1 << tx_shift, TY = kThreads >> tx_shift;
     const int tx = threadIdx.x & (TX - 1), ty = threadIdx.x >> tx_shift;
-    for (int64_t v = (int64_t)blockIdx.x * TY + ty; v < V; v += (int64_t)gridDim.x * TY) {
-        const int p0 = max(ptr[v], 0), p1 = min(ptr[v + 1], nnz), lo = bounds[v], hi = bounds[v + 1];
-        for (int p = p0 + tx; p < p1; p += TX) {
-            float s[1] = {};
-            if (lo < hi) {
-                const int c = col[p];
-                if ((unsigned)c < (unsigned)D) sum_run<float, 1>(r, lo, hi, c, s);
-            }
-            gv[p] = scale * s[0];
+    const int64_t apart = (int64_t)gridDim.x * TY;
+    for (int64_t v0 = (int64_t)blockIdx.x * TY + ty; v0 < V; v0 += apart * kRowBlock) {
+        int p0[kRowBlock], p1[kRowBlock], lo[kRowBlock], hi[kRowBlock];
+#pragma unroll
+        for (int i = 0; i < kRowBlock; ++i) {
+            const int64_t v = min(v0 + i * apart, (int64_t)V - 1);
+            p0[i] = max(ptr[v], 0);
+            p1[i] = v0 + i * apart < V ? min(ptr[v + 1], nnz) : 0;
+            lo[i] = bounds[v];
+            hi[i] = bounds[v + 1];
         }
+#pragma unroll
+        for (int i = 0; i < kRowBlock; ++i)
+            for (int q = p0[i] + tx; q < p1[i]; q += TX) {
+                float s[1] = {};
+                if (lo[i] < hi[i]) {
+                    const int c = col[q];
+                    if ((unsigned)c < (unsigned)D) sum_run<float, 1>(r, lo[i], hi[i], c, s);
+                }
+                gv[q] = scale * s[0];
+            }
     }
 }
 
@@ -624,7 +638,7 @@ hipError_t launch_embedding_masked_bwd(const embedding_args &a, int nnz, const i
     const hipError_t err = sort_columns<float>(a, plan, w, &r, s);
     if (err != hipSuccess) return err;
     const int shift = std::max(3, pow2_shift(nnz / a.V, 8));
-    table_pattern_kernel<<<grid_of(ceil_div(a.V, kThreads >> shift)), kThreads, 0, s>>>(a.V, a.D, nnz, r, w.bounds, a.scale,
+    table_pattern_kernel<<<grid_of(ceil_div(a.V, (kThreads >> shift) * kRowBlock)), kThreads, 0, s>>>(a.V, a.D, nnz, r, w.bounds, a.scale,
                                                                                        ptr, col, gv, shift);
     return hipGetLastError();
 }
