@@ -1598,7 +1598,8 @@ class EmbeddingPlan:
 def embedding_plan(tokens, n_rows, plan: EmbeddingPlan | None = None, stream=None) -> EmbeddingPlan:
     """The order of the tokens (int32 [B]) of a table of n_rows rows, for embedding_bwd and embedding_masked_bwd.  It depends
     on the tokens alone, so it can be made beside the forward pass and serves every gradient of the batch.  A plan given
-    is filled again (its buffer, where that is large enough)."""
+    is filled again (in its buffer, where that is large enough: a graph that reads a plan keeps the one it was captured
+    with)."""
     torch = _torch()
     _vec(tokens, torch.int32, "tokens")
     index = _device_of(tokens)

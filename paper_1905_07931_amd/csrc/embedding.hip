@@ -268,7 +268,7 @@ constexpr int kGroup = 32;  // rows that are added up ahead where all are of one
 template <typename T>
 struct run_rows {
     const T *rows;          // [B][ld]
-    const float *groups;    // [B / 32][ld], a group's where its rows are of one token
+    const float *groups;    // [B / 32][ld], a group's where its rows are of one token; null: not summed
     const float *blocks;    // [B / 1024][ld], of 32 groups; null: not summed
     int64_t ld;
 };
@@ -303,7 +303,7 @@ __device__ __forceinline__ void sum_run(const run_rows<T> &r, int lo, int hi, in
     const T *rows = r.rows + d;
     int g = (lo + kGroup - 1) / kGroup;
     const int end = hi / kGroup;
-    if (g >= end) {
+    if (g >= end || !r.groups) {
         add_rows<T, N>(rows + lo * r.ld, r.ld, hi - lo, sum);
         return;
     }
@@ -530,7 +530,9 @@ bwd_parts carve_bwd(int V, int D, int B, void *ws) {
     return w;
 }
 
-constexpr int kBlocksFrom = 1 << 14;  // tokens from which on groups are summed once more
+// tokens from which on groups are summed ahead (fewer: 32 times 8 rows at most, less than the launch costs for
+// most batches), and from which on groups of groups are
+constexpr int kGroupsFrom = 256, kBlocksFrom = 1 << 14;
 
 // the columns of dX as rows in the tokens' order, and the sums of their groups
 template <typename T>
@@ -543,8 +545,8 @@ hipError_t sort_columns(const embedding_args &a, const plan_parts &plan, const b
     const int tile_grid = a.B > 0 ? grid_of(tiles) : 0, bound_grid = grid_of(ceil_div(std::max(a.V, a.B) + 1ll, kThreads));
     sort_columns_kernel<T><<<tile_grid + bound_grid, kThreads, 0, s>>>(
         a.V, a.D, a.B, static_cast<const T *>(a.X), a.ldx, plan.rank, plan.sorted, rows, ld, b_tiles, tiles, tile_grid, w.bounds);
-    const int groups = a.B / kGroup, blocks = a.B >= kBlocksFrom ? a.B / (kGroup * kGroup) : 0;
-    *r = {rows, w.groups, blocks > 0 ? w.blocks : nullptr, ld};
+    const int groups = a.B >= kGroupsFrom ? a.B / kGroup : 0, blocks = a.B >= kBlocksFrom ? a.B / (kGroup * kGroup) : 0;
+    *r = {rows, groups > 0 ? w.groups : nullptr, blocks > 0 ? w.blocks : nullptr, ld};
     if (groups > 0)
         group_kernel<T><<<grid_of(groups), kThreads, 0, s>>>(a.V, a.B, 1, rows, plan.sorted, w.groups, ld, groups);
     if (blocks > 0)

@@ -224,7 +224,7 @@ __device__ __forceinline__ int anew(int ty) {
     return ty;
 }
 
-// Forward: y stays in registers and becomes r'.  J rows of V columns a thread (J V <= 72 of 128 registers); r and the gate
+// Forward: y stays in registers and becomes r'.  J rows of V columns a thread (J <= 8); r and the gate
 // come ahead, the first of them before the first mean is known.
 template <typename T, int V, int J>
 __global__ __launch_bounds__(kStripThreads) void forward_strip_kernel(norm_args A, strip_grid g) {
@@ -315,7 +315,7 @@ __device__ __forceinline__ void store_row_sum(const norm_args &A, float *rows, i
     if (tx == 0 && k < A.K) rows[((int64_t)i * blocks + block) * A.K + k] = x;
 }
 
-// Backward, for small matrices: r' and dh stay in registers and become t and y (J V <= 16 of each)
+// Backward: r' and dh stay in registers and become t and y (J <= 4, or 8 of one column)
 template <typename T, int V, int J>
 __global__ __launch_bounds__(kStripThreads) void backward_strip_kernel(norm_args A, strip_grid g, float *__restrict__ rows) {
     __shared__ strip_shared sh[2];
@@ -448,7 +448,7 @@ __global__ __launch_bounds__(kStripThreads) void backward_strip_kernel(norm_args
 // ---------------------------------------------------------------------------
 
 constexpr int kPassThreads = 512;
-constexpr int kPassVector = 4;  // columns of a thread of the two passes (the sums of 8 take 96 registers)
+constexpr int kPassVector = 4;  // columns of a thread of the sums (those of 8 take 96 registers); of the results: 16 bytes
 
 // How a workgroup lies over [K][B]: 2^tx_shift threads of V columns each side by side, the others over the rows;
 // blockIdx.y a range of rows.
@@ -831,11 +831,12 @@ __global__ __launch_bounds__(kPassThreads) void backward_kernel(norm_args A, nor
     });
 }
 
-// a row's sum over the blocks of columns: 32 rows and 8 threads to each of a workgroup, blockIdx.y one of the three sums
-__global__ __launch_bounds__(kThreads) void row_sums_kernel(int K, int blocks, const float *__restrict__ rows,
-                                                            float *pre, float *post, float *gate) {
-    constexpr int width = 32, ways = kThreads / width;
-    __shared__ double lds[kThreads];
+// a row's sum over the blocks of columns: 32 rows and 32 threads to each of a workgroup, blockIdx.y one of the three sums
+constexpr int kRowSumThreads = 1024;
+__global__ __launch_bounds__(kRowSumThreads) void row_sums_kernel(int K, int blocks, const float *__restrict__ rows,
+                                                                  float *pre, float *post, float *gate) {
+    constexpr int width = 32, ways = kRowSumThreads / width;
+    __shared__ double lds[kRowSumThreads];
     float *out = blockIdx.y == 0 ? pre : blockIdx.y == 1 ? post : gate;
     if (out == nullptr) return;
     const int64_t k = (int64_t)blockIdx.x * width + threadIdx.x % width;
@@ -858,14 +859,16 @@ __global__ __launch_bounds__(kThreads) void row_sums_kernel(int K, int blocks, c
 // launches
 // ---------------------------------------------------------------------------
 
+int pass_vector(int B) { return B < kPassVector ? 1 : kPassVector; }
+
 int vector_of(int B, int dtype) {
     const int v = dtype == kTypeF32 ? 4 : 8;
     return B >= v ? v : 1;
 }
 
-norm_grid grid_for(int K, int B) {
+norm_grid grid_for(int K, int B, int V) {
     norm_grid g;
-    const int64_t lanes = ceil_div(B, B < kPassVector ? 1 : kPassVector);
+    const int64_t lanes = ceil_div(B, V);
     g.tx_shift = 0;
     while (g.tx_shift < 6 && (1 << g.tx_shift) < lanes) ++g.tx_shift;
     g.col_blocks = (int)ceil_div(lanes, 1 << g.tx_shift);
@@ -878,8 +881,6 @@ norm_grid grid_for(int K, int B) {
     return g;
 }
 
-constexpr int kStripValues = 72;    // of a thread of the forward strips
-constexpr int kBackwardValues = 16;  // of each of both matrices of the backward ones
 constexpr int kStripFill = 256;      // strips that fill the card
 
 // The widest strips that leave kStripFill of them (a thread's V columns at least) and whose rows are `held` values of a
@@ -892,26 +893,22 @@ int rows_held(int K, int B, int V, int dtype, int held, strip_grid *g) {
         shift = 0;
         while ((1 << shift) < lanes) ++shift;  // (fewer than 8 columns)
     } else {
-        while (shift > 0 && (ceil_div(lanes, 1 << shift) < kStripFill || rows() * V > held || (V == 8 && rows() > 8))) --shift;
+        while (shift > 0 && (ceil_div(lanes, 1 << shift) < kStripFill || rows() * V > held)) --shift;
     }
-    if (rows() * V > held || (V == 8 && rows() > 8)) return 0;
+    if (rows() * V > held) return 0;
     *g = {shift, (int)ceil_div(lanes, 1 << shift), std::max(1, 128 / (V * (dtype == kTypeF32 ? 4 : 2) << shift))};
     return (int)rows();
 }
 
-// f(T, V, J) as compile-time values, J at least the rows; V is 1 or WIDE (0: 16 bytes)
-template <int HELD, int WIDE, typename F>
+// f(T, V, J) as compile-time values, J at least the rows (MOST of them, of a vector's kernels); V is 1 or WIDE (0: 16 bytes)
+template <int MOST, int WIDE, typename F>
 hipError_t with_rows(int V, int dtype, int rows, F f) {
     using std::integral_constant;
     auto by_rows = [&](auto t, auto v) {
-        constexpr int most = HELD / decltype(v)::value;
         if (rows <= 2) return f(t, v, integral_constant<int, 2>{});
         if (rows <= 4) return f(t, v, integral_constant<int, 4>{});
-        if constexpr (most >= 8) {
+        if constexpr (MOST >= 8 || decltype(v)::value == 1) {
             if (rows <= 8) return f(t, v, integral_constant<int, 8>{});
-        }
-        if constexpr (most >= 18) {
-            if (rows <= 18) return f(t, v, integral_constant<int, 18>{});
         }
         return hipErrorInvalidValue;
     };
@@ -924,11 +921,13 @@ hipError_t with_rows(int V, int dtype, int rows, F f) {
     return by_type(_Float16{});
 }
 
-template <typename F>
-hipError_t with_vectors(int B, int dtype, F f) {
+// f(T, V): V is 1, or WIDE (0: 16 bytes)
+template <int WIDE, typename F>
+hipError_t with_vectors(int V, int dtype, F f) {
     using std::integral_constant;
     auto by_type = [&](auto t) {
-        return B < kPassVector ? f(t, integral_constant<int, 1>{}) : f(t, integral_constant<int, kPassVector>{});
+        constexpr int wide = WIDE > 0 ? WIDE : kPer16<decltype(t)>;
+        return V == 1 ? f(t, integral_constant<int, 1>{}) : f(t, integral_constant<int, wide>{});
     };
     if (dtype == kTypeF32) return by_type(float{});
     if (dtype == kTypeBF16) return by_type(__bf16{});
@@ -941,25 +940,38 @@ bool short_enough(const norm_args &a) {
     return a.K * ld < (int64_t)1 << 30;
 }
 
+// Strips of up to 2048 rows leave room for several workgroups a CU (us, strips and two passes, gate and both norms:
+// fp32 1024 x 8192 45 and 64, 2048 x 8192 105 and 112, bf16 2048 x 8192 49 and 63).  Up to 4096 rows one workgroup fills a
+// CU and nothing hides its reductions: that still pays where the launches and the join are a part of the time (fp32
+// 4096 x 1024 39 and 44, bf16 28 and 35; 4096 x 4096 equal), not for large matrices (fp32 4096 x 8192 259 and 217,
+// bf16 124 and 113).  Longer columns would spill.
+constexpr int kStripRows = 2048, kMostStripRows = 4096;
+constexpr int64_t kStripBytes = 32 << 20;  // of a matrix of more than kStripRows rows
 int forward_rows(int K, int B, int dtype, strip_grid *g) {
     const int V = vector_of(B, dtype);
-    return rows_held(K, B, V, dtype, V == 1 ? 18 : kStripValues, g);
+    if (V > 1 && (K > kMostStripRows || (K > kStripRows && (int64_t)K * B * (dtype == kTypeF32 ? 4 : 2) > kStripBytes))) return 0;
+    return rows_held(K, B, V, dtype, V == 1 ? 8 : 8 * V, g);
 }
 
-// Small matrices, where the launches are what two passes cost.  Larger ones read the gate twice and leave three sums
-// a row of every strip, in pieces of 32 bytes of a row at most: no less than two passes over whole lines take.
-constexpr int64_t kSmallBytes = 8 << 20;  // of a matrix
+// Backward strips hold two matrices and leave three sums a row each (37 % of a matrix in pieces of 32 bytes).  us, strips
+// and two passes: bf16 1024 x 8192 49 and 70, 300 x 16384 40 and 59; fp32 94 and 100, 48 and 69; but fp32 2048 x 8192 252
+// and 163, 100 x 100000 (3125 strips, whose sums few rows join) 160 and 122.
+constexpr int kBackwardRows = 1024, kMostBackwardStrips = 1024;
+constexpr int64_t kSmallBytes = 8 << 20, kBackwardBytes = 128 << 20;  // of a matrix: any rows that fit, kBackwardRows of them
 int backward_rows(int K, int B, int dtype, strip_grid *g) {
-    if ((int64_t)K * B * (dtype == kTypeF32 ? 4 : 2) > kSmallBytes) return 0;
-    return rows_held(K, B, B < kPassVector ? 1 : kPassVector, dtype, B < kPassVector ? 8 : kBackwardValues, g);
+    const int64_t bytes = (int64_t)K * B * (dtype == kTypeF32 ? 4 : 2);
+    if (bytes > kSmallBytes && (K > kBackwardRows || bytes > kBackwardBytes)) return 0;
+    const int rows = rows_held(K, B, pass_vector(B), dtype, B < kPassVector ? 8 : 4 * kPassVector, g);
+    return rows > 0 && g->strips <= kMostBackwardStrips ? rows : 0;
 }
 
 }  // namespace
 
 size_t residual_norm_workspace_bytes(int K, int B) {
     if (K <= 0 || B <= 0) return 0;
-    const norm_grid g = grid_for(K, B);
-    size_t most = sizeof(double) * kSums * (size_t)g.splits * B + sizeof(float) * (kFactors * (size_t)B + 3 * (size_t)g.col_blocks * K);
+    size_t most = 0, blocks = 0;
+    for (int dtype : {kTypeF32, kTypeBF16}) blocks = std::max(blocks, (size_t)grid_for(K, B, vector_of(B, dtype)).col_blocks);
+    most = sizeof(double) * kSums * (size_t)grid_for(K, B, pass_vector(B)).splits * B + sizeof(float) * (kFactors * (size_t)B + 3 * blocks * K);
     for (int dtype : {kTypeF32, kTypeBF16}) {
         strip_grid sg;
         if (backward_rows(K, B, dtype, &sg) > 0) most = std::max(most, sizeof(float) * 3 * (size_t)sg.strips * K);
@@ -972,27 +984,31 @@ hipError_t launch_residual_norm_fwd(const norm_args &a, void *ws, hipStream_t s)
     strip_grid sg;
     const int rows = short_enough(a) ? forward_rows(a.K, a.B, a.dtype, &sg) : 0;
     if (rows > 0)
-        return with_rows<kStripValues, 0>(vector_of(a.B, a.dtype), a.dtype, rows, [&](auto t, auto v, auto j) {
+        return with_rows<8, 0>(vector_of(a.B, a.dtype), a.dtype, rows, [&](auto t, auto v, auto j) {
             forward_strip_kernel<decltype(t), decltype(v)::value, decltype(j)::value><<<sg.blocks(), kStripThreads, 0, s>>>(a, sg);
             return hipGetLastError();
         });
-    const norm_grid g = grid_for(a.K, a.B);
-    const dim3 grid(g.col_blocks, g.splits);
+    const norm_grid sums = grid_for(a.K, a.B, pass_vector(a.B)), g = grid_for(a.K, a.B, vector_of(a.B, a.dtype));
     const bool post = a.post_gain != nullptr, pre = a.pre_gain != nullptr;
     double *part = static_cast<double *>(ws);
-    float *fac = reinterpret_cast<float *>(part + kSums * (size_t)g.splits * a.B);
-    return with_vectors(a.B, a.dtype, [&](auto t, auto v) {
-        using T = decltype(t);
-        constexpr int N = decltype(v)::value;
-        if (post || pre) {
+    float *fac = reinterpret_cast<float *>(part + kSums * (size_t)sums.splits * a.B);
+    if (post || pre) {
+        const hipError_t err = with_vectors<kPassVector>(pass_vector(a.B), a.dtype, [&](auto t, auto v) {
+            using T = decltype(t);
+            constexpr int N = decltype(v)::value;
             (a.y == nullptr  ? forward_sums_kernel<T, N, kHasPre>
              : !post         ? forward_sums_kernel<T, N, kHasY | kHasPre>
              : !pre          ? forward_sums_kernel<T, N, kHasY | kHasPost>
-                             : forward_sums_kernel<T, N, kHasY | kHasPost | kHasPre>)<<<grid, kPassThreads, 0, s>>>(a, g, part);
-            forward_join_kernel<<<(int)ceil_div(a.B, kJoinColumns), kThreads, 0, s>>>(a.K, a.B, a.eps, g.splits, post, pre,
-                                                                                    part, fac);
-        }
-        forward_kernel<T, N><<<grid, kPassThreads, 0, s>>>(a, g, fac);
+                             : forward_sums_kernel<T, N, kHasY | kHasPost | kHasPre>)
+                <<<dim3(sums.col_blocks, sums.splits), kPassThreads, 0, s>>>(a, sums, part);
+            forward_join_kernel<<<(int)ceil_div(a.B, kJoinColumns), kThreads, 0, s>>>(a.K, a.B, a.eps, sums.splits, post, pre, part,
+                                                                                    fac);
+            return hipGetLastError();
+        });
+        if (err != hipSuccess) return err;
+    }
+    return with_vectors<0>(vector_of(a.B, a.dtype), a.dtype, [&](auto t, auto v) {
+        forward_kernel<decltype(t), decltype(v)::value><<<dim3(g.col_blocks, g.splits), kPassThreads, 0, s>>>(a, g, fac);
         return hipGetLastError();
     });
 }
@@ -1003,7 +1019,7 @@ hipError_t launch_residual_norm_bwd(const norm_args &a, void *ws, hipStream_t s)
     float *dgate = a.gate_kind == kGateRow ? static_cast<float *>(a.dgate) : nullptr;
     auto join_rows = [&](int blocks, const float *rows) {
         if (a.dpre_gain || a.dpost_gain || dgate)
-            row_sums_kernel<<<dim3((unsigned)ceil_div(a.K, 32), 3), kThreads, 0, s>>>(a.K, blocks, rows, a.dpre_gain, a.dpost_gain,
+            row_sums_kernel<<<dim3((unsigned)ceil_div(a.K, 32), 3), kRowSumThreads, 0, s>>>(a.K, blocks, rows, a.dpre_gain, a.dpost_gain,
                                                                                     dgate);
         return hipGetLastError();
     };
@@ -1012,30 +1028,35 @@ hipError_t launch_residual_norm_bwd(const norm_args &a, void *ws, hipStream_t s)
     const int held = short_enough(a) ? backward_rows(a.K, a.B, a.dtype, &sg) : 0;
     if (held > 0) {
         float *rows = static_cast<float *>(ws);
-        const hipError_t err = with_rows<kBackwardValues, kPassVector>(a.B < kPassVector ? 1 : kPassVector, a.dtype, held, [&](auto t, auto v, auto j) {
+        const hipError_t err = with_rows<4, kPassVector>(pass_vector(a.B), a.dtype, held, [&](auto t, auto v, auto j) {
             backward_strip_kernel<decltype(t), decltype(v)::value, decltype(j)::value>
                 <<<sg.blocks(), kStripThreads, 0, s>>>(a, sg, rows);
             return hipGetLastError();
         });
         return err != hipSuccess ? err : join_rows(sg.strips, rows);
     }
-    const norm_grid g = grid_for(a.K, a.B);
-    const dim3 grid(g.col_blocks, g.splits);
+    const norm_grid sums = grid_for(a.K, a.B, pass_vector(a.B)), g = grid_for(a.K, a.B, vector_of(a.B, a.dtype));
     double *part = static_cast<double *>(ws);
-    float *fac = reinterpret_cast<float *>(part + kSums * (size_t)g.splits * a.B), *rows = fac + kFactors * (size_t)a.B;
-    const hipError_t err = with_vectors(a.B, a.dtype, [&](auto t, auto v) {
-        using T = decltype(t);
-        constexpr int N = decltype(v)::value;
-        if (post || pre) {
+    float *fac = reinterpret_cast<float *>(part + kSums * (size_t)sums.splits * a.B), *rows = fac + kFactors * (size_t)a.B;
+    hipError_t err = hipSuccess;
+    if (post || pre)
+        err = with_vectors<kPassVector>(pass_vector(a.B), a.dtype, [&](auto t, auto v) {
+            using T = decltype(t);
+            constexpr int N = decltype(v)::value;
             (!post  ? backward_sums_kernel<T, N, kHasPre>
              : !pre ? backward_sums_kernel<T, N, kHasPost>
-                    : backward_sums_kernel<T, N, kHasPost | kHasPre>)<<<grid, kPassThreads, 0, s>>>(a, g, part);
-            backward_join_kernel<<<(int)ceil_div(a.B, kJoinColumns), kThreads, 0, s>>>(a.K, a.B, a.eps, g.splits, post, pre,
+                    : backward_sums_kernel<T, N, kHasPost | kHasPre>)
+                <<<dim3(sums.col_blocks, sums.splits), kPassThreads, 0, s>>>(a, sums, part);
+            backward_join_kernel<<<(int)ceil_div(a.B, kJoinColumns), kThreads, 0, s>>>(a.K, a.B, a.eps, sums.splits, post, pre,
                                                                                      part, fac);
-        }
-        backward_kernel<T, N><<<grid, kPassThreads, 0, s>>>(a, g, fac, rows);
-        return hipGetLastError();
-    });
+            return hipGetLastError();
+        });
+    if (err == hipSuccess)
+        err = with_vectors<0>(vector_of(a.B, a.dtype), a.dtype, [&](auto t, auto v) {
+            backward_kernel<decltype(t), decltype(v)::value>
+                <<<dim3(g.col_blocks, g.splits), kPassThreads, 0, s>>>(a, g, fac, rows);
+            return hipGetLastError();
+        });
     return err != hipSuccess ? err : join_rows(g.col_blocks, rows);
 }
 

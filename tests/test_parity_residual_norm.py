@@ -147,7 +147,7 @@ def case(K, B, dtype, gate, post, seed, pad=0, off=0):
 
 
 SHAPES = [(1, 1), (2, 3), (10, 1), (10, 4), (64, 7), (100, 8), (300, 65), (784, 33), (1001, 9), (33, 1030), (4097, 2), (257, 257),
-          (5, 5000), (9216, 16)]
+          (5, 5000), (9216, 16), (4500, 37), (4500, 13), (5003, 261), (4099, 5)]
 FORMS = [("none", False, False), ("none", True, False), ("row", True, False), ("row", False, True), ("row", True, True),
          ("full", True, True), ("full", False, False), ("full", True, False)]
 
@@ -204,7 +204,8 @@ def test_the_norm_alone(K, B, dtype):
             close(x, w, tol, str(x.dtype).split(".")[1], "d" + name)
 
 
-@pytest.mark.parametrize("K,B", [(4096, 300), (1000, 2100), (9216, 70), (300, 9000), (20000, 5), (3, 70000)])
+@pytest.mark.parametrize("K,B", [(4096, 300), (1000, 2100), (9216, 70), (300, 9000), (20000, 5), (3, 70000), (2500, 1003), (1500, 2101),
+                                 (1024, 2500), (1025, 2500), (17000, 1), (40, 66000)])
 def test_larger(K, B):
     """Sums over many rows and columns, in several blocks of each."""
     s = case(K, B, "float32", "full", True, 1)
@@ -309,7 +310,7 @@ def test_gradients_against_differences():
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("K,B", [(1, 9), (100, 3), (300, 70), (1000, 700)])
+@pytest.mark.parametrize("K,B", [(1, 9), (100, 3), (300, 70), (1000, 700), (5000, 37), (4500, 261)])
 def test_in_place(K, B, dtype):
     torch = _torch()
     s = case(K, B, dtype, "full", True, 9, pad=3)
