@@ -136,7 +136,8 @@ def test_lookup_in_a_csr_table(V, D, B, density):
 
 @pytest.mark.parametrize("kind", ["zipf", "one", "each", "none", "padded"])
 @pytest.mark.parametrize("dtype,out", PAIRS)
-@pytest.mark.parametrize("V,D,B", [(1, 1, 1), (3, 2, 5), (300, 10, 33), (10, 65, 64), (129, 63, 65), (1000, 300, 257), (5, 100, 2050)])
+@pytest.mark.parametrize("V,D,B", [(1, 1, 1), (3, 2, 5), (300, 10, 33), (10, 65, 64), (129, 63, 65), (1000, 300, 257), (5, 100, 2050),
+                                   (70, 663, 130), (33, 1290, 70)])
 def test_gradient(V, D, B, dtype, out, kind):
     torch = _torch()
     rng = np.random.default_rng(V + D + B)
