@@ -333,7 +333,8 @@ __device__ __forceinline__ void fill_bounds(int V, int B, const int *__restrict_
     const int lane = lane_id();
     for (int64_t i0 = (int64_t)block * kThreads + (threadIdx.x & ~63); i0 <= B; i0 += stride) {
         const int64_t i = i0 + lane;
-        const int from = i == 0 ? 0 : i <= B ? sorted[i - 1] + 1 : V + 1, to = i < B ? sorted[i] : V;
+        // (key_of: a plan of a larger table holds more)
+        const int from = i == 0 ? 0 : i <= B ? key_of(sorted[i - 1], V) + 1 : V + 1, to = i < B ? key_of(sorted[i], V) : V;
         for (uint64_t some = wave_ballot(i <= B && from <= to); some != 0; some &= some - 1) {
             const int j = __builtin_ctzll(some);
             const int last = lane_bcast(to, j);

@@ -234,6 +234,25 @@ def test_gradient_against_differences():
             assert dE[v, d] == (f[0] - f[1]) / 2
 
 
+@pytest.mark.parametrize("V,B", [(50, 40), (50, 3000), (7, 9000), (2000, 30)])
+def test_plan_of_a_larger_table(V, B):
+    """The C call with an order that was made for twice the rows: tokens past the table take no part (small whole numbers:
+    equal bit for bit), and nothing is written past it."""
+    torch, rng = _torch(), np.random.default_rng(7 + V + B)
+    t = tokens_of(2 * V, B, rng, "padded")
+    X = rng.integers(-8, 9, (20, B)).astype(np.float64)
+    dX, _ = matrix(X, "float32")
+    plan = L1.embedding_plan(ints(t), 2 * V)
+    need = L1.workspace_bytes(L1.OP_EMBEDDING_BWD, V, 20, 0, B)
+    ws = torch.full((need + 4096,), 0x5a, dtype=torch.uint8, device=cuda())
+    dE, buf = matrix(np.zeros((V, 20)), "float32", pad=4)
+    assert L1.lib().l1csr_embedding_bwd(V, 20, B, 0, dX.data_ptr(), B, plan.buf.data_ptr(), plan.buf.numel(), 2.0, 0, None, 0,
+                                        dE.data_ptr(), 24, ws.data_ptr(), need, None) == 0
+    torch.cuda.synchronize()
+    assert np.array_equal(h64(dE), gradient(X, t, V, 2.0)[0])
+    assert bool((ws[need:] == 0x5a).all()) and bool(torch.isnan(buf.view(V, 24)[:, 20:]).all())
+
+
 def test_special_values_stay_in_their_places():
     torch = _torch()
     V, D, B = 20, 9, 50
