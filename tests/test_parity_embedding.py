@@ -165,7 +165,7 @@ def test_gradient(V, D, B, dtype, out, kind):
 
 
 @pytest.mark.parametrize("kind", ["zipf", "one", "each", "any", "padded"])
-@pytest.mark.parametrize("B", [1, 31, 32, 33, 63, 64, 1023, 1024, 1025, 4096, 8191, 8192, 8193, 16384, 16385, 24577, 33000])
+@pytest.mark.parametrize("B", [1, 2, 3, 5, 15, 17, 31, 32, 33, 63, 64, 255, 256, 257, 1023, 1024, 1025, 2817, 4096, 8175, 8191, 8192, 8193, 16384, 16385, 24577, 33000])
 def test_every_token_is_counted_once(B, kind):
     """Whole numbers: sums are exact, over runs of equal tokens that begin and end anywhere in the groups, and over the
     borders of the ranked runs."""
