@@ -27,7 +27,6 @@ namespace l1csr {
 
 namespace {
 
-constexpr int kThreads = 256;
 constexpr int kSums = 6;        // most sums of a column
 constexpr int kFactors = 4;     // most factors of a column
 
@@ -502,7 +501,7 @@ __device__ __forceinline__ void for_rows(int k, int k1, int TY, F f) {
 }
 
 // Joins the sums of a workgroup's threads over the rows and stores them: part[q][split][B].  Two sums at a time lie in LDS,
-// and every thread joins a column of them.
+// and the threads share the columns of them.
 template <int V>
 constexpr int kSumsValues = 2 * V * kPassThreads;
 template <typename T, int V, int NS>
@@ -525,40 +524,54 @@ __device__ __forceinline__ void store_sums(const double (&sum)[NS][V], const nor
                 lds[(TY + ty) * width + at] = sum[q + 1][v];
             }
         __syncthreads();
-        for (int j = threadIdx.x; j < 2 * width; j += kPassThreads) {
-            const int i = j >= width ? 1 : 0, at = j - i * width;
-            const int64_t col = first + (at & (TX - 1)) * V + (at >> g.tx_shift);
-            if (col >= B) continue;
-            double t = 0;
-            for (int y = 0; y < TY; ++y) t += lds[(i * TY + y) * width + at];
-            part[((int64_t)(q + i) * g.splits + blockIdx.y) * B + col] = t;
+        // 2 * width sums of TY values, each by `ways` threads (9216 x 1 fp32: 6.8 us, by one thread each 17.2)
+        const int sums = 2 * width, ways = min(16, kPassThreads / sums), i = (threadIdx.x & (sums - 1)) / width;
+        const int at = threadIdx.x & (width - 1);
+        double t = 0;
+        if ((int)threadIdx.x < sums * ways)
+            for (int y = threadIdx.x / sums; y < TY; y += ways) t += lds[(i * TY + y) * width + at];
+        if (ways > 1) {
+            __syncthreads();
+            lds[threadIdx.x] = t;
+            __syncthreads();
+            if ((int)threadIdx.x < sums)
+                for (int w = 1; w < ways; ++w) t += lds[w * sums + threadIdx.x];
         }
+        const int64_t col = first + (at & (TX - 1)) * V + (at >> g.tx_shift);
+        if ((int)threadIdx.x < sums && col < B) part[((int64_t)(q + i) * g.splits + blockIdx.y) * B + col] = t;
     }
 }
 
-constexpr int kJoinColumns = 32;  // of a workgroup of the join; the other threads share the ranges of rows
+// 256 columns in 288 ranges: 5.6 us (four sums) and 7.7 (six); 14.4 and 20.7 with 256 threads on 32 columns
+constexpr int kJoinThreads = 1024;
+constexpr int kJoinColumns = 16;  // of a workgroup of the join; the other threads share the ranges of rows
 
 // Joins the sums over the ranges of rows; true in the threads that hold a column's
 template <int NS>
 __device__ __forceinline__ bool join_sums(const double *__restrict__ part, int splits, int B, int col, double *lds,
                                           double (&sum)[NS]) {
-    constexpr int ways = kThreads / kJoinColumns;
-    const int way = threadIdx.x / kJoinColumns;
+    constexpr int ways = kJoinThreads / kJoinColumns;
+    static_assert(NS <= ways, "a thread's share of the second step is one sum");
+    const int way = threadIdx.x / kJoinColumns, column = threadIdx.x % kJoinColumns;
 #pragma unroll
     for (int q = 0; q < NS; ++q) {
         double t = 0;
         if (col < B)
-#pragma unroll 8
+#pragma unroll 4
             for (int i = way; i < splits; i += ways) t += part[((int64_t)q * splits + i) * B + col];
-        lds[q * kThreads + threadIdx.x] = t;
+        lds[q * kJoinThreads + threadIdx.x] = t;
+    }
+    __syncthreads();
+    if (way < NS) {  // a sum each
+        double t = 0, *p = lds + way * kJoinThreads + column;
+#pragma unroll 8
+        for (int i = 0; i < ways; ++i) t += p[i * kJoinColumns];
+        p[0] = t;
     }
     __syncthreads();
     if (way != 0 || col >= B) return false;
 #pragma unroll
-    for (int q = 0; q < NS; ++q) {
-        sum[q] = 0;
-        for (int i = 0; i < ways; ++i) sum[q] += lds[q * kThreads + i * kJoinColumns + threadIdx.x];
-    }
+    for (int q = 0; q < NS; ++q) sum[q] = lds[q * kJoinThreads + column];
     return true;
 }
 
@@ -619,9 +632,9 @@ __global__ __launch_bounds__(kPassThreads) void forward_sums_kernel(norm_args A,
 }
 
 // a column's factors: q, s
-__global__ __launch_bounds__(kThreads) void forward_join_kernel(int K, int B, float eps, int splits, bool post, bool pre,
+__global__ __launch_bounds__(kJoinThreads) void forward_join_kernel(int K, int B, float eps, int splits, bool post, bool pre,
                                                                 const double *__restrict__ part, float *__restrict__ fac) {
-    __shared__ double lds[4 * kThreads];
+    __shared__ double lds[4 * kJoinThreads];
     const int col = blockIdx.x * kJoinColumns + threadIdx.x % kJoinColumns;
     double sum[4];
     if (!join_sums<4>(part, splits, B, col, lds, sum)) return;
@@ -740,9 +753,9 @@ __global__ __launch_bounds__(kPassThreads) void backward_sums_kernel(norm_args A
 }
 
 // a column's factors: s, f = s^2 c, q, g = q^2 e
-__global__ __launch_bounds__(kThreads) void backward_join_kernel(int K, int B, float eps, int splits, bool post, bool pre,
+__global__ __launch_bounds__(kJoinThreads) void backward_join_kernel(int K, int B, float eps, int splits, bool post, bool pre,
                                                                  const double *__restrict__ part, float *__restrict__ fac) {
-    __shared__ double lds[kSums * kThreads];
+    __shared__ double lds[kSums * kJoinThreads];
     const int col = blockIdx.x * kJoinColumns + threadIdx.x % kJoinColumns;
     double sum[kSums];
     if (!join_sums<kSums>(part, splits, B, col, lds, sum)) return;
@@ -1009,7 +1022,7 @@ hipError_t launch_residual_norm_fwd(const norm_args &a, void *ws, hipStream_t s)
              : !pre          ? forward_sums_kernel<T, N, kHasY | kHasPost>
                              : forward_sums_kernel<T, N, kHasY | kHasPost | kHasPre>)
                 <<<dim3(sums.col_blocks, sums.splits), kPassThreads, 0, s>>>(a, sums, part);
-            forward_join_kernel<<<(int)ceil_div(a.B, kJoinColumns), kThreads, 0, s>>>(a.K, a.B, a.eps, sums.splits, post, pre, part,
+            forward_join_kernel<<<(int)ceil_div(a.B, kJoinColumns), kJoinThreads, 0, s>>>(a.K, a.B, a.eps, sums.splits, post, pre, part,
                                                                                     fac);
             return hipGetLastError();
         });
@@ -1055,7 +1068,7 @@ hipError_t launch_residual_norm_bwd(const norm_args &a, void *ws, hipStream_t s)
              : !pre ? backward_sums_kernel<T, N, kHasPost>
                     : backward_sums_kernel<T, N, kHasPost | kHasPre>)
                 <<<dim3(sums.col_blocks, sums.splits), kPassThreads, 0, s>>>(a, sums, part);
-            backward_join_kernel<<<(int)ceil_div(a.B, kJoinColumns), kThreads, 0, s>>>(a.K, a.B, a.eps, sums.splits, post, pre,
+            backward_join_kernel<<<(int)ceil_div(a.B, kJoinColumns), kJoinThreads, 0, s>>>(a.K, a.B, a.eps, sums.splits, post, pre,
                                                                                      part, fac);
             return hipGetLastError();
         });
