@@ -962,26 +962,33 @@ bool short_enough(const norm_args &a) {
 }
 
 // Strips of up to 2048 rows leave room for several workgroups a CU (us, strips and two passes, gate and both norms:
-// fp32 1024 x 8192 45 and 64, 2048 x 8192 105 and 112, bf16 2048 x 8192 49 and 63).  Up to 4096 rows one workgroup fills a
-// CU and nothing hides its reductions: that still pays where the launches and the join are a part of the time (fp32
-// 4096 x 1024 39 and 44, bf16 28 and 35; 4096 x 4096 equal), not for large matrices (fp32 4096 x 8192 259 and 217,
-// bf16 124 and 113).  Longer columns would spill.
-constexpr int kStripRows = 2048, kMostStripRows = 4096;
+// fp32 1024 x 8192 45 and 64, 2048 x 8192 105 and 112, 2000 x 64 13 and 17, bf16 2048 x 8192 49 and 63).  Up to 4096 rows one
+// workgroup fills a CU and nothing hides its reductions: that still pays where the launches and the join are most of the
+// time (fp32 2800 x 64 17 and 17, 2800 x 1024 31 and 35, bf16 4000 x 256 20 and 22, 4000 x 1024 28 and 29), but not for
+// large matrices (fp32 4096 x 8192 259 and 217, bf16 124 and 113), nor for the longest fp32 columns, which are held four a
+// thread at least (4000 x 64 23.6 and 17.4, 4000 x 512 33 and 27; rows of under 64 bytes are soon read: 4000 x 8 11 and
+// 17).  Longer columns would spill.
+constexpr int kStripRows = 2048, kMostStripRows = 4096, kMostFp32Rows = 2816;
 constexpr int64_t kStripBytes = 32 << 20;  // of a matrix of more than kStripRows rows
+constexpr int kShortRow = 64;              // bytes
 int forward_rows(int K, int B, int dtype, strip_grid *g) {
-    const int V = vector_of(B, dtype);
-    if (V > 1 && (K > kMostStripRows || (K > kStripRows && (int64_t)K * B * (dtype == kTypeF32 ? 4 : 2) > kStripBytes))) return 0;
+    const int V = vector_of(B, dtype), size = dtype == kTypeF32 ? 4 : 2;
+    if (V > 1 && (K > kMostStripRows || (K > kStripRows && (int64_t)K * B * size > kStripBytes))) return 0;
+    if (V > 1 && dtype == kTypeF32 && K > kMostFp32Rows && B * (int64_t)size >= kShortRow) return 0;
     return rows_held(K, B, V, dtype, V == 1 ? 8 : 8 * V, g);
 }
 
 // Backward strips hold two matrices and leave three sums a row each (37 % of a matrix in pieces of 32 bytes).  us, strips
 // and two passes: bf16 1024 x 8192 49 and 70, 300 x 16384 40 and 59; fp32 94 and 100, 48 and 69; but fp32 2048 x 8192 252
-// and 163, 100 x 100000 (3125 strips, whose sums few rows join) 160 and 122.
+// and 163, 100 x 100000 (3125 strips, whose sums few rows join) 160 and 122.  Of more than 2048 rows only those of
+// under 64 bytes: fp32 4000 x 8 21 and 24, 2000 x 64 24.2 and 24.5, 2800 x 64 37 and 25, 4000 x 64 50 and 25, 4000 x 512 62
+// and 40, bf16 2000 x 64 22 and 27, 4000 x 64 40 and 28, 4000 x 512 48 and 43, 2800 x 256 36 and 37.
 constexpr int kBackwardRows = 1024, kMostBackwardStrips = 1024;
 constexpr int64_t kSmallBytes = 8 << 20, kBackwardBytes = 128 << 20;  // of a matrix: any rows that fit, kBackwardRows of them
 int backward_rows(int K, int B, int dtype, strip_grid *g) {
-    const int64_t bytes = (int64_t)K * B * (dtype == kTypeF32 ? 4 : 2);
+    const int64_t row = B * (dtype == kTypeF32 ? 4ll : 2ll), bytes = K * row;
     if (bytes > kSmallBytes && (K > kBackwardRows || bytes > kBackwardBytes)) return 0;
+    if (K > kStripRows && row >= kShortRow) return 0;
     const int rows = rows_held(K, B, pass_vector(B), dtype, B < kPassVector ? 8 : 4 * kPassVector, g);
     return rows > 0 && g->strips <= kMostBackwardStrips ? rows : 0;
 }
