@@ -147,7 +147,7 @@ def case(K, B, dtype, gate, post, seed, pad=0, off=0):
 
 
 SHAPES = [(1, 1), (2, 3), (10, 1), (10, 4), (64, 7), (100, 8), (300, 65), (784, 33), (1001, 9), (33, 1030), (4097, 2), (257, 257),
-          (5, 5000), (9216, 16), (4500, 37), (4500, 13), (5003, 261), (4099, 5)]
+          (5, 5000), (9216, 16), (4500, 37), (4500, 13), (5003, 261), (4099, 5), (9000, 3), (2817, 16), (2816, 17), (2049, 15), (2049, 33)]
 FORMS = [("none", False, False), ("none", True, False), ("row", True, False), ("row", False, True), ("row", True, True),
          ("full", True, True), ("full", False, False), ("full", True, False)]
 
