@@ -14,7 +14,7 @@ import functools
 import math
 import os
 from array import array
-from dataclasses import dataclass
+from dataclasses import dataclass, field
 
 __all__ = [
     "CSR", "CSC", "L1CSRError", "lib", "status_str", "workspace_bytes",
@@ -1593,13 +1593,14 @@ class EmbeddingPlan:
     n_rows: int
     B: int
     buf: object  # device buffer, None for B = 0
+    outgrown: list = field(default_factory=list)  # earlier buffers, which graphs may read
 
 
 def embedding_plan(tokens, n_rows, plan: EmbeddingPlan | None = None, stream=None) -> EmbeddingPlan:
     """The order of the tokens (int32 [B]) of a table of n_rows rows, for embedding_bwd and embedding_masked_bwd.  It depends
     on the tokens alone, so it can be made beside the forward pass and serves every gradient of the batch.  A plan given
-    is filled again (in its buffer, where that is large enough: a graph that reads a plan keeps the one it was captured
-    with)."""
+    is filled again, in its buffer where that is large enough; one that it outgrows lives as long as the plan, so a graph
+    keeps the one it was captured with."""
     torch = _torch()
     _vec(tokens, torch.int32, "tokens")
     index = _device_of(tokens)
@@ -1609,6 +1610,8 @@ def embedding_plan(tokens, n_rows, plan: EmbeddingPlan | None = None, stream=Non
         plan = EmbeddingPlan(n_rows, B, None)
     buf = plan.buf
     if need > 0 and (buf is None or buf.numel() < need or buf.get_device() != index):
+        if buf is not None:
+            plan.outgrown.append(buf)
         buf = _empty_bytes(need, tokens.device, stream)
     _check(lib().l1csr_embedding_plan(n_rows, B, tokens.data_ptr(), _p(buf), 0 if buf is None else buf.numel(),
                                       _stream(stream)), "l1csr_embedding_plan")

@@ -416,6 +416,32 @@ def test_graph_replays():
             assert torch.equal(dE, L1.embedding_bwd(dX, t, V, scale=2.0))
 
 
+def test_graph_keeps_its_plan_when_the_plan_grows():
+    """A graph captured with a plan, which is filled again for a larger batch: replays read the order they were captured with."""
+    torch, rng = _torch(), np.random.default_rng(11)
+    V, D, B = 30, 8, 500
+    t = tokens_of(V, B, rng, "zipf")
+    X = rng.integers(-8, 9, (D, B)).astype(np.float64)
+    dX, _ = matrix(X, "float32")
+    plan, dE = L1.embedding_plan(ints(t), V), torch.empty(V, D, device=cuda())
+    want = gradient(X, t, V, 1.0)[0]
+    L1.embedding_bwd(dX, None, V, dE=dE, plan=plan)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        L1.embedding_bwd(dX, None, V, dE=dE, plan=plan)
+    larger = tokens_of(V, 9000, rng, "any")
+    L1.embedding_plan(ints(larger), V, plan=plan)
+    junk = [torch.full((3 * B,), 0x7fffffff, dtype=torch.int32, device=cuda()) for _ in range(64)]
+    for _ in range(3):
+        dE.fill_(float("nan"))
+        graph.replay()
+        assert np.array_equal(h64(dE), want)
+    big, _ = matrix(rng.integers(-8, 9, (D, 9000)).astype(np.float64), "float32")
+    assert np.array_equal(h64(L1.embedding_bwd(big, None, V, plan=plan)), gradient(h64(big), larger, V, 1.0)[0])
+    del junk
+
+
 def test_first_call_of_a_process():
     """The table of element types is filled by the call that needs it, whichever comes first."""
     torch = _torch()
