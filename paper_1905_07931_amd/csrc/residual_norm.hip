@@ -38,7 +38,7 @@ __device__ __forceinline__ void logistic(float g, float, float &a, float &b) {
     const float x = -fabsf(g), y = x * log2e;
     const float rest = fmaf(x, log2e_rest, fmaf(x, log2e, -y)) * ln2;
     float e = __builtin_amdgcn_exp2f(y);
-    if (x > -INFINITY) e = fmaf(e, rest, e);
+    if (y > -INFINITY) e = fmaf(e, rest, e);  // (the product leaves fp32 ahead of g: its rest is infinite then)
     const float d = 1.f + e, r0 = __builtin_amdgcn_rcpf(d), r = fmaf(fmaf(-d, r0, 1.f), r0, r0), small = e * r;
     a = g >= 0.f ? r : small;  // (a NaN is in both)
     b = g >= 0.f ? small : r;

@@ -413,3 +413,31 @@ def test_streams_graphs_and_reproducibility():
             eager = step(stream=streams[1])
             torch.cuda.synchronize()
             assert all(torch.equal(a, b) for a, b in zip(eager, k))
+
+
+# shapes that take the strips and shapes that take the two passes, of vectors and of single columns
+BOTH_WAYS = [(50, 9), (300, 2), (5003, 9), (9000, 3)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("post", [False, True])
+@pytest.mark.parametrize("K,B", BOTH_WAYS)
+def test_logistic_gates_at_the_ends_of_their_type(K, B, post, dtype):
+    """A gate of the type's lowest value is closed, one of its highest open, and neither touches anything else."""
+    torch = _torch()
+    for kind in ("full", "row"):
+        s = case(K, B, dtype, kind, post, 7)
+        top = torch.finfo(s["gate"].dtype).max
+        at = (slice(None), (0, 1)) if kind == "full" else ((3, K - 1),)  # open, closed: tokens, or features
+        s["gate"][at] = torch.tensor([top, -top], dtype=s["gate"].dtype, device=cuda())
+        kw = dict(gate=s["gate"], post_gain=s["post"], pre_gain=s["pre"], sigmoid=True)
+        rn, hh = L1.residual_norm_fwd(s["r"], s["y"], **kw)
+        d = L1.residual_norm_bwd(rn, s["dr"], s["dh"], s["y"], **kw)
+        for x in (rn, hh, d.r, d.y, d.gate, d.pre_gain, *([d.post_gain] if post else [])):
+            assert bool(torch.isfinite(x).all()), kind
+        assert not bool(d.gate[at].any())
+        opened, closed = ((slice(None), 0), (slice(None), 1)) if kind == "full" else (3, K - 1)
+        assert torch.equal(rn[closed], s["r"][closed])
+        if not post:  # (with a post gain y's part in its own mean has a gradient too)
+            assert torch.equal(rn[opened], (s["r"].float() + s["y"].float()).to(s["r"].dtype)[opened])
+            assert torch.equal(d.y[opened], d.r[opened]) and not bool(d.y[closed].any())
