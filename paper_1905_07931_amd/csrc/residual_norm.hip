@@ -228,7 +228,6 @@ template <typename T, int V, int J>
 __global__ __launch_bounds__(kStripThreads) void forward_strip_kernel(norm_args A, strip_grid g) {
     __shared__ strip_shared sh[1];
     constexpr int P = J * V > 64 ? 1 : 2;  // rows of r and the gate that are under way
-    using partial = std::conditional_t<sizeof(T) == 4, double, float>;  // a thread's sum over its rows, 9 at most in 16 bits
     const strip_place at(g);
     if (at.strip >= g.strips) return;
     const int64_t c = (((int64_t)at.strip << g.tx_shift) + at.tx) * V;
@@ -253,16 +252,13 @@ __global__ __launch_bounds__(kStripThreads) void forward_strip_kernel(norm_args 
     float x[J][V], q[V];
     const float *factor = sh[0].factor[0] + at.tx * V;
     auto mean_square = [&](auto value) {
-        partial part[V] = {};
+        double sum[1][V] = {};  // (squares of bf16 values and of r' leave fp32)
 #pragma unroll
         for (int j = 0; j < J; ++j) {
             if (j >= rows) continue;
 #pragma unroll
-            for (int v = 0; v < V; ++v) part[v] += (partial)value(j, v) * value(j, v);
+            for (int v = 0; v < V; ++v) sum[0][v] += (double)value(j, v) * value(j, v);
         }
-        double sum[1][V];
-#pragma unroll
-        for (int v = 0; v < V; ++v) sum[0][v] = part[v];
         strip_sums<V, 1>(sum, g.tx_shift, sh, [&](int i, const double(&t)[1]) {
             sh[0].factor[0][i] = (float)(1 / sqrt(t[0] / A.K + A.eps));
         });
