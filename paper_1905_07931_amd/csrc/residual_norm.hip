@@ -624,6 +624,27 @@ __global__ __launch_bounds__(kPassThreads) void forward_sums_kernel(norm_args A,
             }
         }
     });
+    if constexpr (post && pre) {
+        // Squares of finite values are finite: a column with an infinite r or x comes here.  r' is infinite there, or NaN, and so
+        // is its square, whatever r x gave (0 times infinity, or one infinity less another).  Looked at once behind the sums: in
+        // the loop it takes 12 to 15 % of the call in 16 bits (4096 x 8192 104 -> 119 us).
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            if (sum[1][v] + sum[3][v] < INFINITY) continue;
+            bool nan = false;
+            for (int k = k0; k < k1; k += TY) {
+                T r[V], y[V], gate[V];
+                c.load(A.r, A.ldr, k, r);
+                c.load(A.y, A.ldy, k, y);
+                if (full) c.load(A.gate, A.ldg, k, gate);
+                const gate_values<T, V> a(A, k, gate);
+                const float w = A.alpha * A.post_gain[k];
+                const double z = widen(r[v]) + (double)(a.a[v] * w) * widen(y[v]);
+                nan = nan || z != z;
+            }
+            sum[2][v] = nan ? NAN : INFINITY;
+        }
+    }
     store_sums<T, V, NS>(sum, g, c, A.B, lds, part);
 }
 
