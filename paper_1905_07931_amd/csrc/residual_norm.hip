@@ -424,7 +424,7 @@ __global__ __launch_bounds__(kStripThreads) void backward_strip_kernel(norm_args
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const float at_ = A.alpha * t[j][v], yq = y[j][v] * q[v];
-            dy[v] = a.a[v] * at_ * w * q[v] - e[v] * yq;
+            dy[v] = a.a[v] * at_ * w * q[v] - (post ? e[v] * yq : 0.f);  // (y may be infinite where it has no norm)
             dg[v] = at_ * yq * w * a.da[v];
             sums[0] += v >= own ? a.a[v] * at_ * yq : 0.f;
             sums[1] += v >= own ? dg[v] : 0.f;
@@ -856,7 +856,7 @@ __global__ __launch_bounds__(kPassThreads) void backward_kernel(norm_args A, nor
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 const float at = A.alpha * t[v], yq = widen(y[u][v]) * q[v];
-                dy[v] = a.a[v] * at * w * q[v] - e[v] * yq;
+                dy[v] = a.a[v] * at * w * q[v] - (post ? e[v] * yq : 0.f);  // (y may be infinite where it has no norm)
                 dg[v] = at * yq * w * a.da[v];
                 sums[0] += v >= c.own ? a.a[v] * at * yq : 0.f;
                 sums[1] += v >= c.own ? dg[v] : 0.f;
