@@ -1599,8 +1599,9 @@ class EmbeddingPlan:
 def embedding_plan(tokens, n_rows, plan: EmbeddingPlan | None = None, stream=None) -> EmbeddingPlan:
     """The order of the tokens (int32 [B]) of a table of n_rows rows, for embedding_bwd and embedding_masked_bwd.  It depends
     on the tokens alone, so it can be made beside the forward pass and serves every gradient of the batch.  A plan given
-    is filled again, in its buffer where that is large enough; one that it outgrows lives as long as the plan, so a graph
-    keeps the one it was captured with."""
+    is filled again, in its buffer where that is large enough (graphs captured with that buffer then read the new order:
+    one that is to keep its own needs a plan of its own), else in one of at least twice the size; one that it outgrows lives
+    as long as the plan, so a graph keeps the one it was captured with."""
     torch = _torch()
     _vec(tokens, torch.int32, "tokens")
     index = _device_of(tokens)
@@ -1608,13 +1609,15 @@ def embedding_plan(tokens, n_rows, plan: EmbeddingPlan | None = None, stream=Non
     need = workspace_bytes(OP_EMBEDDING_PLAN, n_rows, 0, 0, B)
     if plan is None:
         plan = EmbeddingPlan(n_rows, B, None)
-    buf = plan.buf
+    buf = old = plan.buf
     if need > 0 and (buf is None or buf.numel() < need or buf.get_device() != index):
-        if buf is not None:
-            plan.outgrown.append(buf)
-        buf = _empty_bytes(need, tokens.device, stream)
+        # (twice the size that was too small: what a plan outgrew on a device is together no larger than what it has)
+        grown = 0 if old is None or old.get_device() != index else 2 * old.numel()
+        buf = _empty_bytes(max(need, grown), tokens.device, stream)
     _check(lib().l1csr_embedding_plan(n_rows, B, tokens.data_ptr(), _p(buf), 0 if buf is None else buf.numel(),
                                       _stream(stream)), "l1csr_embedding_plan")
+    if old is not None and buf is not old:
+        plan.outgrown.append(old)
     plan.n_rows, plan.B, plan.buf = n_rows, B, buf
     return plan
 

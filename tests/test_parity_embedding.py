@@ -450,3 +450,28 @@ def test_first_call_of_a_process():
     L1._DTYPES.clear()
     X = L1.embedding_fwd(W, ints([1, 2]), X=torch.empty(4, 2, device=cuda()))
     assert np.array_equal(h64(X), dense[[1, 2]].T)
+
+
+def test_a_plan_that_grows_step_by_step_keeps_little():
+    """The buffers that a plan outgrew are together no larger than the one it has."""
+    torch, V = _torch(), 50
+    t = torch.arange(3000, dtype=torch.int32, device=cuda()) % V
+    plan = L1.embedding_plan(t[:1], V)
+    for B in range(2, 3001):
+        L1.embedding_plan(t[:B], V, plan=plan)
+    assert sum(b.numel() for b in plan.outgrown) <= plan.buf.numel() <= 2 * L1.workspace_bytes(L1.OP_EMBEDDING_PLAN, V, 0, 0, 3000)
+    dX = torch.ones(4, 3000, device=cuda())
+    assert bool((L1.embedding_bwd(dX, None, V, plan=plan) == 60).all())
+
+
+def test_a_plan_whose_refill_fails_stays_as_it_was():
+    torch, V = _torch(), 50
+    t = torch.arange(3000, dtype=torch.int32, device=cuda()) % V
+    plan = L1.embedding_plan(t[:100], V)
+    buf = plan.buf
+    for _ in range(2):
+        with pytest.raises(L1.L1CSRError):
+            L1.embedding_plan(t, (1 << 30) + 1, plan=plan)  # more rows than the order's keys hold
+    assert plan.buf is buf and plan.outgrown == [] and (plan.n_rows, plan.B) == (V, 100)
+    dX = torch.ones(4, 100, device=cuda())
+    assert bool((L1.embedding_bwd(dX, None, V, plan=plan) == 2).all())
