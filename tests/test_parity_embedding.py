@@ -475,3 +475,13 @@ def test_a_plan_whose_refill_fails_stays_as_it_was():
     assert plan.buf is buf and plan.outgrown == [] and (plan.n_rows, plan.B) == (V, 100)
     dX = torch.ones(4, 100, device=cuda())
     assert bool((L1.embedding_bwd(dX, None, V, plan=plan) == 2).all())
+
+
+@pytest.mark.parametrize("V,D,density", [(1, 700, 0.5), (300, 4097, 0.05), (40, 5000, 1.0), (2000, 1, 0.5), (50, 257, 0.0)])
+def test_lookup_of_one_token_in_a_csr_table(V, D, density):
+    rng = np.random.default_rng(V + D)
+    W, dense, _ = csr_table(V, D, density, rng)
+    for t in (0, V - 1, V // 2, V, -1):
+        X = L1.embedding_fwd(W, ints([t]), scale=2.0)
+        want = 2.0 * dense[t].astype(np.float64) if 0 <= t < V else np.zeros(D)
+        assert X.shape == (D, 1) and np.array_equal(h64(X)[:, 0], want)

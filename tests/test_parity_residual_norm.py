@@ -686,3 +686,102 @@ def test_a_block_without_a_norm_has_a_gradient_without_its_values(K, B, kind, dt
         want = L1.residual_norm_bwd(s["r"], s["dr"], y=s["y"], **more, **kw)
         got = L1.residual_norm_bwd(s["r"], s["dr"], y=y, **more, **kw)
         assert torch.equal(got.y, want.y) and torch.equal(got.r, want.r)
+
+
+# The tests above with small shapes run in strips; these are the same in two passes (the only way with a workspace forward).
+
+@pytest.mark.parametrize("K,B", [(5003, 30), (4500, 261), (9000, 3)])
+def test_passes_of_a_block_that_takes_back_the_residual(K, B):
+    """r' is a thousandth of r and of x: the sum over r'^2 from its three parts keeps its digits.  The gain is 1, so x = y there
+    without a rounding; a part has at most K + 8 roundings of 2^-53 (its products, sums and the joining) and all are at most R^2 |r'|^2, R^2 =
+    (|r| + |x|)^2 / |r'|^2 (4e6): s is within (K + 8) 2^-54 R^2 of its own (q's own error moves r, x and r' together: R, not
+    R^2, times as little), and h's entries have those of r' besides."""
+    rng = np.random.default_rng(0)
+    y = rng.standard_normal((K, B))
+    q = 1 / np.sqrt((y * y).mean(0))
+    s = dict(y=view(y, "float32"), post=vec(np.ones(K)), pre=vec(np.ones(K)))
+    s["r"] = view(-y * q + 1e-3 * rng.standard_normal((K, B)), "float32")
+    eps = float(np.float32(1e-12))
+    rn, hh = L1.residual_norm_fwd(s["r"], s["y"], post_gain=s["post"], pre_gain=s["pre"], eps=1e-12)
+    r64, y64 = h64(s["r"]), h64(s["y"])
+    want_r, want_h, tr, _ = forward(r64, y64, None, h64(s["post"]), h64(s["pre"]), 1.0, eps, False)
+    close(rn, want_r, tr, "float32", "r'")
+    x, size = np.abs(want_r - r64), np.sqrt((want_r ** 2).sum(0))
+    R2 = (np.sqrt((r64 ** 2).sum(0)) + np.sqrt((x ** 2).sum(0))) ** 2 / size ** 2
+    scale = np.sqrt(K) / size  # s without eps, no smaller
+    close(hh, want_h, scale * tr + np.abs(want_h) * (4 * E + (K + 8) * 2.0 ** -54 * R2), "float32", "h")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_passes_of_zero_columns_and_special_values(dtype):
+    torch = _torch()
+    s = case(5003, 21, dtype, "full", True, 6)
+    s["r"][:, 3], s["y"][:, 3], s["dh"][:, 3], s["dr"][:, 3] = 0, 0, 0, 0  # padding
+    kw = dict(gate=s["gate"], post_gain=s["post"], pre_gain=s["pre"], sigmoid=True)
+    rn, hh = L1.residual_norm_fwd(s["r"], s["y"], **kw)
+    got = L1.residual_norm_bwd(rn, s["dr"], s["dh"], s["y"], **kw)
+    for x in (rn, hh, got.r, got.y, got.gate):
+        assert bool(torch.isfinite(x).all()) and not bool(x[:, 3].any())
+    s["r"][7, 5], s["y"][9, 6], s["y"][5000, 20] = float("nan"), float("inf"), float("nan")
+    bad = (5, 6, 20)
+    good = [b for b in range(21) if b not in bad]
+    rn2, hh2 = L1.residual_norm_fwd(s["r"], s["y"], **kw)
+    got2 = L1.residual_norm_bwd(rn2, s["dr"], s["dh"], s["y"], **kw)
+    for a, b in ((rn2, rn), (hh2, hh), (got2.r, got.r), (got2.y, got.y), (got2.gate, got.gate)):
+        assert torch.equal(a[:, good], b[:, good])  # the other columns have the same bits
+    for c in bad:
+        assert bool(torch.isnan(hh2[:, c]).all())
+    assert int(torch.isnan(rn2[:, 5]).sum()) == 1
+    # large gates: the logistic function at its ends
+    s = case(4500, 9, dtype, "full", False, 7)
+    s["gate"][:, 0], s["gate"][:, 1], s["gate"][:, 2], s["gate"][:, 3] = 1000.0, -1000.0, float("inf"), -float("inf")
+    rn, _ = L1.residual_norm_fwd(s["r"], s["y"], gate=s["gate"], sigmoid=True)
+    d = L1.residual_norm_bwd(rn, s["dr"], None, s["y"], gate=s["gate"], sigmoid=True)
+    whole = (s["r"].float() + s["y"].float()).to(s["r"].dtype)
+    for c in (0, 2):
+        assert torch.equal(rn[:, c], whole[:, c]) and torch.equal(d.y[:, c], s["dr"][:, c])
+    for c in (1, 3):
+        assert torch.equal(rn[:, c], s["r"][:, c]) and not bool(d.y[:, c].any())
+    assert not bool(d.gate[:, :4].any())
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_passes_in_graphs_beside_each_other(dtype):
+    """Forward and backward captured twice and replayed on two streams, with an eager call of two passes between."""
+    torch = _torch()
+    sets = []
+    for K, B in ((5003, 70), (4500, 261)):
+        s = case(K, B, dtype, "full", True, K)
+        o = [torch.empty(K, B, dtype=s["r"].dtype, device=cuda()) for _ in range(5)]
+
+        def step(s=s, o=o, stream=None):
+            kw = dict(gate=s["gate"], post_gain=s["post"], pre_gain=s["pre"], sigmoid=True, stream=stream)
+            L1.residual_norm_fwd(s["r"], s["y"], r_out=o[0], h=o[1], **kw)
+            d = L1.residual_norm_bwd(o[0], s["dr"], s["dh"], s["y"], dr=o[2], dy=o[3], dgate=o[4], **kw)
+            return [*o, d.post_gain, d.pre_gain]
+        step()
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            res = step()
+        sets.append((g, s, res, step))
+    streams = [torch.cuda.Stream() for _ in sets]
+    big, gain = torch.randn(6000, 300, device=cuda()).to(sets[0][1]["r"].dtype), torch.ones(6000, device=cuda())
+    for turn in range(4):
+        for _, s, res, _ in sets:
+            s["r"].normal_()
+            s["dh"].normal_()
+            for x in res:
+                x.fill_(float("nan"))
+        torch.cuda.synchronize()
+        for st, (g, *_) in zip(streams, sets):
+            with torch.cuda.stream(st):
+                g.replay()
+        rn, _ = L1.residual_norm_fwd(big, big, post_gain=gain, pre_gain=gain)
+        L1.residual_norm_bwd(rn, big, big, big, post_gain=gain, pre_gain=gain)
+        torch.cuda.synchronize()
+        kept = [[x.clone() for x in res] for _, _, res, _ in sets]
+        for (_, _, _, step), k in zip(sets, kept):
+            eager = step(stream=streams[1])
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(eager, k))
