@@ -708,7 +708,7 @@ int l1csr_preference_loss_scaled(int32_t C, int32_t B, int dtype, const void *lo
  * Such tokens take no part in the gradients either.  D = the inputs of the first layer; a table tied to the
  * output layer is that layer's W[C][K] (V = C, D = K).  scale is finite.
  *
- * l1csr_embedding_fwd: E of `dtype`, X of x_dtype: the same or fp32; one rounding.
+ * l1csr_embedding_fwd: E of `dtype`, X of x_dtype: the same or fp32; the product is fp32, rounded once to x_dtype.
  * l1csr_embedding_csr_fwd: the table kept in CSR (V x D, fp32); X fp32.
  * l1csr_embedding_plan: the tokens' order (by token, then by position), which the gradients add up in, into the
  *   caller's buffer plan of l1csr_workspace_bytes(L1CSR_OP_EMBEDDING_PLAN, V, 0, 0, B) bytes.  The plan depends on
@@ -744,7 +744,8 @@ int l1csr_embedding_masked_bwd(int32_t V, int32_t D, int64_t nnz, const int32_t 
  * r is the residual, y the block's output, h the next block's input.  y NULL: r' = r, the norm alone (r_out NULL).
  * All matrices are of `dtype`; the gains float [K].  gate_kind: L1CSR_GATE_NONE (a = 1), L1CSR_GATE_ROW (gate is
  * float [K], one for all tokens) or L1CSR_GATE_FULL (gate [K][ldg] of `dtype`); a(g) = g, or the logistic function
- * of g with gate_sigmoid.  h comes from the unrounded r'.  Sums are in double; eps > 0, alpha finite.
+ * of g with gate_sigmoid.  h comes from the unrounded r'.  Sums over a column are in double, those over the tokens fp32
+ * over up to 512 of them and double over those; eps > 0, alpha finite.
  * r_out and h may each be r or y themselves (with the same leading dimension), but not each other.
  *
  * l1csr_residual_norm_bwd: from r_out (r' as stored; pre_gain given), dr_out (d loss / d r' from its further uses; NULL: 0,
@@ -782,10 +783,10 @@ int l1csr_residual_norm_bwd(int32_t K, int32_t B, int dtype, const void *r_out, 
  * pointers; NULL: in place) with ld_out (NULL: cols) and dtype_out (NULL: dtype; each the tensor's type or fp32)
  * takes the results.  grad_scale > 0 is a factor that the gradients hold (the losses' grad_scale, a power of two
  * best): it is taken out.  stats[2] (device) = norm, f (l1csr_grad_norm: norm, 1 / grad_scale).
- * max_norm >= 0 (infinity: no limit), eps > 0.  Squares and their sum are in double, f multiplies in double, one
- * rounding.  A norm that is not finite gives what the formula gives (an infinite one 0 or NaN, NaN everywhere for a
- * NaN); with zero_nonfinite != 0 it gives f = 0 and zeros everywhere instead, so that nothing of such a step
- * reaches the momentum or the weights.  No tensors: norm 0.
+ * max_norm >= 0 (infinity: no limit), eps > 0.  Squares and their sum are in double, f multiplies in double; the
+ * product is rounded to fp32 and from there to the result's type.  A norm that is not finite gives what the formula
+ * gives (an infinite one 0 or NaN, NaN everywhere for a NaN); with zero_nonfinite != 0 it gives f = 0 and zeros
+ * everywhere instead, so that nothing of such a step reaches the momentum or the weights.  No tensors: norm 0.
  * A result may be its own tensor (same type and leading dimension), but nothing written may overlap anything else
  * (L1CSR_EINVAL; a tensor given twice and columns of one buffer that cross are refused).
  * ws, 16-byte aligned, as l1csr_workspace_bytes(L1CSR_OP_GRAD_NORM, n, 0, 0, 0).  Results are reproducible.

@@ -154,7 +154,8 @@ __device__ __forceinline__ int key_of(int token, int V) { return (int)min((unsig
 
 // Up to kCounted tokens are ranked in one launch: a workgroup has all keys in LDS and kOwn tokens, each by 64 threads, of which
 // every one counts the smaller keys (and the equal ones ahead) of its share, four a step: 1656 tokens take 3.6 us, 4096 4.2
-// and 8192 8.8, by runs and their merge 12.5, 14.0 and 14.7.  It grows with the square: larger batches go by runs.
+// and 8192 8.8, by runs and their merge 12.5, 14.0 and 14.7.  It grows with the square: larger batches go by runs.  (The
+// limit is that of the array of keys, 32 KB; where both take the same time lies higher and has not been measured.)
 constexpr int kCounted = 8192, kOwn = 16;
 __global__ __launch_bounds__(kRankThreads) void count_kernel(int V, int B, const int *__restrict__ tokens,
                                                              int *__restrict__ rank, int *__restrict__ sorted) {

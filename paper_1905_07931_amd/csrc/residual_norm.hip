@@ -14,8 +14,9 @@
 // - two passes, for longer columns: both means of a call come from one pass over ranges of rows.  Forward: with
 //   x = alpha a w_post y, r' = r + q x and sum r'^2 = sum r^2 + 2 q sum r x + q^2 sum x^2.  Backward:
 //   sum k y t = sum k y dr' + s sum k y u - s^3 c sum k y r'.
-// Sums over a column are in double (the forward expansion cancels where a block takes back what the residual holds), in
-// a fixed order.
+// Sums over a column are in double (the forward expansion cancels where a block takes back what the residual holds; squares
+// of bf16 values leave fp32), in a fixed order.  Sums over tokens are fp32 over the columns of a wave, 512 at most, and double over
+// those.
 #include <algorithm>
 #include <type_traits>
 
@@ -979,12 +980,13 @@ bool short_enough(const norm_args &a) {
 }
 
 // Strips of up to 2048 rows leave room for several workgroups a CU (us, strips and two passes, gate and both norms:
-// fp32 1024 x 8192 45 and 64, 2048 x 8192 105 and 112, 2000 x 64 13 and 17, bf16 2048 x 8192 49 and 63).  Up to 4096 rows one
+// fp32 1024 x 8192 45 and 64, 2048 x 8192 105 and 112, 2000 x 64 13 and 17, bf16 2048 x 8192 50 and 66).  Up to 4096 rows one
 // workgroup fills a CU and nothing hides its reductions: that still pays where the launches and the join are most of the
-// time (fp32 2800 x 64 17 and 17, 2800 x 1024 31 and 35, bf16 4000 x 256 20 and 22, 4000 x 1024 28 and 29), but not for
-// large matrices (fp32 4096 x 8192 259 and 217, bf16 124 and 113), nor for the longest fp32 columns, which are held four a
-// thread at least (4000 x 64 23.6 and 17.4, 4000 x 512 33 and 27; rows of under 64 bytes are soon read: 4000 x 8 11 and
-// 17).  Longer columns would spill.
+// time (fp32 2800 x 64 17 and 17, 2800 x 1024 31 and 35; bf16, inputs in the caches, 4000 x 256 18.7 and 20.5, 4000 x 1024 24
+// and 28, but 24.5 and 22, 41 and 29 from cold memory), but not for large matrices (fp32 4096 x 8192 259 and 217, bf16 124 and
+// 113), nor for the longest fp32 columns, which are held four a thread at least (4000 x 64 23.6 and 17.4, 4000 x 512 33 and 27;
+// rows of under 64 bytes are soon read: 4000 x 8 11 and 17).  Longer columns would spill.  Everything is read once and
+// still takes 1.4 to 1.9 times its bytes (5.1 TB/s, cold): a workgroup's loads wait while it takes its means.
 constexpr int kStripRows = 2048, kMostStripRows = 4096, kMostFp32Rows = 2816;
 constexpr int64_t kStripBytes = 32 << 20;  // of a matrix of more than kStripRows rows
 constexpr int kShortRow = 64;              // bytes
@@ -996,7 +998,8 @@ int forward_rows(int K, int B, int dtype, strip_grid *g) {
 }
 
 // Backward strips hold two matrices and leave three sums a row each (37 % of a matrix in pieces of 32 bytes).  us, strips
-// and two passes: bf16 1024 x 8192 49 and 70, 300 x 16384 40 and 59; fp32 94 and 100, 48 and 69; but fp32 2048 x 8192 252
+// and two passes (from cold memory the strips take 73 and 46 in bf16, 98 and 55 in fp32, 1.8 to 3 times their bytes): bf16
+// 1024 x 8192 49 and 70, 300 x 16384 40 and 59; fp32 94 and 100, 48 and 69; but fp32 2048 x 8192 252
 // and 163, 100 x 100000 (3125 strips, whose sums few rows join) 160 and 122.  Of more than 2048 rows only those of
 // under 64 bytes: fp32 4000 x 8 21 and 24, 2000 x 64 24.2 and 24.5, 2800 x 64 37 and 25, 4000 x 64 50 and 25, 4000 x 512 62
 // and 40, bf16 2000 x 64 22 and 27, 4000 x 64 40 and 28, 4000 x 512 48 and 43, 2800 x 256 36 and 37.
