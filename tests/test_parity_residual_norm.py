@@ -443,179 +443,6 @@ def test_logistic_gates_at_the_ends_of_their_type(K, B, post, dtype):
             assert torch.equal(d.y[opened], d.r[opened]) and not bool(d.y[closed].any())
 
 
-# shapes that take the strips and shapes that take the two passes, of vectors and of single columns
-BOTH_WAYS = [(50, 9), (300, 2), (5003, 9), (9000, 3)]
-
-
-@pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("post", [False, True])
-@pytest.mark.parametrize("K,B", BOTH_WAYS)
-def test_logistic_gates_at_the_ends_of_their_type(K, B, post, dtype):
-    """A gate of the type's lowest value is closed, one of its highest open, and neither touches anything else."""
-    torch = _torch()
-    for kind in ("full", "row"):
-        s = case(K, B, dtype, kind, post, 7)
-        top = torch.finfo(s["gate"].dtype).max
-        at = (slice(None), (0, 1)) if kind == "full" else ((3, K - 1),)  # open, closed: tokens, or features
-        s["gate"][at] = torch.tensor([top, -top], dtype=s["gate"].dtype, device=cuda())
-        kw = dict(gate=s["gate"], post_gain=s["post"], pre_gain=s["pre"], sigmoid=True)
-        rn, hh = L1.residual_norm_fwd(s["r"], s["y"], **kw)
-        d = L1.residual_norm_bwd(rn, s["dr"], s["dh"], s["y"], **kw)
-        for x in (rn, hh, d.r, d.y, d.gate, d.pre_gain, *([d.post_gain] if post else [])):
-            assert bool(torch.isfinite(x).all()), kind
-        assert not bool(d.gate[at].any())
-        opened, closed = ((slice(None), 0), (slice(None), 1)) if kind == "full" else (3, K - 1)
-        assert torch.equal(rn[closed], s["r"][closed])
-        if not post:  # (with a post gain y's part in its own mean has a gradient too)
-            assert torch.equal(rn[opened], (s["r"].float() + s["y"].float()).to(s["r"].dtype)[opened])
-            assert torch.equal(d.y[opened], d.r[opened]) and not bool(d.y[closed].any())
-
-
-@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
-@pytest.mark.parametrize("size", [1e-12, 1e12, 1e20, 1e30])
-@pytest.mark.parametrize("K,B", [(300, 20), (2000, 24), (10, 1), (5003, 21), (9000, 3)])
-def test_magnitudes_in_strips_and_passes(K, B, size, dtype):
-    """Values whose squares leave fp32's range, in the types that have them."""
-    s = case(K, B, dtype, "row", True, 4)
-    s["r"] *= size
-    s["y"] *= size
-    eps = float(np.float32(1e-38))
-    args = [h64(s[k]) for k in ("y", "gate", "post", "pre")]
-    kw = dict(gate=s["gate"], post_gain=s["post"], pre_gain=s["pre"], eps=1e-38)
-    rn, hh = L1.residual_norm_fwd(s["r"], s["y"], **kw)
-    want_r, want_h, tr, th = forward(h64(s["r"]), *args, 1.0, eps, False)
-    close(rn, want_r, tr, dtype, "r'")
-    close(hh, want_h, th, dtype, "h")
-    got = L1.residual_norm_bwd(rn, s["dr"], s["dh"], s["y"], **kw)
-    for name, (w, tol) in backward(h64(rn), h64(s["dr"]), h64(s["dh"]), *args, 1.0, eps, False).items():
-        x = getattr(got, name)
-        close(x, w, tol, str(x.dtype).split(".")[1], "d" + name)
-
-
-@pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("K,B", [(300, 20), (2000, 24), (10, 1), (5003, 21), (9000, 3)])
-def test_a_block_whose_gain_takes_it_past_the_squares(K, B, dtype):
-    """h comes from the unrounded r', whose squares leave fp32 (and which leaves fp16 itself)."""
-    s = case(K, B, dtype, "none", True, 5)
-    s["post"] *= 1e25
-    eps = float(np.float32(1e-6))
-    _, hh = L1.residual_norm_fwd(s["r"], s["y"], post_gain=s["post"], pre_gain=s["pre"])
-    _, want, _, th = forward(h64(s["r"]), h64(s["y"]), None, h64(s["post"]), h64(s["pre"]), 1.0, eps, False)
-    close(hh, want, th, dtype, "h")
-
-
-# shapes that take the strips and shapes that take the two passes, of vectors and of single columns
-BOTH_WAYS = [(50, 9), (300, 2), (5003, 9), (9000, 3)]
-
-
-@pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("post", [False, True])
-@pytest.mark.parametrize("K,B", BOTH_WAYS)
-def test_logistic_gates_at_the_ends_of_their_type(K, B, post, dtype):
-    """A gate of the type's lowest value is closed, one of its highest open, and neither touches anything else."""
-    torch = _torch()
-    for kind in ("full", "row"):
-        s = case(K, B, dtype, kind, post, 7)
-        top = torch.finfo(s["gate"].dtype).max
-        at = (slice(None), (0, 1)) if kind == "full" else ((3, K - 1),)  # open, closed: tokens, or features
-        s["gate"][at] = torch.tensor([top, -top], dtype=s["gate"].dtype, device=cuda())
-        kw = dict(gate=s["gate"], post_gain=s["post"], pre_gain=s["pre"], sigmoid=True)
-        rn, hh = L1.residual_norm_fwd(s["r"], s["y"], **kw)
-        d = L1.residual_norm_bwd(rn, s["dr"], s["dh"], s["y"], **kw)
-        for x in (rn, hh, d.r, d.y, d.gate, d.pre_gain, *([d.post_gain] if post else [])):
-            assert bool(torch.isfinite(x).all()), kind
-        assert not bool(d.gate[at].any())
-        opened, closed = ((slice(None), 0), (slice(None), 1)) if kind == "full" else (3, K - 1)
-        assert torch.equal(rn[closed], s["r"][closed])
-        if not post:  # (with a post gain y's part in its own mean has a gradient too)
-            assert torch.equal(rn[opened], (s["r"].float() + s["y"].float()).to(s["r"].dtype)[opened])
-            assert torch.equal(d.y[opened], d.r[opened]) and not bool(d.y[closed].any())
-
-
-@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
-@pytest.mark.parametrize("size", [1e-12, 1e12, 1e20, 1e30])
-@pytest.mark.parametrize("K,B", [(300, 20), (2000, 24), (10, 1), (5003, 21), (9000, 3)])
-def test_magnitudes_in_strips_and_passes(K, B, size, dtype):
-    """Values whose squares leave fp32's range, in the types that have them."""
-    s = case(K, B, dtype, "row", True, 4)
-    s["r"] *= size
-    s["y"] *= size
-    eps = float(np.float32(1e-38))
-    args = [h64(s[k]) for k in ("y", "gate", "post", "pre")]
-    kw = dict(gate=s["gate"], post_gain=s["post"], pre_gain=s["pre"], eps=1e-38)
-    rn, hh = L1.residual_norm_fwd(s["r"], s["y"], **kw)
-    want_r, want_h, tr, th = forward(h64(s["r"]), *args, 1.0, eps, False)
-    close(rn, want_r, tr, dtype, "r'")
-    close(hh, want_h, th, dtype, "h")
-    got = L1.residual_norm_bwd(rn, s["dr"], s["dh"], s["y"], **kw)
-    for name, (w, tol) in backward(h64(rn), h64(s["dr"]), h64(s["dh"]), *args, 1.0, eps, False).items():
-        x = getattr(got, name)
-        close(x, w, tol, str(x.dtype).split(".")[1], "d" + name)
-
-
-@pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("K,B", [(300, 20), (2000, 24), (10, 1), (5003, 21), (9000, 3)])
-def test_a_block_whose_gain_takes_it_past_the_squares(K, B, dtype):
-    """h comes from the unrounded r', whose squares leave fp32 (and which leaves fp16 itself)."""
-    s = case(K, B, dtype, "none", True, 5)
-    s["post"] *= 1e25
-    eps = float(np.float32(1e-6))
-    _, hh = L1.residual_norm_fwd(s["r"], s["y"], post_gain=s["post"], pre_gain=s["pre"])
-    _, want, _, th = forward(h64(s["r"]), h64(s["y"]), None, h64(s["post"]), h64(s["pre"]), 1.0, eps, False)
-    close(hh, want, th, dtype, "h")
-
-
-@pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("K,B", [(300, 20), (5003, 21)])
-def test_infinite_residuals_and_gates(K, B, dtype):
-    """r' is infinite where one of its terms is: its column's h is 0 but there, whatever the other term; where r' is NaN (both
-    infinite, of unlike signs) the column is."""
-    torch = _torch()
-    inf = float("inf")
-    s = case(K, B, dtype, "full", True, 8)
-    #          column: r, gate, y at row 7
-    put = {3: (inf, 1, -1), 4: (-inf, 1, 1), 5: (inf, 1, 0), 6: (inf, 0, 1), 8: (0, inf, 1), 9: (2, inf, -1), 10: (inf, inf, 1)}
-    for c, (r, gate, y) in put.items():
-        s["r"][7, c], s["gate"][7, c], s["y"][7, c] = r, gate, y
-    s["r"][7, 12], s["gate"][7, 12], s["y"][7, 12] = -inf, inf, 1
-    rn, hh = L1.residual_norm_fwd(s["r"], s["y"], gate=s["gate"], post_gain=s["post"].abs_(), pre_gain=s["pre"])
-    others = [k for k in range(K) if k != 7]
-    for c, (r, gate, y) in put.items():
-        assert float(rn[7, c]) == (r if abs(r) == inf else y * gate), c
-        assert bool(torch.isnan(hh[7, c])) and not bool(hh[others, c].any()), c
-    assert bool(torch.isnan(rn[7, 12])) and bool(torch.isnan(hh[:, 12]).all())
-    rest = [c for c in range(B) if c not in put and c != 12]
-    assert bool(torch.isfinite(hh[:, rest]).all()) and bool(torch.isfinite(rn[others]).all())
-
-
-# shapes that take the strips and shapes that take the two passes, of vectors and of single columns
-BOTH_WAYS = [(50, 9), (300, 2), (5003, 9), (9000, 3)]
-
-
-@pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("post", [False, True])
-@pytest.mark.parametrize("K,B", BOTH_WAYS)
-def test_logistic_gates_at_the_ends_of_their_type(K, B, post, dtype):
-    """A gate of the type's lowest value is closed, one of its highest open, and neither touches anything else."""
-    torch = _torch()
-    for kind in ("full", "row"):
-        s = case(K, B, dtype, kind, post, 7)
-        top = torch.finfo(s["gate"].dtype).max
-        at = (slice(None), (0, 1)) if kind == "full" else ((3, K - 1),)  # open, closed: tokens, or features
-        s["gate"][at] = torch.tensor([top, -top], dtype=s["gate"].dtype, device=cuda())
-        kw = dict(gate=s["gate"], post_gain=s["post"], pre_gain=s["pre"], sigmoid=True)
-        rn, hh = L1.residual_norm_fwd(s["r"], s["y"], **kw)
-        d = L1.residual_norm_bwd(rn, s["dr"], s["dh"], s["y"], **kw)
-        for x in (rn, hh, d.r, d.y, d.gate, d.pre_gain, *([d.post_gain] if post else [])):
-            assert bool(torch.isfinite(x).all()), kind
-        assert not bool(d.gate[at].any())
-        opened, closed = ((slice(None), 0), (slice(None), 1)) if kind == "full" else (3, K - 1)
-        assert torch.equal(rn[closed], s["r"][closed])
-        if not post:  # (with a post gain y's part in its own mean has a gradient too)
-            assert torch.equal(rn[opened], (s["r"].float() + s["y"].float()).to(s["r"].dtype)[opened])
-            assert torch.equal(d.y[opened], d.r[opened]) and not bool(d.y[closed].any())
-
-
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
 @pytest.mark.parametrize("size", [1e-12, 1e12, 1e20, 1e30])
 @pytest.mark.parametrize("K,B", [(300, 20), (2000, 24), (10, 1), (5003, 21), (9000, 3)])
